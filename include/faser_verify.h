@@ -109,6 +109,42 @@ typedef struct fsr_rank_params {
     int32_t reserved; /* must be 0 */
 } fsr_rank_params;
 
+/* Static shape of the calls on a latent cache. */
+typedef struct fsr_latent_params {
+    int32_t B;         /* requests in the batch (>= 0) */
+    int32_t N_cap;     /* rows allocated: of q/out or of the new rows (cu_q[B] <= N_cap); of the gathered rows (cu_k[B] <= N_cap) */
+    int32_t H;         /* query heads; they all read the same cache row (attention only) */
+    int32_t D_latent;  /* elements of a token's latent vector: any that fill 16-byte pieces; attention: 256 or 512 */
+    int32_t D_rope;    /* elements of its position part, likewise; attention: 32 or 64 */
+    int32_t P;         /* tokens per page, any */
+    int32_t max_pages; /* row stride of block_tables */
+    int32_t n_pages;   /* pages in the cache */
+    int32_t dtype;     /* FSR_F32 or FSR_BF16: element type of the cache, the rows and q */
+    int32_t out_dtype; /* attention: FSR_F32 always allowed; FSR_BF16 with bf16 inputs */
+    float scale;       /* attention: softmax scale, > 0 */
+    int32_t max_q_len; /* attention: upper bound on the rows of any one request, or 0 if unknown.  A hint, as in
+                          fsr_attn_params: requests with more rows are still computed correctly. */
+    int32_t max_workgroups; /* 0, or the compute units that the call's stream owns (as in fsr_attn_params) */
+    int32_t reserved;  /* must be 0 */
+} fsr_latent_params;
+
+/* Static shape of one call of latent attention in its expanded form. */
+typedef struct fsr_expanded_params {
+    int32_t B;         /* requests in the batch (>= 0) */
+    int32_t N_cap;     /* rows allocated in q/out; cu_q[B] <= N_cap */
+    int32_t T_cap;     /* rows allocated in kv/k_rope; cu_k[B] <= T_cap */
+    int32_t H;         /* heads */
+    int32_t D_nope;    /* elements of a head's key that carry no position */
+    int32_t D_rope;    /* elements of the position part, one row for all heads */
+    int32_t D_v;       /* elements of a head's value: D_nope/D_rope/D_v are 128/64/128 or 64/32/64 */
+    int32_t dtype;     /* FSR_F32 or FSR_BF16: element type of q, kv, k_rope */
+    int32_t out_dtype; /* FSR_F32 always allowed; FSR_BF16 with bf16 inputs */
+    float scale;       /* softmax scale, > 0 */
+    int32_t max_q_len; /* upper bound on the rows of any one request, or 0 if unknown (a hint, as above) */
+    int32_t max_workgroups; /* 0, or the compute units that the call's stream owns */
+    int32_t reserved;  /* must be 0 */
+} fsr_expanded_params;
+
 /* Static description of the last failure on the calling thread ("" if none).  Host. */
 const char* fsr_last_error(void);
 
@@ -443,6 +479,86 @@ int fsr_frontier_commit(const int32_t* spec_lens, const int32_t* chunk_len,
                         const int32_t* emitted, int32_t emitted_stride, int32_t* pos,
                         int32_t* active, int32_t* n_out, int32_t* acc_total, int32_t* out_tokens,
                         int32_t B, int32_t out_stride, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Caches that several readers share.
+ *
+ * Latent caches: a target model may store, per token, one latent vector from which the keys and values of all heads are linear
+ * images, followed by a key part that carries the position.  The verification step (Sec. 2.1) over such a cache:
+ *     fsr_latent_append     the call's rows enter the paged cache [n_pages, P, D_latent + D_rope]
+ *     fsr_latent_attention  queries that have been taken into the latent's space attend over it (few rows a request), or
+ *     fsr_latent_gather     the cached rows come back as contiguous rows, the caller's up-projection makes keys and values
+ *     fsr_latent_attention_expanded   of them, and many rows a request attend over those (a chunk of a prompt).
+ *
+ * fsr_latent_append: row j of request i (row cu_q[i] + j) is the token at position ctx_lens[i] + j; it is copied, bit for bit.
+ *   latent_new [N_cap, D_latent], rope_new [N_cap, D_rope] dtype; rows >= cu_q[B] are not read
+ *   Positions without a page and page ids outside the pool are skipped, as in fsr_kv_append.
+ * fsr_latent_gather: row cu_k[i] + t of latent_out [N_cap, D_latent] and rope_out [N_cap, D_rope] is position t of request i, for
+ *   t < cu_k[i+1] - cu_k[i]; rows >= cu_k[B] are not written.  Positions behind the table are read as zeros, page ids are
+ *   clamped into the pool.
+ * Both: pointers 16-byte aligned, no workspace.
+ */
+int fsr_latent_append(const void* latent_new, const void* rope_new, void* cache, const int32_t* block_tables, const int32_t* ctx_lens,
+                      const int32_t* cu_q, const fsr_latent_params* p /*host*/, void* stream);
+int fsr_latent_gather(const void* cache, const int32_t* block_tables, const int32_t* cu_k, void* latent_out, void* rope_out,
+                      const fsr_latent_params* p /*host*/, void* stream);
+
+/* Workspace bytes needed by fsr_latent_attention for shapes up to *p (host query); covers every smaller B, N_cap and H. */
+int fsr_latent_workspace_bytes(const fsr_latent_params* p /*host*/, size_t* out_bytes /*host*/);
+
+/*
+ * Verification attention over a latent cache.  With x_t the cache row of position t of request i, row j of its q_i rows is at
+ * position c + j (c = ctx_lens[i]) and attends to positions 0 .. c + j:
+ *     out[row, h, :] = softmax_t(scale * q[row, h, :] . x_t) . x_t[0 : D_latent]
+ *   q     [N_cap, H, D_latent + D_rope] dtype: a head's query, its position-free part taken into the latent's space
+ *   cache [n_pages, P, D_latent + D_rope] dtype; the call's own rows are in it already (fsr_latent_append)
+ *   block_tables, ctx_lens, cu_q as for fsr_verify_attention
+ *   out   [N_cap, H, D_latent] out_dtype; rows >= cu_q[B] are not written
+ *   lse   [N_cap, H] float32, nullable: natural-log sum of exp of the scaled scores
+ *   workspace >= fsr_latent_workspace_bytes(p) bytes, 256-byte aligned
+ * Scores, softmax statistics and sums are fp32.  With bf16 out the weights enter the second product in bf16 (an error of the size
+ * of the output's own rounding); with fp32 out of bf16 inputs they are carried as a hi+lo pair.  Values that a row does not see
+ * do not reach it, infinities and NaN included.
+ */
+int fsr_latent_attention(const void* q, const void* cache, const int32_t* block_tables, const int32_t* ctx_lens, const int32_t* cu_q,
+                         void* out, float* lse, const fsr_latent_params* p /*host*/, void* workspace, size_t ws_bytes, void* stream);
+
+/* Workspace bytes needed by fsr_latent_attention_expanded for shapes up to *p (host query). */
+int fsr_expanded_workspace_bytes(const fsr_expanded_params* p /*host*/, size_t* out_bytes /*host*/);
+
+/*
+ * Latent attention in its expanded form.  Request i has n rows (cu_q) and L keys (cu_k); its rows are the last n positions, so
+ * row j attends to keys 0 .. L - n + j:
+ *     z[t] = scale * (q[row, h, 0 : D_nope] . kv[t, h, 0 : D_nope] + q[row, h, D_nope :] . k_rope[t])
+ *     out[row, h, :] = softmax_t(z) . kv[t, h, D_nope :]
+ * A row that sees no key (n > L) gets zeros and lse = -inf.
+ *   q      [N_cap, H, D_nope + D_rope]   kv [T_cap, H, D_nope + D_v]   k_rope [T_cap, D_rope]   dtype, 16-byte aligned
+ *   cu_q, cu_k [B+1] int32 offsets of the rows and of the keys
+ *   out    [N_cap, H, D_v] out_dtype; rows >= cu_q[B] are not written      lse [N_cap, H] float32, nullable
+ * Accuracy as for fsr_latent_attention.
+ */
+int fsr_latent_attention_expanded(const void* q, const void* kv, const void* k_rope, const int32_t* cu_q, const int32_t* cu_k, void* out,
+                                  float* lse, const fsr_expanded_params* p /*host*/, void* workspace, size_t ws_bytes, void* stream);
+
+/* Workspace bytes needed by fsr_verify_attention_shared for shapes up to *p (host query). */
+int fsr_shared_workspace_bytes(const fsr_attn_params* p /*host*/, size_t* out_bytes /*host*/);
+
+/*
+ * fsr_verify_attention for a batch whose requests share prefixes.  Requests cu_groups[g] .. cu_groups[g+1]-1 form group g; their
+ * first prefix_lens[g] positions hold the same tokens, and are read once for all of the group's rows, through the block table
+ * of its first request (any length: where the prefix ends inside a page, the other requests' copies of that page hold the same
+ * values).  Positions from prefix_lens[g] on are read through a request's own table.  Results are those of
+ * fsr_verify_attention, up to the order of sums and the rounding of the weights (see fsr_latent_attention).
+ *   cu_groups   [n_groups+1] int32, ascending; requests outside cu_groups[0] .. cu_groups[n_groups]-1 get no output
+ *   prefix_lens [n_groups] int32, 0 allowed.  A request whose ctx_lens is below its group's prefix counts as one of exactly the
+ *               prefix: all its rows see the prefix whole, and row j its own positions prefix .. prefix + j.
+ *   q, caches, block_tables, ctx_lens, cu_q, out, lse and *p as for fsr_verify_attention (any page size, any H_q / H_kv).
+ *   workspace   >= fsr_shared_workspace_bytes(p) bytes, 256-byte aligned
+ */
+int fsr_verify_attention_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                                const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* cu_groups, const int32_t* prefix_lens,
+                                int32_t n_groups, void* out, float* lse, const fsr_attn_params* p /*host*/, void* workspace,
+                                size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
  * Measurement aid (not a step of the verification path): one launch that reads `bytes` bytes at

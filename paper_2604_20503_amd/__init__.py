@@ -11,6 +11,7 @@ from .binding import (  # noqa: F401
     attn_path,
     attn_plan,
     attn_workspace_bytes,
+    expanded_workspace_bytes,
     frontier_commit,
     frontier_init,
     frontier_plan,
@@ -18,17 +19,24 @@ from .binding import (  # noqa: F401
     kv_append,
     kv_append_kv8,
     last_error,
+    latent_append,
+    latent_attention,
+    latent_attention_expanded,
+    latent_gather,
+    latent_workspace_bytes,
     library_path,
     load_library,
     prune_compact,
     prune_restore,
     prune_scatter,
+    shared_workspace_bytes,
     spec_accept,
     survivor_compact,
     survivor_mask,
     topk_rank_check,
     verify_attention,
     verify_attention_kv8,
+    verify_attention_shared,
     verify_attention_static,
     version,
 )
@@ -38,4 +46,6 @@ __all__ = [
     "FsrError", "accept_workspace_bytes", "attn_path", "attn_plan", "attn_workspace_bytes", "frontier_commit", "frontier_init",
     "frontier_plan", "hbm_read_probe", "kv_append", "kv_append_kv8", "last_error", "library_path", "load_library", "prune_compact", "prune_restore", "prune_scatter",
     "spec_accept", "survivor_compact", "survivor_mask", "topk_rank_check", "verify_attention", "verify_attention_kv8", "verify_attention_static", "verify_chunked", "version",
+    "expanded_workspace_bytes", "latent_append", "latent_attention", "latent_attention_expanded", "latent_gather", "latent_workspace_bytes",
+    "shared_workspace_bytes", "verify_attention_shared",
 ]

@@ -28,6 +28,8 @@ SYMBOLS = [
     "fsr_verify_attention_planned", "fsr_verify_attention_static", "fsr_static_scratch_bytes", "fsr_verify_attention", "fsr_verify_attention_kv8", "fsr_verify_attention_kv8_planned", "fsr_kv_append", "fsr_kv_append_kv8",
     "fsr_accept_workspace_bytes", "fsr_spec_accept", "fsr_prune_compact", "fsr_prune_restore",
     "fsr_prune_scatter", "fsr_survivor_mask", "fsr_survivor_compact", "fsr_topk_rank_check", "fsr_frontier_init", "fsr_frontier_plan", "fsr_frontier_commit",
+    "fsr_latent_append", "fsr_latent_gather", "fsr_latent_workspace_bytes", "fsr_latent_attention", "fsr_expanded_workspace_bytes",
+    "fsr_latent_attention_expanded", "fsr_shared_workspace_bytes", "fsr_verify_attention_shared",
     "fsr_hbm_read_probe",
 ]
 
@@ -51,6 +53,12 @@ _ARGUMENTS = {
     "fsr_survivor_compact": f"i:accepted_len i:cu_q b:keep_mask {_MAPS}",
     "fsr_topk_rank_check": "t:logits i:draft_tokens i:cu_q i:cu_d i:rank b:keep_mask S:params n:stream",
     "fsr_prune_restore": "t:compact i:dst_row t:restored b:has_value n:row_bytes n:N n:pad_word n:stream",
+    "fsr_latent_append": f"t:latent t:rope t:cache {_LENGTHS} i:cu_q S:params n:stream",
+    "fsr_latent_gather": "t:cache i:block_tables i:cu_k t:latent t:rope S:params n:stream",
+    "fsr_latent_attention": f"t:q t:cache {_LENGTHS} i:cu_q t:out f:lse S:params t:workspace n:ws_bytes n:stream",
+    "fsr_latent_attention_expanded": "t:q t:kv t:k_rope i:cu_q i:cu_k t:out f:lse S:params t:workspace n:ws_bytes n:stream",
+    "fsr_verify_attention_shared":
+        f"{_ATTENTION} {_LENGTHS} i:cu_q i:cu_groups i:prefix_lens n:n_groups t:out f:lse S:params t:workspace n:ws_bytes n:stream",
     "fsr_prune_scatter": "t:compact i:src_row i:n_rows t:out n:row_bytes n:N_cap n:stream",
 }
 
@@ -80,6 +88,17 @@ class PruneParams(ctypes.Structure):
 
 class RankParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "N_cap", "D_cap", "V", "K", "dtype", "reserved")]
+
+
+class LatentParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("B", "N_cap", "H", "D_latent", "D_rope", "P", "max_pages", "n_pages", "dtype", "out_dtype")] + \
+               [("scale", ctypes.c_float), ("max_q_len", ctypes.c_int32), ("max_workgroups", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class ExpandedParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "N_cap", "T_cap", "H", "D_nope", "D_rope", "D_v", "dtype", "out_dtype")] + \
+               [("scale", ctypes.c_float), ("max_q_len", ctypes.c_int32), ("max_workgroups", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -363,6 +382,182 @@ def kv_append_kv8(k_new, v_new, k_cache, v_cache, k_scale, v_scale, block_tables
     if v_new.shape != k_new.shape or v_cache.shape != k_cache.shape or k_cache.dtype != torch.uint8 or v_cache.dtype != torch.uint8:
         raise ValueError("rows must share a shape; caches must be uint8 tensors of one shape")
     _call("fsr_kv_append_kv8", k_new, v_new, k_cache, v_cache, k_scale, v_scale, block_tables, ctx_lens, cu_q, p)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# caches that several readers share
+# ---------------------------------------------------------------------------------------------------------------
+def _on_current_device(**tensors):
+    """The launch goes to the current device: tensors that live elsewhere are refused here."""
+    here = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must live on the GPU")
+        if here is None:
+            here = torch._C._cuda_getDevice()
+        if t.device.index != here:
+            raise ValueError(f"{name} lives on {t.device}, the current device is cuda:{here}")
+
+
+def _check_offsets(B, block_tables=None, **offsets):
+    if block_tables is not None and (block_tables.dim() != 2 or block_tables.shape[0] != B):
+        raise ValueError(f"block_tables must be [{B}, max_pages], got {tuple(block_tables.shape)}")
+    for name, t in offsets.items():
+        if tuple(t.shape) != (B + 1,):
+            raise ValueError(f"{name} must have {B + 1} entries, got {tuple(t.shape)}")
+
+
+def _outputs(shape, out, lse, out_dtype, dtype, device):
+    """(out, its type): the caller's buffers checked, or a new one."""
+    out_dtype = out_dtype or (out.dtype if out is not None else dtype)
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=device)
+    elif tuple(out.shape) != tuple(shape) or out.dtype != out_dtype:
+        raise ValueError(f"out must be {tuple(shape)} of {out_dtype}, got {tuple(out.shape)} of {out.dtype}")
+    if lse is not None and tuple(lse.shape) != tuple(shape[:2]):
+        raise ValueError(f"lse must be {tuple(shape[:2])}, got {tuple(lse.shape)}")
+    return out, out_dtype
+
+
+def _scratch(size_of, params, workspace, device):
+    """(workspace, bytes): the caller's (checked by the call itself), or a new one."""
+    if workspace is None:
+        workspace = torch.empty(_workspace_of(size_of, params), dtype=torch.uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _latent_params(cache, block_tables, B, N_cap, H, D_latent, dtype, out_dtype, scale=1.0, max_q_len=0, max_workgroups=0) -> LatentParams:
+    if cache.dim() != 3 or not 0 < D_latent < cache.shape[2]:
+        raise ValueError(f"cache must be [n_pages, P, D_latent + D_rope] with D_latent = {D_latent}, got {tuple(cache.shape)}")
+    n_pages, P, D = cache.shape
+    return LatentParams(B=B, N_cap=N_cap, H=H, D_latent=D_latent, D_rope=D - D_latent, P=P, max_pages=block_tables.shape[1], n_pages=n_pages,
+                        dtype=_code(dtype), out_dtype=_code(out_dtype), scale=float(scale), max_q_len=int(max_q_len),
+                        max_workgroups=int(max_workgroups), reserved=0)
+
+
+def latent_append(latent, rope, cache, block_tables, ctx_lens, cu_q):
+    """fsr_latent_append: store the call's rows, latent [N_cap, D_latent] and rope [N_cap, D_rope], into the paged latent cache
+    [n_pages, P, D_latent + D_rope] (in place)."""
+    B = ctx_lens.shape[0]
+    _check_offsets(B, block_tables, cu_q=cu_q)
+    if latent.dim() != 2 or rope.dim() != 2 or latent.shape[0] != rope.shape[0] or cache.dim() != 3 or latent.shape[1] + rope.shape[1] != cache.shape[2]:
+        raise ValueError("latent [N_cap, D_latent] and rope [N_cap, D_rope] must make up the rows of cache [n_pages, P, D_latent + D_rope]")
+    if not (latent.dtype == rope.dtype == cache.dtype):
+        raise ValueError("latent, rope and cache must share a dtype")
+    _on_current_device(latent=latent, rope=rope, cache=cache, block_tables=block_tables, ctx_lens=ctx_lens, cu_q=cu_q)
+    p = _latent_params(cache, block_tables, B, latent.shape[0], 1, latent.shape[1], cache.dtype, cache.dtype)
+    _call("fsr_latent_append", latent, rope, cache, block_tables, ctx_lens, cu_q, p)
+
+
+def latent_gather(cache, block_tables, cu_k, *, T_cap, D_latent, latent=None, rope=None):
+    """fsr_latent_gather: positions 0 .. of every request (cu_k: offsets of their rows) out of the paged latent cache.  Returns
+    (latent [T_cap, D_latent], rope [T_cap, D_rope]); rows from cu_k[B] on are not written."""
+    B = cu_k.shape[0] - 1
+    _check_offsets(B, block_tables, cu_k=cu_k)
+    p = _latent_params(cache, block_tables, B, int(T_cap), 1, D_latent, cache.dtype, cache.dtype)
+    if latent is None:
+        latent = torch.empty((T_cap, D_latent), dtype=cache.dtype, device=cache.device)
+    if rope is None:
+        rope = torch.empty((T_cap, p.D_rope), dtype=cache.dtype, device=cache.device)
+    if tuple(latent.shape) != (T_cap, D_latent) or tuple(rope.shape) != (T_cap, p.D_rope) or not (latent.dtype == rope.dtype == cache.dtype):
+        raise ValueError("latent must be [T_cap, D_latent] and rope [T_cap, D_rope], of the cache's dtype")
+    _on_current_device(cache=cache, block_tables=block_tables, cu_k=cu_k, latent=latent, rope=rope)
+    _call("fsr_latent_gather", cache, block_tables, cu_k, latent, rope, p)
+    return latent, rope
+
+
+def latent_attention(q, cache, block_tables, ctx_lens, cu_q, *, scale, D_latent, out=None, lse=None, out_dtype=None, workspace=None,
+                     max_q_len=0, max_workgroups=0):
+    """fsr_latent_attention.  q [N_cap, H, D_latent + D_rope], cache [n_pages, P, D_latent + D_rope]; returns (out [N_cap, H, D_latent], lse)."""
+    B = ctx_lens.shape[0]
+    _check_offsets(B, block_tables, cu_q=cu_q)
+    if q.dim() != 3 or cache.dim() != 3 or q.shape[2] != cache.shape[2] or q.dtype != cache.dtype:
+        raise ValueError("q [N_cap, H, D_latent + D_rope] and cache [n_pages, P, D_latent + D_rope] must share width and dtype")
+    out, out_dtype = _outputs((q.shape[0], q.shape[1], D_latent), out, lse, out_dtype, q.dtype, q.device)
+    p = _latent_params(cache, block_tables, B, q.shape[0], q.shape[1], D_latent, q.dtype, out_dtype, scale, max_q_len, max_workgroups)
+    _on_current_device(q=q, cache=cache, block_tables=block_tables, ctx_lens=ctx_lens, cu_q=cu_q, out=out, lse=lse, workspace=workspace)
+    token = _guard_workspace(workspace)
+    workspace, ws_bytes = _scratch("fsr_latent_workspace_bytes", p, workspace, q.device)
+    _call("fsr_latent_attention", q, cache, block_tables, ctx_lens, cu_q, out, lse, p, workspace, ws_bytes)
+    _note_workspace_use(token)
+    return out, lse
+
+
+def latent_attention_expanded(q, kv, k_rope, cu_q, cu_k, *, scale, out=None, lse=None, out_dtype=None, workspace=None, max_q_len=0,
+                              max_workgroups=0):
+    """fsr_latent_attention_expanded.  q [N_cap, H, D_nope + D_rope], kv [T_cap, H, D_nope + D_v] (a head's key, then its value),
+    k_rope [T_cap, D_rope]; returns (out [N_cap, H, D_v], lse)."""
+    B = cu_q.shape[0] - 1
+    _check_offsets(B, cu_q=cu_q, cu_k=cu_k)
+    if q.dim() != 3 or kv.dim() != 3 or k_rope.dim() != 2 or kv.shape[1] != q.shape[1] or k_rope.shape[0] != kv.shape[0]:
+        raise ValueError("q [N_cap, H, D_nope + D_rope], kv [T_cap, H, D_nope + D_v] and k_rope [T_cap, D_rope] must fit together")
+    D_nope = q.shape[2] - k_rope.shape[1]
+    D_v = kv.shape[2] - D_nope
+    if D_nope <= 0 or D_v <= 0:
+        raise ValueError("q must be wider than k_rope, and kv wider than the rest of q")
+    if not (q.dtype == kv.dtype == k_rope.dtype):
+        raise ValueError("q, kv and k_rope must share a dtype")
+    out, out_dtype = _outputs((q.shape[0], q.shape[1], D_v), out, lse, out_dtype, q.dtype, q.device)
+    p = ExpandedParams(B=B, N_cap=q.shape[0], T_cap=kv.shape[0], H=q.shape[1], D_nope=D_nope, D_rope=k_rope.shape[1], D_v=D_v,
+                       dtype=_code(q.dtype), out_dtype=_code(out_dtype), scale=float(scale), max_q_len=int(max_q_len),
+                       max_workgroups=int(max_workgroups), reserved=0)
+    _on_current_device(q=q, kv=kv, k_rope=k_rope, cu_q=cu_q, cu_k=cu_k, out=out, lse=lse, workspace=workspace)
+    token = _guard_workspace(workspace)
+    workspace, ws_bytes = _scratch("fsr_expanded_workspace_bytes", p, workspace, q.device)
+    _call("fsr_latent_attention_expanded", q, kv, k_rope, cu_q, cu_k, out, lse, p, workspace, ws_bytes)
+    _note_workspace_use(token)
+    return out, lse
+
+
+def verify_attention_shared(q, k_cache, v_cache, block_tables, ctx_lens, cu_q, cu_groups, prefix_lens, *, scale, out=None, lse=None,
+                            out_dtype=None, workspace=None, max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR):
+    """fsr_verify_attention_shared: verify_attention for groups of requests (cu_groups) whose first prefix_lens positions are the
+    same tokens, read once per group through its first request's block table.  Returns (out, lse)."""
+    B = ctx_lens.shape[0]
+    _check_offsets(B, block_tables, cu_q=cu_q)
+    if cu_groups.dim() != 1 or prefix_lens.dim() != 1 or cu_groups.shape[0] != prefix_lens.shape[0] + 1:
+        raise ValueError("cu_groups must have one entry more than prefix_lens")
+    if q.dim() != 3 or k_cache.dim() != 4 or v_cache.shape != k_cache.shape or not (q.dtype == k_cache.dtype == v_cache.dtype):
+        raise ValueError("q, k_cache and v_cache must share dtype; caches must share shape")
+    out, out_dtype = _outputs(tuple(q.shape), out, lse, out_dtype, q.dtype, q.device)
+    p = _attn_params(q, k_cache, block_tables, B, out_dtype, scale, max_q_len, max_workgroups, kv_layout)
+    _on_current_device(q=q, k_cache=k_cache, v_cache=v_cache, block_tables=block_tables, ctx_lens=ctx_lens, cu_q=cu_q, cu_groups=cu_groups,
+                       prefix_lens=prefix_lens, out=out, lse=lse, workspace=workspace)
+    token = _guard_workspace(workspace)
+    workspace, ws_bytes = _scratch("fsr_shared_workspace_bytes", p, workspace, q.device)
+    _call("fsr_verify_attention_shared", q, k_cache, v_cache, block_tables, ctx_lens, cu_q, cu_groups, prefix_lens, prefix_lens.shape[0], out,
+          lse, p, workspace, ws_bytes)
+    _note_workspace_use(token)
+    return out, lse
+
+
+def latent_workspace_bytes(*, N_cap, H, D_latent, D_rope, dtype, out_dtype) -> int:
+    """Workspace of latent_attention for calls of up to N_cap rows."""
+    p = LatentParams(B=1, N_cap=N_cap, H=H, D_latent=D_latent, D_rope=D_rope, P=1, max_pages=1, n_pages=1, dtype=_code(dtype),
+                     out_dtype=_code(out_dtype), scale=1.0, max_q_len=0, max_workgroups=0, reserved=0)
+    return _workspace_of("fsr_latent_workspace_bytes", p)
+
+
+def expanded_workspace_bytes(*, N_cap, H, D_nope, D_rope, D_v, dtype, out_dtype) -> int:
+    """Workspace of latent_attention_expanded for calls of up to N_cap rows."""
+    p = ExpandedParams(B=1, N_cap=N_cap, T_cap=1, H=H, D_nope=D_nope, D_rope=D_rope, D_v=D_v, dtype=_code(dtype), out_dtype=_code(out_dtype),
+                       scale=1.0, max_q_len=0, max_workgroups=0, reserved=0)
+    return _workspace_of("fsr_expanded_workspace_bytes", p)
+
+
+def shared_workspace_bytes(*, N_cap, H_q, H_kv, D, dtype, out_dtype) -> int:
+    """Workspace of verify_attention_shared for calls of up to N_cap rows."""
+    p = AttnParams(B=1, N_cap=N_cap, H_q=H_q, H_kv=H_kv, D=D, P=1, max_pages=1, n_pages=1, dtype=_code(dtype), out_dtype=_code(out_dtype),
+                   scale=1.0, max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR)
+    return _workspace_of("fsr_shared_workspace_bytes", p)
+
+
+def _workspace_of(size_of, p) -> int:
+    out = ctypes.c_size_t(0)
+    _check(getattr(load_library(), size_of)(ctypes.byref(p), ctypes.byref(out)))
+    return int(out.value)
 
 
 def accept_workspace_bytes(*, B, V, S_max, mode=PROBS, temperature=1.0) -> int:

@@ -1,0 +1,708 @@
+// Attention of many query rows on one stream of keys: what attention over a latent cache, its expanded form and attention
+// behind a shared prefix have in common.
+//
+// A *sequence* is a set of query rows that read the same keys (a request's rows, or all rows of the requests that share a
+// prefix); per stream head, G query heads of a call row read the same key.  The rows of a sequence are packed (packed row r =
+// call row r / G, query head r % G of the stream head) and cut into tiles of M rows; an *item* is one tile with all its keys.
+//     z[r, t] = scale * q[r] . k[t],   o[r] = sum_t exp(z[r, t] - m) v[t] / sum_t exp(z[r, t] - m)
+//
+// Schedule: the key tiles of all items lie end to end on a line (every item with kItemCost units in front for taking it up),
+// and the line is cut into equal shares, one per workgroup of a persistent grid.  Lengths stay on the device: every workgroup
+// adds them up for itself.  An item inside one share is finished there; one that a share boundary cuts leaves unnormalised
+// fp32 sums of its pieces in the workspace, at most two per share, which a second launch adds in the order of the shares
+// (no atomics: results do not depend on timing).
+#pragma once
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "common.hpp"
+#include "device_utils.hpp"
+
+namespace fsr {
+namespace row_tiles {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+typedef __attribute__((__vector_size__(8 * sizeof(short)))) short s16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kTileRows = 128;     // most rows of a tile
+constexpr int kItemCost = 2;       // key tiles that taking up an item is worth
+constexpr int kDescInts = 8;       // merge descriptor of a share
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+enum : int { kLatent = 0, kExpanded = 1, kShared = 2 };
+
+struct Args {
+    const void* q;       // [N_cap, H, D_k]
+    const char* k_head;  // first (or only) part of a key row
+    const char* k_tail;  // rest of a key row
+    const char* v;       // value row (latent: the first part of the key row)
+    const int32_t* bt;
+    const int32_t* ctx;
+    const int32_t* cu_q;
+    const int32_t* cu_k;      // expanded: offsets of the keys
+    const int32_t* cu_groups; // shared
+    const int32_t* prefix;    // shared
+    void* out;
+    float* lse;
+    int B, N_cap, H, H_stream, G, n_groups, T_cap;
+    int P, max_pages, n_pages;
+    uint32_t page_slots;                    // slots that a page advances by
+    long long head_stride, tail_stride, v_stride;  // bytes from a slot to the next
+    long long head_hk, v_hk;                // bytes from a stream head to the next
+    float scale, scale_log2;  // softmax scale, and times log2(e)
+    int nb, shares_cap, min_share, m_cap;
+    float* part_o;    // [2 * shares_cap][m_cap][D_v]
+    float* part_ml;   // [2 * shares_cap][m_cap][2] score that the weights refer to, sum
+    int32_t* desc;    // [shares_cap][kDescInts]
+    float* row_o;     // shared: [2][N_cap * H][D_v] sums of items that are whole: prefix, own
+    float* row_ml;    // shared: [2][N_cap * H][2]
+    int32_t* refs;    // shared: [2][N_cap * H][2] pieces (0: in row_o) and first share of the item
+};
+
+struct Seq {
+    int row0, rows;      // call rows
+    int k_begin, k_end;  // keys
+    int base;            // packed row r sees keys up to base + r / G
+    int table;           // row of the block table
+    uint32_t first;      // expanded: slot of the first key
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+template <int OP>
+__device__ __forceinline__ int n_sequences(const Args& a) { return OP == kShared ? a.n_groups + a.B : a.B; }
+
+// Sequence s.  Metadata that does not hold together (offsets out of order, lengths beyond the table) never leads outside the
+// tensors: offsets are clamped to the rows that are allocated, positions to the table.
+template <int OP>
+__device__ __forceinline__ Seq sequence(const Args& a, int s) {
+    Seq q;
+    q.first = 0;
+    if constexpr (OP == kExpanded) {
+        q.row0 = clamp_to(a.cu_q[s], 0, a.N_cap);
+        q.rows = clamp_to(a.cu_q[s + 1], q.row0, a.N_cap) - q.row0;
+        const int first = clamp_to(a.cu_k[s], 0, a.T_cap);
+        const int keys = clamp_to(a.cu_k[s + 1], first, a.T_cap) - first;
+        q.first = (uint32_t)first;
+        q.k_begin = 0;
+        q.k_end = keys;
+        q.base = keys - q.rows;
+        q.table = 0;
+        return q;
+    }
+    const int cap = (int)min((long long)a.max_pages * a.P, 1LL << 30);
+    if (OP == kShared && s < a.n_groups) {
+        const int i0 = clamp_to(a.cu_groups[s], 0, a.B), i1 = clamp_to(a.cu_groups[s + 1], i0, a.B);
+        q.row0 = clamp_to(a.cu_q[i0], 0, a.N_cap);
+        q.rows = clamp_to(a.cu_q[i1], q.row0, a.N_cap) - q.row0;
+        q.k_begin = 0;
+        q.k_end = i1 > i0 ? clamp_to(a.prefix[s], 0, cap) : 0;
+        if (q.k_end == 0) q.rows = 0;  // no item: the rows are their own part's alone
+        q.base = 1 << 30;              // every row sees the whole prefix
+        q.table = min(i0, a.B - 1);
+        return q;
+    }
+    const int i = OP == kShared ? s - a.n_groups : s;
+    q.row0 = clamp_to(a.cu_q[i], 0, a.N_cap);
+    q.rows = clamp_to(a.cu_q[i + 1], q.row0, a.N_cap) - q.row0;
+    q.k_begin = 0;
+    if constexpr (OP == kShared) {
+        int lo = 0, hi = a.n_groups;  // the group that holds request i
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (a.cu_groups[mid] <= i) lo = mid; else hi = mid;
+        }
+        const bool in = a.cu_groups[lo] <= i && i < a.cu_groups[lo + 1];
+        q.k_begin = in ? clamp_to(a.prefix[lo], 0, cap) : 0;
+        if (!in) q.rows = 0;  // requests outside the groups have no output
+    }
+    const int c = clamp_to(a.ctx[i], q.k_begin, cap);
+    q.base = c;
+    q.k_end = min(c + min(q.rows, cap), cap);
+    q.table = i;
+    return q;
+}
+
+__device__ __forceinline__ int ceil_div(int x, int y) { return (x + y - 1) / y; }
+
+template <class C>
+__device__ __forceinline__ int row_tiles_of(const Args& a, const Seq& q) {
+    return (int)(((long long)q.rows * a.G + C::kM - 1) / C::kM);
+}
+
+// Key tiles of row tile rt.
+template <class C>
+__device__ __forceinline__ int key_tiles(const Args& a, const Seq& q, int rt) {
+    int end = q.k_end;
+    if constexpr (C::kOp == kExpanded) end = min(end, q.base + min(q.rows, (rt + 1) * C::kM));  // (G = 1) the last row's last key
+    return end > q.k_begin ? ceil_div(end - q.k_begin, C::kKeys) : 0;
+}
+
+// Units of the line in front of row tile rt of a stream head.
+template <class C>
+__device__ __forceinline__ long long units_before(const Args& a, const Seq& q, int rt) {
+    if constexpr (C::kOp != kExpanded) return (long long)rt * (kItemCost + key_tiles<C>(a, q, 0));
+    // expanded: key_tiles grows by M / kKeys per row tile from the first tile that sees a key, except that the last tile may
+    // hold fewer rows (it is summed by itself)
+    static_assert(C::kOp != kExpanded || C::kM % C::kKeys == 0, "whole key tiles per row tile");
+    constexpr int kStep = C::kM / C::kKeys;
+    const int n = row_tiles_of<C>(a, q);
+    const int full = min(rt, max(n - 1, 0));
+    const int t0 = q.base >= 0 ? ceil_div(q.base, C::kKeys) : -((-q.base) / C::kKeys);  // ceil(base / kKeys)
+    // tiles r in [r0, full) see t0 + kStep * (r + 1) key tiles
+    const int r0 = t0 >= -kStep + 1 ? 0 : min((-t0) / kStep, full);
+    const long long m = full - r0;
+    long long sum = m * t0 + (long long)kStep * (m * (r0 + 1) + m * (m - 1) / 2);
+    sum += (long long)kItemCost * full;
+    if (rt > full) sum += kItemCost + key_tiles<C>(a, q, n - 1);
+    return sum;
+}
+
+template <class C>
+__device__ __forceinline__ long long sequence_units(const Args& a, const Seq& q) {
+    return units_before<C>(a, q, row_tiles_of<C>(a, q)) * a.H_stream;
+}
+
+struct Line {
+    long long total;
+    int shares;
+    int seq;               // sequence in which this share begins
+    long long seq_start;   // its first unit
+    long long lo, hi;      // this share
+};
+
+__device__ __forceinline__ long long share_begin(long long total, int shares, int s) { return total * s / shares; }
+
+__device__ __forceinline__ int share_of(long long total, int shares, long long u) {
+    int s = (int)(u * shares / total);
+    while (s + 1 < shares && share_begin(total, shares, s + 1) <= u) ++s;
+    while (s > 0 && share_begin(total, shares, s) > u) --s;
+    return s;
+}
+
+__device__ __forceinline__ long long shfl_up64(long long v, int d) {
+    const int lo = __shfl_up((int)(uint32_t)v, d, kWave), hi = __shfl_up((int)(v >> 32), d, kWave);
+    return ((long long)hi << 32) | (uint32_t)lo;
+}
+
+// Adds up the line; `scratch`: LDS for kThreads + 1 sums.
+template <class C>
+__device__ __forceinline__ Line find_share(const Args& a, int share, long long* scratch) {
+    const int n = n_sequences<C::kOp>(a), tid = threadIdx.x;
+    const int each = ceil_div(n, kThreads);
+    const int s0 = min(tid * each, n), s1 = min(s0 + each, n);
+    long long mine = 0;
+    for (int s = s0; s < s1; ++s) mine += sequence_units<C>(a, sequence<C::kOp>(a, s));
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const long long up = shfl_up64(upto, o);
+        if ((tid & (kWave - 1)) >= o) upto += up;
+    }
+    if ((tid & (kWave - 1)) == kWave - 1) scratch[kThreads + (tid >> 6)] = upto;
+    __syncthreads();
+    for (int w = 0; w < (tid >> 6); ++w) upto += scratch[kThreads + w];
+    scratch[tid] = upto;
+    __syncthreads();
+    Line l;
+    l.total = scratch[kThreads - 1];
+    l.shares = (int)min((long long)a.nb, max(1LL, l.total / a.min_share));
+    l.seq = n;
+    l.seq_start = l.total;
+    l.lo = l.hi = 0;
+    if (l.total > 0 && share < l.shares) {
+        l.lo = share_begin(l.total, l.shares, share);
+        l.hi = share_begin(l.total, l.shares, share + 1);
+        int first = 0, last = kThreads - 1;  // the chunk of sequences that holds unit lo
+        while (first < last) {
+            const int mid = (first + last) >> 1;
+            if (scratch[mid] <= l.lo) first = mid + 1; else last = mid;
+        }
+        first = uniform(first);
+        long long at = first ? scratch[first - 1] : 0;
+        for (int s = first * each; s < n; ++s) {
+            const long long u = sequence_units<C>(a, sequence<C::kOp>(a, s));
+            if (at + u > l.lo) {
+                l.seq = s;
+                l.seq_start = at;
+                break;
+            }
+            at += u;
+        }
+    }
+    __syncthreads();  // the scratch memory is given back
+    return l;
+}
+
+// The piece of an item that a workgroup works on.
+struct Piece {
+    Seq q;
+    int hk, rt;
+    int t0, t1;          // its key tiles
+    bool whole;          // all of the item's tiles
+    int slot;            // of the partial sums of a piece that is not
+    int share0, pieces;  // where the item's pieces lie
+};
+
+// Where the packed row r of an item goes.
+struct Place {
+    int row, head;
+};
+__device__ __forceinline__ Place place_of(const Args& a, int row0, int hk, long long r) {
+    const int j = (int)(r / a.G);
+    return Place{row0 + j, hk * a.G + (int)(r - (long long)j * a.G)};
+}
+
+// Slot of key `key` of a sequence (kept inside its table and the pool).
+template <int OP>
+__device__ __forceinline__ uint32_t slot_of(const Args& a, const Seq& q, int key) {
+    if constexpr (OP == kExpanded) return q.first + (uint32_t)key;
+    const uint32_t pg = (uint32_t)key / (uint32_t)a.P;
+    const int page = clamp_to(a.bt[(size_t)q.table * a.max_pages + pg], 0, a.n_pages - 1);
+    return (uint32_t)page * a.page_slots + ((uint32_t)key - pg * (uint32_t)a.P);
+}
+
+__device__ __forceinline__ uint32_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// D_v columns of a row: out of the accumulators of one lane, four neighbouring columns at a time.
+__device__ __forceinline__ void store4(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
+__device__ __forceinline__ void store4(uint16_t* p, f32x4 x) {
+    *reinterpret_cast<u32x2*>(p) = u32x2{bf16_bits(x[0]) | (bf16_bits(x[1]) << 16), bf16_bits(x[2]) | (bf16_bits(x[3]) << 16)};
+}
+
+// Logarithm of exp(m) * l, -inf without any weight.
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2; }
+__device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+// Result of a row's share of the keys: sums o[4] at columns d .. d + 3 (called for all of the lane's columns), the score m that the
+// weights refer to (-inf: no key), their sum l.
+template <class C, class ForEach4>
+__device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_tile, bool first_lane, float m, float l, ForEach4 each) {
+    const long long packed = (long long)p.rt * C::kM + r_tile;
+    const Place at = place_of(a, p.q.row0, p.hk, packed);
+    const size_t row = (size_t)at.row * a.H + at.head;
+    const bool prefix = C::kOp == kShared && p.q.base == 1 << 30;
+    const bool joined = C::kOp == kShared && (prefix || p.q.k_begin > 0);  // two items make the row
+    if (p.whole && !joined) {
+        using Out = typename C::Out;
+        Out* out = (Out*)a.out + row * C::kDv;
+        const float inv = inverse(l);
+        each([&](int d, f32x4 x) { store4(out + d, x * inv); });
+        if (first_lane && a.lse) a.lse[row] = log_sum(m, l);
+        if (C::kOp == kShared && first_lane) {
+            const size_t n = (size_t)a.N_cap * a.H;
+            a.refs[2 * (n + row)] = -1;  // nothing is left to be joined
+        }
+        return;
+    }
+    float *o, *ml;
+    if (p.whole) {
+        const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
+        o = a.row_o + k * C::kDv;
+        ml = a.row_ml + k * 2;
+    } else {
+        const size_t k = (size_t)p.slot * a.m_cap + r_tile;
+        o = a.part_o + k * C::kDv;
+        ml = a.part_ml + k * 2;
+    }
+    each([&](int d, f32x4 x) { store4(o + d, x); });
+    if (first_lane) {
+        ml[0] = m;
+        ml[1] = l;
+        if (C::kOp == kShared && p.t0 == 0) {  // whoever begins the item says where its pieces are
+            const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
+            a.refs[2 * k] = p.whole ? 0 : p.pieces;
+            a.refs[2 * k + 1] = p.share0;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// Products in fp32: every wave takes 16 rows of the tile, with operands straight from memory.  S^T = K Q^T and O^T = V^T P^T
+// on v_mfma_f32_16x16x4_f32; the accumulator layout of S^T (lane: keys 4 (lane / 16) + e, row lane % 16) is the operand
+// layout of P^T if step e of the second product takes keys 4 g + e of lane group g.
+// ---------------------------------------------------------------------------------------------------------------
+template <int OP, int KH, int KT, int DV, class IN, class OUT>
+struct Simple {
+    static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
+    static constexpr int kM = 64, kKeys = 64, kPerSimd = 1;
+    typedef IN In;
+    typedef OUT Out;
+};
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
+__device__ __forceinline__ f32x4 load4(const uint16_t* p) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    const uint32_t lo = x[0], hi = x[1];
+    return f32x4{widen((uint16_t)lo), widen((uint16_t)(lo >> 16)), widen((uint16_t)hi), widen((uint16_t)(hi >> 16))};
+}
+
+// Last key that packed row r sees.
+__device__ __forceinline__ int last_key(const Args& a, const Seq& q, long long r) {
+    return (int)min((long long)q.k_end - 1, (long long)q.base + r / a.G);
+}
+
+template <class C>
+__device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
+    typedef typename C::In In;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lg = lane >> 4;
+    const long long n_packed = (long long)p.q.rows * a.G, first = (long long)p.rt * C::kM + wave * 16;
+    if (first >= n_packed) return;
+    const long long r = min(first + li, n_packed - 1);
+    const Place at = place_of(a, p.q.row0, p.hk, r);
+    const In* qp = (const In*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
+    f32x4 q[C::kDk / 16];
+#pragma unroll
+    for (int s = 0; s < C::kDk / 16; ++s) q[s] = load4(qp + 16 * s + 4 * lg);
+    const int seen = last_key(a, p.q, r);
+    f32x4 acc[C::kDv / 16];
+#pragma unroll
+    for (int b = 0; b < C::kDv / 16; ++b) acc[b] = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+    const int k_first = p.q.k_begin + p.t0 * C::kKeys, k_last = min(p.q.k_begin + p.t1 * C::kKeys, p.q.k_end);
+#pragma unroll 1
+    for (int kb = k_first; kb < k_last; kb += 16) {
+        const uint32_t slot = slot_of<C::kOp>(a, p.q, min(kb + li, k_last - 1));
+        const In* kh = (const In*)(a.k_head + (size_t)slot * a.head_stride + (size_t)p.hk * a.head_hk);
+        f32x4 z = {0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < C::kHead / 16; ++s) {
+            const f32x4 k4 = load4(kh + 16 * s + 4 * lg);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q[s][e], z, 0, 0, 0);
+        }
+        if constexpr (C::kTail > 0) {
+            const In* kt = (const In*)(a.k_tail + (size_t)slot * a.tail_stride);
+#pragma unroll
+            for (int s = 0; s < C::kTail / 16; ++s) {
+                const f32x4 k4 = load4(kt + 16 * s + 4 * lg);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q[C::kHead / 16 + s][e], z, 0, 0, 0);
+            }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int key = kb + 4 * lg + e;
+            z[e] = key <= seen && key < k_last ? z[e] : -INFINITY;
+            top = fmaxf(top, z[e]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float m_new = fmaxf(m, top);  // (of the products: their multiples by log2(e) may be beyond fp32)
+        const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f((m - m_use) * a.scale_log2);
+        f32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f((z[e] - m_use) * a.scale_log2);
+        l = l * alpha + ((x[0] + x[1]) + (x[2] + x[3]));
+        m = m_new;
+#pragma unroll
+        for (int b = 0; b < C::kDv / 16; ++b) acc[b] *= alpha;
+        const bool masked = __any(kb + 15 > seen || kb + 15 >= k_last);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t vs = (uint32_t)__shfl((int)slot, 4 * lg + e, kWave);
+            const In* vp = (const In*)(a.v + (size_t)vs * a.v_stride + (size_t)p.hk * a.v_hk);
+            float v[C::kDv / 16];
+            uint32_t odd = 0;
+#pragma unroll
+            for (int b = 0; b < C::kDv / 16; ++b) {
+                v[b] = widen(vp[16 * b + li]);
+                odd |= (__builtin_bit_cast(uint32_t, v[b]) & 0x7f800000u) == 0x7f800000u;
+            }
+            if (!masked || !__any(odd)) {
+#pragma unroll
+                for (int b = 0; b < C::kDv / 16; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b], x[e], acc[b], 0, 0, 0);
+            } else {
+                // a value that is not finite must not meet the zero weight of a row that does not see it: each kind is
+                // multiplied as 1 and takes its place only in rows that give it weight
+#pragma unroll
+                for (int b = 0; b < C::kDv / 16; ++b) {
+                    const bool fine = (__builtin_bit_cast(uint32_t, v[b]) & 0x7f800000u) != 0x7f800000u;
+                    acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fine ? v[b] : 0.0f, x[e], acc[b], 0, 0, 0);
+                    const f32x4 none = {0, 0, 0, 0};
+                    const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] == INFINITY ? 1.0f : 0.0f, x[e], none, 0, 0, 0);
+                    const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] == -INFINITY ? 1.0f : 0.0f, x[e], none, 0, 0, 0);
+                    const f32x4 nan = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] != v[b] ? 1.0f : 0.0f, x[e], none, 0, 0, 0);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        float add = up[u] != 0.0f ? INFINITY : 0.0f;
+                        add += down[u] != 0.0f ? -INFINITY : 0.0f;
+                        acc[b][u] += nan[u] != 0.0f ? __builtin_nanf("") : add;
+                    }
+                }
+            }
+        }
+    }
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    if (first + li < n_packed)
+        hand_over<C>(a, p, wave * 16 + li, lg == 0, m * a.scale, l, [&](auto put) {
+#pragma unroll
+            for (int b = 0; b < C::kDv / 16; ++b) put(16 * b + 4 * lg, acc[b]);
+        });
+}
+
+// Items of a share, one after the other.
+template <class C, class Run>
+__device__ __forceinline__ void walk(const Args& a, int share, const Line& line, Run run) {
+    int32_t* desc = a.desc + (size_t)share * kDescInts;
+    if (C::kOp != kShared && threadIdx.x == 0) desc[0] = 0;
+    const int n = n_sequences<C::kOp>(a);
+    long long seq_start = line.seq_start;
+    for (int s = line.seq; s < n && seq_start < line.hi; ++s) {
+        const Seq q = sequence<C::kOp>(a, s);
+        const int tiles = row_tiles_of<C>(a, q);
+        const long long head_units = units_before<C>(a, q, tiles);
+        int hk = seq_start < line.lo ? (int)((line.lo - seq_start) / head_units) : 0;
+        if (tiles > 0)
+            for (; hk < a.H_stream; ++hk) {
+                const long long head_start = seq_start + hk * head_units;
+                if (head_start >= line.hi) break;
+                int rt = 0;
+                if (head_start < line.lo) {  // the row tile that holds unit lo
+                    int last = tiles - 1;
+                    while (rt < last) {
+                        const int mid = (rt + last + 1) >> 1;
+                        if (head_start + units_before<C>(a, q, mid) <= line.lo) rt = mid; else last = mid - 1;
+                    }
+                }
+                for (; rt < tiles; ++rt) {
+                    const long long item = head_start + units_before<C>(a, q, rt);
+                    if (item >= line.hi) break;
+                    Piece p;
+                    p.q = q;
+                    p.hk = hk;
+                    p.rt = rt;
+                    const int nk = key_tiles<C>(a, q, rt);
+                    const long long t0 = line.lo - item - kItemCost, t1 = line.hi - item - kItemCost;
+                    p.t0 = t0 > 0 ? (int)min(t0, (long long)nk) : 0;
+                    p.t1 = t1 > 0 ? (int)min(t1, (long long)nk) : 0;
+                    p.whole = p.t0 == 0 && p.t1 == nk;
+                    p.slot = 0;
+                    p.share0 = share;
+                    p.pieces = 1;
+                    if (nk == 0 ? item < line.lo : p.t0 >= p.t1) continue;  // nothing of it is this share's
+                    if (!p.whole) {
+                        p.share0 = share_of(line.total, line.shares, item + kItemCost);
+                        p.pieces = share_of(line.total, line.shares, item + kItemCost + nk - 1) - p.share0 + 1;
+                        p.slot = 2 * share + (p.t0 == 0 ? 1 : 0);  // an item that begins here, or one that began before
+                        if (C::kOp != kShared && p.t0 == 0 && threadIdx.x == 0) {
+                            const long long first = (long long)rt * C::kM, rows = min((long long)q.rows * a.G - first, (long long)C::kM);
+                            desc[1] = q.row0; desc[2] = hk; desc[3] = rt; desc[4] = (int)rows;
+                            desc[0] = p.pieces;
+                        }
+                    }
+                    run(p);
+                }
+            }
+        seq_start += head_units * a.H_stream;
+    }
+}
+
+// Neighbouring shares read the same keys: they go to the same one of the 8 dies (workgroups are dealt to them in turn).
+__device__ __forceinline__ int share_of_block(int block, int nb) {
+    const int per = nb >> 3, rest = nb & 7, die = block & 7;
+    return (block >> 3) + die * per + min(die, rest);
+}
+
+template <class C>
+__global__ __launch_bounds__(kThreads, C::kPerSimd) void simple_kernel(Args a) {
+    __shared__ long long scratch[kThreads + kWaves];
+    const int share = share_of_block(blockIdx.x, a.nb);
+    const Line line = find_share<C>(a, share, scratch);
+    walk<C>(a, share, line, [&](const Piece& p) { run_simple<C>(a, p); });
+}
+
+// Sums of a row's pieces, joined: a wave per row, D_v / 64 columns a lane.
+template <int DV>
+struct Joined {
+    float o[DV / 64];
+    float m = -INFINITY, l = 0.0f;
+    __device__ __forceinline__ Joined() {
+#pragma unroll
+        for (int k = 0; k < DV / 64; ++k) o[k] = 0.0f;
+    }
+    __device__ __forceinline__ void add(const float* po, const float* ml, int lane) {
+        const float pm = ml[0], pl = ml[1];
+        if (pl == 0.0f) return;  // no visible key
+        float x[DV / 64];
+#pragma unroll
+        for (int k = 0; k < DV / 64; ++k) x[k] = po[lane * (DV / 64) + k];
+        const float m_new = fmaxf(m, pm);
+        const float use = m_new == -INFINITY ? 0.0f : m_new;
+        const float wa = __builtin_amdgcn_exp2f((m - use) * kLog2e), wb = __builtin_amdgcn_exp2f((pm - use) * kLog2e);
+#pragma unroll
+        for (int k = 0; k < DV / 64; ++k) o[k] = o[k] * wa + x[k] * wb;
+        l = l * wa + pl * wb;
+        m = m_new;
+    }
+    template <class Out>
+    __device__ __forceinline__ void write(Out* out, float* lse, int lane) const {
+        const float inv = inverse(l);
+#pragma unroll
+        for (int k = 0; k < DV / 64; ++k) {
+            if constexpr (sizeof(Out) == 2) out[lane * (DV / 64) + k] = (uint16_t)bf16_bits(o[k] * inv);
+            else out[lane * (DV / 64) + k] = o[k] * inv;
+        }
+        if (lse && lane == 0) *lse = log_sum(m, l);
+    }
+};
+
+// Joins the items that begin in a share and go on behind it.  blockIdx.x: share, blockIdx.y: rows of the tile, kWaves at a time.
+template <class C>
+__global__ __launch_bounds__(kThreads) void join_shares_kernel(Args a) {
+    const int32_t* desc = a.desc + (size_t)blockIdx.x * kDescInts;
+    const int pieces = desc[0];
+    if (pieces <= 0) return;
+    const int lane = threadIdx.x & 63, share = blockIdx.x;
+    for (int r = blockIdx.y * kWaves + (threadIdx.x >> 6); r < desc[4]; r += gridDim.y * kWaves) {
+        Joined<C::kDv> sum;
+        for (int k = 0; k < pieces; ++k) {
+            const size_t at = (size_t)(2 * (share + k) + (k == 0 ? 1 : 0)) * a.m_cap + r;
+            sum.add(a.part_o + at * C::kDv, a.part_ml + at * 2, lane);
+        }
+        const Place to = place_of(a, desc[1], desc[2], (long long)desc[3] * C::kM + r);
+        const size_t row = (size_t)to.row * a.H + to.head;
+        sum.write((typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
+    }
+}
+
+// Joins what a row's prefix and its own keys left.  A wave per (call row, query head).
+template <class C>
+__global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
+    const int lane = threadIdx.x & 63;
+    const size_t n = (size_t)a.N_cap * a.H;
+    const size_t row = (size_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const int i0 = clamp_to(a.cu_groups[0], 0, a.B), i1 = clamp_to(a.cu_groups[a.n_groups], 0, a.B);
+    const int call_row = (int)(row / a.H), head = (int)(row - (size_t)call_row * a.H);
+    if (row >= n || call_row < a.cu_q[i0] || call_row >= a.cu_q[i1]) return;
+    const int own = a.refs[2 * (n + row)];
+    if (own < 0) return;  // no prefix, and whole: written already
+    // the rows of the tile that held it: by its request for its own keys, by its group for the prefix
+    int lo = i0, hi = i1;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.cu_q[mid] <= call_row) lo = mid; else hi = mid;
+    }
+    int g0 = 0, g1 = a.n_groups;
+    while (g1 - g0 > 1) {
+        const int mid = (g0 + g1) >> 1;
+        if (a.cu_groups[mid] <= lo) g0 = mid; else g1 = mid;
+    }
+    Joined<C::kDv> sum;
+    auto take = [&](int part, int seq) {
+        const Seq q = sequence<C::kOp>(a, seq);
+        if (part == 0 && q.k_end == 0) return;
+        const size_t k = part * n + row;
+        const int pieces = clamp_to(a.refs[2 * k], 0, a.shares_cap), share0 = a.refs[2 * k + 1];
+        if (pieces == 0) {
+            sum.add(a.row_o + k * C::kDv, a.row_ml + k * 2, lane);
+            return;
+        }
+        const long long packed = (long long)(call_row - q.row0) * a.G + head % a.G;
+        const int r = clamp_to((int)(packed % C::kM), 0, a.m_cap - 1);
+        for (int j = 0; j < pieces; ++j) {
+            const int share = clamp_to(share0 + j, 0, a.shares_cap - 1);
+            const size_t at = (size_t)(2 * share + (j == 0 ? 1 : 0)) * a.m_cap + r;
+            sum.add(a.part_o + at * C::kDv, a.part_ml + at * 2, lane);
+        }
+    };
+    take(0, g0);
+    take(1, a.n_groups + lo);
+    sum.write((typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------------------
+constexpr int kSharesCap = 512;
+
+struct Layout {
+    size_t part_o, part_ml, desc, row_o, row_ml, refs, total;
+};
+
+// Workspace: slots of two pieces per share, and for a batch behind shared prefixes two results per row and head.
+inline Layout layout_of(int m_cap, int dv, long long rows, bool shared) {
+    Layout l{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t p = at; at += align_up(bytes, 256); return p; };
+    l.part_o = take((size_t)2 * kSharesCap * m_cap * dv * sizeof(float));
+    l.part_ml = take((size_t)2 * kSharesCap * m_cap * 2 * sizeof(float));
+    l.desc = take((size_t)kSharesCap * kDescInts * sizeof(int32_t));
+    if (shared) {
+        l.row_o = take((size_t)2 * rows * dv * sizeof(float));
+        l.row_ml = take((size_t)2 * rows * 2 * sizeof(float));
+        l.refs = take((size_t)2 * rows * 2 * sizeof(int32_t));
+    }
+    l.total = at;
+    return l;
+}
+
+inline void place(Args& a, const Layout& l, void* workspace) {
+    char* w = (char*)workspace;
+    a.part_o = (float*)(w + l.part_o);
+    a.part_ml = (float*)(w + l.part_ml);
+    a.desc = (int32_t*)(w + l.desc);
+    a.row_o = (float*)(w + l.row_o);
+    a.row_ml = (float*)(w + l.row_ml);
+    a.refs = (int32_t*)(w + l.refs);
+    a.shares_cap = kSharesCap;
+}
+
+// Compute units of the current device.
+inline int compute_units() {
+    static thread_local int cached_dev = -1, cached = 0;
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) {
+        (void)hipGetLastError();
+        return 256;
+    }
+    if (dev != cached_dev) {
+        int n = 0;
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) {
+            (void)hipGetLastError();
+            n = 256;
+        }
+        cached_dev = dev;
+        cached = n;
+    }
+    return cached;
+}
+
+template <class C>
+int launch(Args a, int max_workgroups, void* stream, const char* who) {
+    int nb = compute_units() * C::kPerSimd;
+    if (max_workgroups > 0) nb = std::min(nb, max_workgroups * C::kPerSimd);
+    a.nb = std::min(nb, kSharesCap);
+    a.min_share = kItemCost + 1;
+    hipStream_t s = (hipStream_t)stream;
+    hipLaunchKernelGGL((simple_kernel<C>), dim3(a.nb), dim3(kThreads), 0, s, a);
+    int rc = check_launch(who);
+    if (rc != FSR_OK) return rc;
+    if (C::kOp == kShared) {
+        const size_t rows = (size_t)a.N_cap * a.H;
+        hipLaunchKernelGGL((join_rows_kernel<C>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.nb, std::max(1, a.m_cap / 16)), dim3(kThreads), 0, s, a);
+    }
+    return check_launch(who);
+}
+
+}  // namespace row_tiles
+}  // namespace fsr
