@@ -110,6 +110,7 @@ int check_attention(const fsr_latent_params* p, const char* who) {
         return fail(FSR_EUNSUP, "%s: out_dtype=%d with dtype=%d", who, p->out_dtype, p->dtype);
     if (!(p->scale > 0.0f) || p->scale > 2.0e38f) return fail(FSR_EINVAL, "%s: scale=%g must be > 0 and finite", who, (double)p->scale);
     if (p->B > 65535 || p->H > 65535) return fail(FSR_EUNSUP, "%s: B and H are limited to 65535", who);
+    if ((long long)p->N_cap * p->H > (1LL << 30)) return fail(FSR_EUNSUP, "%s: N_cap * H exceeds 2^30 rows", who);
     if ((long long)p->max_pages * p->P > (1LL << 30)) return fail(FSR_EUNSUP, "%s: max_pages * P exceeds 2^30 tokens", who);
     if ((long long)p->n_pages * p->P > 0xffffffffLL) return fail(FSR_EUNSUP, "%s: n_pages * P exceeds 2^32 slots", who);
     return FSR_OK;
@@ -120,8 +121,8 @@ int rows_cap(const fsr_latent_params* p) { return (int)std::max(1LL, std::min((l
 template <int DL, int DR>
 int run(const Args& a, const fsr_latent_params* p, void* stream, const char* who) {
     if (p->dtype == FSR_F32) return launch<Simple<kLatent, DL, DR, DL, float, float>>(a, p->max_workgroups, stream, who);
-    if (p->out_dtype == FSR_F32) return launch<Simple<kLatent, DL, DR, DL, uint16_t, float>>(a, p->max_workgroups, stream, who);
-    return launch<Simple<kLatent, DL, DR, DL, uint16_t, uint16_t>>(a, p->max_workgroups, stream, who);
+    if (p->out_dtype == FSR_F32) return launch<Tiled<kLatent, DL, DR, DL, float>>(a, p->max_workgroups, stream, who);
+    return launch<Tiled<kLatent, DL, DR, DL, uint16_t>>(a, p->max_workgroups, stream, who);
 }
 
 }  // namespace
@@ -179,8 +180,9 @@ extern "C" int fsr_latent_attention(const void* q, const void* cache, const int3
     a.out = out; a.lse = lse;
     a.B = p->B; a.N_cap = p->N_cap; a.H = p->H; a.H_stream = 1; a.G = p->H;
     a.P = p->P; a.max_pages = p->max_pages; a.n_pages = p->n_pages;
+    a.p_shift = (p->P & (p->P - 1)) == 0 ? __builtin_ctz((unsigned)p->P) : -1;
     a.page_slots = (uint32_t)p->P;
-    a.head_stride = a.tail_stride = a.v_stride = row;
+    a.head_stride = a.tail_stride = a.v_stride = (uint32_t)row;
     a.scale = p->scale;
     a.scale_log2 = p->scale * kLog2e;
     a.m_cap = rows_cap(p);

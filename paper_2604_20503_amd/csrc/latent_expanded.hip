@@ -32,8 +32,8 @@ int rows_cap(const fsr_expanded_params* p) { return std::max(1, std::min(p->N_ca
 template <int DN, int DR, int DV>
 int run(const Args& a, const fsr_expanded_params* p, void* stream, const char* who) {
     if (p->dtype == FSR_F32) return launch<Simple<kExpanded, DN, DR, DV, float, float>>(a, p->max_workgroups, stream, who);
-    if (p->out_dtype == FSR_F32) return launch<Simple<kExpanded, DN, DR, DV, uint16_t, float>>(a, p->max_workgroups, stream, who);
-    return launch<Simple<kExpanded, DN, DR, DV, uint16_t, uint16_t>>(a, p->max_workgroups, stream, who);
+    if (p->out_dtype == FSR_F32) return launch<Tiled<kExpanded, DN, DR, DV, float>>(a, p->max_workgroups, stream, who);
+    return launch<Tiled<kExpanded, DN, DR, DV, uint16_t>>(a, p->max_workgroups, stream, who);
 }
 
 }  // namespace
@@ -70,8 +70,8 @@ extern "C" int fsr_latent_attention_expanded(const void* q, const void* kv, cons
     a.out = out; a.lse = lse;
     a.B = p->B; a.N_cap = p->N_cap; a.T_cap = p->T_cap; a.H = p->H; a.H_stream = p->H; a.G = 1;
     a.P = 1; a.max_pages = 1; a.n_pages = 1;
-    a.head_stride = a.v_stride = p->H * row;
-    a.tail_stride = p->D_rope * elem;
+    a.head_stride = a.v_stride = (uint32_t)(p->H * row);
+    a.tail_stride = (uint32_t)(p->D_rope * elem);
     a.head_hk = a.v_hk = row;
     a.scale = p->scale;
     a.scale_log2 = p->scale * kLog2e;

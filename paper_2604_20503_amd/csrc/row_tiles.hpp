@@ -31,7 +31,7 @@ typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;      // of the kernels below, where a configuration does not say otherwise
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTileRows = 128;     // most rows of a tile
 constexpr int kItemCost = 2;       // key tiles that taking up an item is worth
@@ -55,9 +55,9 @@ struct Args {
     void* out;
     float* lse;
     int B, N_cap, H, H_stream, G, n_groups, T_cap;
-    int P, max_pages, n_pages;
+    int P, p_shift, max_pages, n_pages;  // p_shift: log2(P), or -1 if P is no power of two
     uint32_t page_slots;                    // slots that a page advances by
-    long long head_stride, tail_stride, v_stride;  // bytes from a slot to the next
+    uint32_t head_stride, tail_stride, v_stride;   // bytes from a slot to the next
     long long head_hk, v_hk;                // bytes from a stream head to the next
     float scale, scale_log2;  // softmax scale, and times log2(e)
     int nb, shares_cap, min_share, m_cap;
@@ -135,11 +135,11 @@ __device__ __forceinline__ Seq sequence(const Args& a, int s) {
     return q;
 }
 
-__device__ __forceinline__ int ceil_div(int x, int y) { return (x + y - 1) / y; }
+__device__ __forceinline__ int ceil_div(int x, int y) { return (int)((uint32_t)(x + y - 1) / (uint32_t)y); }  // 0 <= x, 0 < y
 
 template <class C>
 __device__ __forceinline__ int row_tiles_of(const Args& a, const Seq& q) {
-    return (int)(((long long)q.rows * a.G + C::kM - 1) / C::kM);
+    return ceil_div(q.rows * a.G, C::kM);
 }
 
 // Key tiles of row tile rt.
@@ -175,33 +175,36 @@ __device__ __forceinline__ long long sequence_units(const Args& a, const Seq& q)
     return units_before<C>(a, q, row_tiles_of<C>(a, q)) * a.H_stream;
 }
 
+// Units are 64-bit numbers below 2^53: a quotient is taken in fp64 and put right where it is one off.
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+    long long q = (long long)((double)x / (double)y);
+    q -= q * y > x;
+    return q + ((q + 1) * y <= x);
+}
+
 struct Line {
-    long long total;
-    int shares;
+    long long each;        // units of a share, one more in the first `longer` shares
+    int longer, shares;
     int seq;               // sequence in which this share begins
     long long seq_start;   // its first unit
     long long lo, hi;      // this share
+    __device__ __forceinline__ long long begin(int s) const { return each * s + min(s, longer); }
+    __device__ __forceinline__ int share_of(long long u) const {
+        const long long head = (each + 1) * longer;
+        return (int)(u < head ? quotient(u, each + 1) : longer + quotient(u - head, each));
+    }
 };
-
-__device__ __forceinline__ long long share_begin(long long total, int shares, int s) { return total * s / shares; }
-
-__device__ __forceinline__ int share_of(long long total, int shares, long long u) {
-    int s = (int)(u * shares / total);
-    while (s + 1 < shares && share_begin(total, shares, s + 1) <= u) ++s;
-    while (s > 0 && share_begin(total, shares, s) > u) --s;
-    return s;
-}
 
 __device__ __forceinline__ long long shfl_up64(long long v, int d) {
     const int lo = __shfl_up((int)(uint32_t)v, d, kWave), hi = __shfl_up((int)(v >> 32), d, kWave);
     return ((long long)hi << 32) | (uint32_t)lo;
 }
 
-// Adds up the line; `scratch`: LDS for kThreads + 1 sums.
+// Adds up the line; `scratch`: LDS for C::kBlocC::kBlockThreads and one sum per wave.
 template <class C>
 __device__ __forceinline__ Line find_share(const Args& a, int share, long long* scratch) {
     const int n = n_sequences<C::kOp>(a), tid = threadIdx.x;
-    const int each = ceil_div(n, kThreads);
+    const int each = ceil_div(n, C::kBlockThreads);
     const int s0 = min(tid * each, n), s1 = min(s0 + each, n);
     long long mine = 0;
     for (int s = s0; s < s1; ++s) mine += sequence_units<C>(a, sequence<C::kOp>(a, s));
@@ -211,21 +214,23 @@ __device__ __forceinline__ Line find_share(const Args& a, int share, long long* 
         const long long up = shfl_up64(upto, o);
         if ((tid & (kWave - 1)) >= o) upto += up;
     }
-    if ((tid & (kWave - 1)) == kWave - 1) scratch[kThreads + (tid >> 6)] = upto;
+    if ((tid & (kWave - 1)) == kWave - 1) scratch[C::kBlockThreads + (tid >> 6)] = upto;
     __syncthreads();
-    for (int w = 0; w < (tid >> 6); ++w) upto += scratch[kThreads + w];
+    for (int w = 0; w < (tid >> 6); ++w) upto += scratch[C::kBlockThreads + w];
     scratch[tid] = upto;
     __syncthreads();
     Line l;
-    l.total = scratch[kThreads - 1];
-    l.shares = (int)min((long long)a.nb, max(1LL, l.total / a.min_share));
+    const long long total = scratch[C::kBlockThreads - 1];
+    l.shares = (int)max(1LL, min((long long)a.nb, quotient(total, a.min_share)));
+    l.each = quotient(total, l.shares);
+    l.longer = (int)(total - l.each * l.shares);
     l.seq = n;
-    l.seq_start = l.total;
+    l.seq_start = total;
     l.lo = l.hi = 0;
-    if (l.total > 0 && share < l.shares) {
-        l.lo = share_begin(l.total, l.shares, share);
-        l.hi = share_begin(l.total, l.shares, share + 1);
-        int first = 0, last = kThreads - 1;  // the chunk of sequences that holds unit lo
+    if (total > 0 && share < l.shares) {
+        l.lo = l.begin(share);
+        l.hi = l.begin(share + 1);
+        int first = 0, last = C::kBlockThreads - 1;  // the chunk of sequences that holds unit lo
         while (first < last) {
             const int mid = (first + last) >> 1;
             if (scratch[mid] <= l.lo) first = mid + 1; else last = mid;
@@ -260,18 +265,26 @@ struct Piece {
 struct Place {
     int row, head;
 };
-__device__ __forceinline__ Place place_of(const Args& a, int row0, int hk, long long r) {
-    const int j = (int)(r / a.G);
-    return Place{row0 + j, hk * a.G + (int)(r - (long long)j * a.G)};
+__device__ __forceinline__ Place place_of(const Args& a, int row0, int hk, int r) {
+    const int j = (int)((uint32_t)r / (uint32_t)a.G);
+    return Place{row0 + j, hk * a.G + (r - j * a.G)};
 }
 
-// Slot of key `key` of a sequence (kept inside its table and the pool).
+// Where a key of a sequence lies: its page as the table has it (fetched ahead of use) and its place there.
+struct Where {
+    int page;
+    uint32_t place;
+};
 template <int OP>
-__device__ __forceinline__ uint32_t slot_of(const Args& a, const Seq& q, int key) {
-    if constexpr (OP == kExpanded) return q.first + (uint32_t)key;
-    const uint32_t pg = (uint32_t)key / (uint32_t)a.P;
-    const int page = clamp_to(a.bt[(size_t)q.table * a.max_pages + pg], 0, a.n_pages - 1);
-    return (uint32_t)page * a.page_slots + ((uint32_t)key - pg * (uint32_t)a.P);
+__device__ __forceinline__ Where find_key(const Args& a, const Seq& q, int key) {
+    if constexpr (OP == kExpanded) return Where{0, q.first + (uint32_t)key};
+    const uint32_t pg = a.p_shift >= 0 ? (uint32_t)key >> a.p_shift : (uint32_t)key / (uint32_t)a.P;
+    return Where{a.bt[(size_t)q.table * a.max_pages + pg], (uint32_t)key - pg * (uint32_t)a.P};
+}
+template <int OP>
+__device__ __forceinline__ uint32_t slot_of(const Args& a, Where w) {  // (inside the pool whatever the table holds)
+    if constexpr (OP == kExpanded) return w.place;
+    return (uint32_t)clamp_to(w.page, 0, a.n_pages - 1) * a.page_slots + w.place;
 }
 
 __device__ __forceinline__ uint32_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
@@ -290,8 +303,7 @@ __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.
 // weights refer to (-inf: no key), their sum l.
 template <class C, class ForEach4>
 __device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_tile, bool first_lane, float m, float l, ForEach4 each) {
-    const long long packed = (long long)p.rt * C::kM + r_tile;
-    const Place at = place_of(a, p.q.row0, p.hk, packed);
+    const Place at = place_of(a, p.q.row0, p.hk, p.rt * C::kM + r_tile);
     const size_t row = (size_t)at.row * a.H + at.head;
     const bool prefix = C::kOp == kShared && p.q.base == 1 << 30;
     const bool joined = C::kOp == kShared && (prefix || p.q.k_begin > 0);  // two items make the row
@@ -337,7 +349,7 @@ __device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_t
 template <int OP, int KH, int KT, int DV, class IN, class OUT>
 struct Simple {
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
-    static constexpr int kM = 64, kKeys = 64, kPerSimd = 1;
+    static constexpr int kM = 64, kKeys = 64, kBlockThreads = kThreads, kPerUnit = 1;  // (kPerUnit: workgroups of a compute unit)
     typedef IN In;
     typedef OUT Out;
 };
@@ -352,17 +364,17 @@ __device__ __forceinline__ f32x4 load4(const uint16_t* p) {
 }
 
 // Last key that packed row r sees.
-__device__ __forceinline__ int last_key(const Args& a, const Seq& q, long long r) {
-    return (int)min((long long)q.k_end - 1, (long long)q.base + r / a.G);
+__device__ __forceinline__ int last_key(const Args& a, const Seq& q, int r) {
+    return min(q.k_end - 1, q.base + (int)((uint32_t)r / (uint32_t)a.G));
 }
 
 template <class C>
 __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
     typedef typename C::In In;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lg = lane >> 4;
-    const long long n_packed = (long long)p.q.rows * a.G, first = (long long)p.rt * C::kM + wave * 16;
+    const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + wave * 16;
     if (first >= n_packed) return;
-    const long long r = min(first + li, n_packed - 1);
+    const int r = min(first + li, n_packed - 1);
     const Place at = place_of(a, p.q.row0, p.hk, r);
     const In* qp = (const In*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
     f32x4 q[C::kDk / 16];
@@ -376,7 +388,7 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
     const int k_first = p.q.k_begin + p.t0 * C::kKeys, k_last = min(p.q.k_begin + p.t1 * C::kKeys, p.q.k_end);
 #pragma unroll 1
     for (int kb = k_first; kb < k_last; kb += 16) {
-        const uint32_t slot = slot_of<C::kOp>(a, p.q, min(kb + li, k_last - 1));
+        const uint32_t slot = slot_of<C::kOp>(a, find_key<C::kOp>(a, p.q, min(kb + li, k_last - 1)));
         const In* kh = (const In*)(a.k_head + (size_t)slot * a.head_stride + (size_t)p.hk * a.head_hk);
         f32x4 z = {0, 0, 0, 0};
 #pragma unroll
@@ -458,6 +470,326 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
         });
 }
 
+// ---------------------------------------------------------------------------------------------------------------
+// bf16: a workgroup takes 128 rows and 64 keys at a time through LDS.
+//
+// Heads of 64 and 128: a wave takes 32 rows.  S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds, of 32
+// keys, the scores of one row (row = lane % 32, keys 8 (e / 4) + 4 (lane / 32) + e % 4 for e < 16), so that statistics of a row
+// take one exchange between the lane halves, and eight scores in a row are the operand of P^T for 16 keys, if V^T is read with
+// its keys in the same order: two transposing LDS reads of four keys each.  The queries stay in registers, scores and weights
+// never leave them.  K and V go from memory to LDS without passing through registers, the next tile while this one is computed.
+//
+// Latents: 32 rows of 512 sums and 576 query elements would take 400 of a lane's registers; a wave takes 16 rows, on
+// v_mfma_f32_16x16x32_bf16 (a lane: row lane % 16, keys 4 (lane / 16) + e of each 16), and a workgroup has eight waves.
+//
+// LDS rows are read across (16 bytes of each of 16 or 32 keys) and, for V^T, in blocks of 4 keys x 32 bytes; their 16-byte chunks
+// are permuted by row such that both reach all banks.
+// ---------------------------------------------------------------------------------------------------------------
+template <int OP, int KH, int KT, int DV, class OUT>
+struct Tiled {
+    static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
+    static constexpr bool kAlias = OP == kLatent;     // values are the first part of the keys
+    static constexpr bool kPair = sizeof(OUT) == 4;   // weights enter the second product as a pair of bf16
+    static constexpr int kM = kTileRows, kKeys = 64;
+    static constexpr int kRows = kAlias ? 16 : 32;    // of a wave
+    static constexpr int kBlockThreads = kM / kRows * kWave, kWaves = kBlockThreads / kWave;
+    static constexpr int kPerUnit = 8 / kWaves;       // workgroups of a compute unit, two waves to a SIMD
+    static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kAlias ? 0 : kTailAt + kKeys * KT * 2;
+    static constexpr int kBuf = kTailAt + kKeys * KT * 2 + (kAlias ? 0 : kKeys * DV * 2);
+    typedef uint16_t In;
+    typedef OUT Out;
+};
+
+// Where chunk c of LDS row `row` with CH chunks of 16 bytes lies: at c ^ permutation.
+template <int CH>
+__device__ __forceinline__ int permutation(int row) { return CH >= 16 ? (row & 7) << 1 : CH == 8 ? row & 7 : (row >> 2) & 3; }
+
+__device__ __forceinline__ void to_lds(const char* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// A wave's part of 64 rows of CH chunks: rows (wave * kEach + i) * kRows ..; lane k of the wave holds the slot of row k.
+template <int CH, int WAVES>
+__device__ __forceinline__ void load_rows(const char* base, uint32_t stride, uint32_t slot, char* to, int wave, int lane) {
+    constexpr int kRows = 64 / CH, kLoads = 64 / kRows, kEach = (kLoads + WAVES - 1) / WAVES;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (kLoads % WAVES != 0 && wave * kEach + i >= kLoads) break;
+        const int row0 = (wave * kEach + i) * kRows, row = row0 + lane / CH;
+        const uint32_t at = kRows == 1 ? (uint32_t)__builtin_amdgcn_readlane((int)slot, row0) : (uint32_t)__shfl((int)slot, row, kWave);
+        to_lds(base + (uint64_t)at * stride + (((lane % CH) ^ permutation<CH>(row)) << 4), to + row0 * CH * 16);
+    }
+}
+
+template <class C>
+__device__ __forceinline__ void load_tile(const Args& a, const Piece& p, uint32_t slot, char* buf, int wave, int lane) {
+    load_rows<C::kHead / 8, C::kWaves>(a.k_head + (size_t)p.hk * a.head_hk, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
+    if constexpr (C::kTail > 0) load_rows<C::kTail / 8, C::kWaves>(a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
+    if constexpr (!C::kAlias) load_rows<C::kDv / 8, C::kWaves>(a.v + (size_t)p.hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
+}
+
+__device__ __forceinline__ float other_half(float x) {  // of the lane 32 further
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    const uint32_t lo = both[0], hi = both[1];
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? lo : hi);
+}
+
+// Kinds of elements of an operand: the finite ones, or 1 where an element is of the kind.
+enum : int { kFinite = 0, kUp = 1, kDown = 2, kNan = 3 };
+template <int KIND>
+__device__ __forceinline__ bf16x8 elements(s16x8 x) {
+    s16x8 y;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint16_t b = (uint16_t)x[k];
+        const bool odd = (b & 0x7f80u) == 0x7f80u;
+        if (KIND == kFinite) y[k] = (short)(odd ? 0 : b);
+        else y[k] = (short)((KIND == kNan ? odd && (b & 0x7fu) : b == (KIND == kUp ? 0x7f80u : 0xff80u)) ? 0x3f80 : 0);
+    }
+    return __builtin_bit_cast(bf16x8, y);
+}
+
+template <class C>
+struct Rows {
+    static constexpr int kStep = C::kRows == 16 ? 32 : 16;    // elements of a key that one instruction takes
+    static constexpr int kBlock = C::kRows == 16 ? 16 : 32;   // columns that one instruction makes
+    typedef std::conditional_t<C::kRows == 16, f32x4, f32x16> Acc;
+    static constexpr int kHeadSteps = C::kHead / kStep, kTailSteps = C::kTail / kStep, kBlocks = C::kDv / kBlock;
+    // 16-byte chunks by which an operand's places differ repeat after 16 (128 elements)
+    static constexpr int kOwnK = std::min(kHeadSteps, 128 / kStep), kOwnV = std::min(kBlocks, 128 / kBlock);
+    bf16x8 q[kHeadSteps + kTailSteps];
+    Acc acc[kBlocks];
+    float m, l;          // exponent reference (times log2(e)), sum of this lane's weights
+    int seen;            // last key of the lane's row
+    // LDS offsets of the lane's operands, as far as the permutation of chunks makes them its own
+    int k_at[kOwnK], tail_at[std::max(kTailSteps, 1)], v_at[kOwnV];
+
+    __device__ __forceinline__ void place_operands(int lane) {
+        const int li = lane % C::kRows, h = lane / C::kRows;
+        constexpr int CH = C::kHead / 8, CT = C::kTail / 8, CV = C::kDv / 8, kPer = kStep / 8;
+#pragma unroll
+        for (int s = 0; s < kOwnK; ++s) k_at[s] = li * CH * 16 + (((kPer * s + h) ^ permutation<CH>(li)) << 4);
+        if constexpr (CT > 0)
+#pragma unroll
+            for (int s = 0; s < kTailSteps; ++s) tail_at[s] = li * CT * 16 + (((kPer * s + h) ^ permutation<CT>(li)) << 4);
+        // lane g of 16 fetches 8 bytes of key row g / 4 of four, for 16 columns
+        const int g = lane & 15, group = lane >> 4;
+        const int r = C::kRows == 16 ? 4 * group + (g >> 2) : 4 * h + (g >> 2), column = C::kRows == 16 ? 0 : 16 * (group & 1);
+#pragma unroll
+        for (int b = 0; b < kOwnV; ++b) v_at[b] = r * CV * 16 + (g & 1) * 8 + ((((kBlock * b + column) / 8 + ((g & 3) >> 1)) ^ permutation<CV>(r)) << 4);
+    }
+};
+
+__device__ __forceinline__ f32x16 product(bf16x8 x, bf16x8 y, f32x16 sum) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, sum, 0, 0, 0); }
+__device__ __forceinline__ f32x4 product(bf16x8 x, bf16x8 y, f32x4 sum) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, sum, 0, 0, 0); }
+
+template <int KIND, int N, class Acc>
+__device__ __forceinline__ void take_kind(Acc& acc, const s16x8 (&v)[N], const bf16x8 (&weights)[N], float value) {
+    Acc t;
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(Acc) / 4); ++e) t[e] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < N; ++s) t = product(elements<KIND>(v[s]), weights[s], t);
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(Acc) / 4); ++e) acc[e] += t[e] != 0.0f ? value : 0.0f;
+}
+
+// The largest, or the sum, of a row's values over the lanes that hold it.
+template <int ROWS>
+__device__ __forceinline__ float row_max(float x) {
+    if constexpr (ROWS == 16) x = fmaxf(x, __shfl_xor(x, 16, kWave));
+    return fmaxf(x, other_half(x));
+}
+template <int ROWS>
+__device__ __forceinline__ float row_sum(float x) {
+    if constexpr (ROWS == 16) x += __shfl_xor(x, 16, kWave);
+    return x + other_half(x);
+}
+
+// 32 keys of the tile in `buf`.
+template <class C, bool MASKED>
+__device__ __forceinline__ void take_keys(Rows<C>& w, const char* buf, int block, int key0, float scale_log2, int lane) {
+    typedef Rows<C> R;
+    constexpr int kParts = C::kRows == 16 ? 2 : 1;                       // instructions' worth of keys among the 32
+    constexpr int kScores = 32 * C::kRows / kWave, kEach = kScores / kParts;  // scores of a lane: 8 or 16
+    constexpr int kKeysPart = 32 / kParts, kSteps = C::kRows == 16 ? 1 : 2;  // steps of the second product
+    const int h = lane / C::kRows;
+    typename R::Acc part[kParts];
+    {
+        constexpr int CH = C::kHead / 8;
+#pragma unroll
+        for (int u = 0; u < kParts; ++u)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) part[u][e] = 0.0f;
+        const char* row = buf + C::kHeadAt + block * 32 * CH * 16;
+#pragma unroll
+        for (int s = 0; s < R::kHeadSteps; ++s)  // (the permutation concerns the last bits of a chunk's number only)
+#pragma unroll
+            for (int u = 0; u < kParts; ++u) {
+                const bf16x8 k = *reinterpret_cast<const bf16x8*>(row + u * kKeysPart * CH * 16 + w.k_at[s % R::kOwnK] + (s / R::kOwnK) * 256);
+                part[u] = product(k, w.q[s], part[u]);
+            }
+    }
+    if constexpr (C::kTail > 0) {
+        constexpr int CH = C::kTail / 8;
+        const char* row = buf + C::kTailAt + block * 32 * CH * 16;
+#pragma unroll
+        for (int s = 0; s < R::kTailSteps; ++s)
+#pragma unroll
+            for (int u = 0; u < kParts; ++u) {
+                const bf16x8 k = *reinterpret_cast<const bf16x8*>(row + u * kKeysPart * CH * 16 + w.tail_at[s]);
+                part[u] = product(k, w.q[R::kHeadSteps + s], part[u]);
+            }
+    }
+    float z[kScores];  // key (e / kEach) * kKeysPart + 8 ((e % kEach) / 4) + 4 h + e % 4
+#pragma unroll
+    for (int e = 0; e < kScores; ++e) z[e] = part[e / kEach][e % kEach];
+    bool careful = false;  // the tile holds values that are not finite, in front of rows that do not see them
+    if constexpr (MASKED) {
+        if constexpr (C::kAlias) {  // such a value is in the key, too, and has made its scores infinite or NaN
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kScores; ++e) sum += z[e] - z[e];
+            careful = __any(sum != 0.0f);
+        }
+#pragma unroll
+        for (int e = 0; e < kScores; ++e)
+            z[e] = key0 + (e / kEach) * kKeysPart + 8 * (e % kEach >> 2) + 4 * h + (e & 3) <= w.seen ? z[e] : -INFINITY;
+    }
+    float top = fmaxf(z[0], z[1]);
+#pragma unroll
+    for (int e = 2; e < kScores; ++e) top = fmaxf(top, z[e]);
+    top = row_max<C::kRows>(top) * scale_log2;
+    // The reference follows the largest score only where that is more than a factor of 2^8 ahead of it: weights up to 2^8 lose
+    // nothing, and the accumulators are rescaled a few times per row instead of a few times per tile.
+    if (__any(top > w.m + 8.0f)) {
+        const float m = top > w.m + 8.0f ? top : w.m;
+        const float alpha = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - m);
+        w.m = m;
+        w.l *= alpha;
+#pragma unroll
+        for (int b = 0; b < R::kBlocks; ++b) w.acc[b] *= alpha;
+    }
+    const float m = w.m == -INFINITY ? 0.0f : w.m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kScores; ++e) {
+        z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -m));
+        sum += z[e];
+    }
+    w.l += sum;
+    bf16x8 hi[kSteps], lo[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            hi[s][e] = (__bf16)z[8 * s + e];
+            if constexpr (C::kPair) lo[s][e] = (__bf16)(z[8 * s + e] - (float)hi[s][e]);
+        }
+    constexpr int CH = C::kDv / 8, kApart = C::kRows == 16 ? 16 : 8;  // key rows between an operand's two halves
+    const char* row = buf + C::kVAt + block * 32 * CH * 16;
+#pragma unroll
+    for (int b = 0; b < R::kBlocks; ++b) {
+        s16x8 v[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const char* at = row + 16 * s * CH * 16 + w.v_at[b % R::kOwnV] + (b / R::kOwnV) * 256;
+            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + kApart * CH * 16));
+            v[s] = s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        }
+        if constexpr (MASKED) {
+            if constexpr (!C::kAlias) {
+                bool odd = false;
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) odd |= ((uint16_t)v[s][k] & 0x7f80u) == 0x7f80u;
+                careful = __any(odd);
+            }
+            if (careful) {
+                // a value that is not finite must not meet the zero weight of a row that does not see it: each kind is
+                // multiplied as 1 and takes its place only in rows that give it weight
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    w.acc[b] = product(elements<kFinite>(v[s]), hi[s], w.acc[b]);
+                    if constexpr (C::kPair) w.acc[b] = product(elements<kFinite>(v[s]), lo[s], w.acc[b]);
+                }
+                take_kind<kUp>(w.acc[b], v, hi, INFINITY);
+                take_kind<kDown>(w.acc[b], v, hi, -INFINITY);
+                take_kind<kNan>(w.acc[b], v, hi, __builtin_nanf(""));
+                continue;
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const bf16x8 x = __builtin_bit_cast(bf16x8, v[s]);
+            if constexpr (C::kPair) w.acc[b] = product(x, lo[s], w.acc[b]);
+            w.acc[b] = product(x, hi[s], w.acc[b]);
+        }
+    }
+}
+
+template <class C>
+__device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* buf0, char* buf1) {
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), li = lane % C::kRows, h = lane / C::kRows;
+    const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + wave * C::kRows;
+    const bool active = first < n_packed;  // a wave without rows helps to load
+    typedef Rows<C> R;
+    R w;
+    w.m = -INFINITY;
+    w.l = 0.0f;
+    w.seen = -1;
+    w.place_operands(lane);
+#pragma unroll
+    for (int b = 0; b < R::kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < (int)(sizeof(typename R::Acc) / 4); ++e) w.acc[b][e] = 0.0f;
+    int seen_first = 0, seen_last = 0;  // by the wave's first and last row
+    if (active) {
+        const int r = min(first + li, n_packed - 1);
+        const Place at = place_of(a, p.q.row0, p.hk, r);
+        const uint16_t* qp = (const uint16_t*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
+#pragma unroll
+        for (int s = 0; s < C::kDk / R::kStep; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(qp + R::kStep * s + 8 * h);
+        w.seen = last_key(a, p.q, r);
+        seen_first = last_key(a, p.q, first);
+        seen_last = last_key(a, p.q, min(first + C::kRows - 1, n_packed - 1));
+    }
+    auto find = [&](int t) { return find_key<C::kOp>(a, p.q, min(p.q.k_begin + t * C::kKeys + lane, p.q.k_end - 1)); };
+    __syncthreads();  // nobody reads the buffers any more
+    if (p.t0 < p.t1) {
+        int t = p.t0;
+        load_tile<C>(a, p, slot_of<C::kOp>(a, find(t)), buf0, wave, lane);
+        Where next = find(min(t + 1, p.t1 - 1));
+        auto step = [&](char* now, char* then) {
+            __syncthreads();  // the tile has arrived, and nobody reads the other buffer any more
+            if (t + 1 < p.t1) {
+                load_tile<C>(a, p, slot_of<C::kOp>(a, next), then, wave, lane);
+                next = find(min(t + 2, p.t1 - 1));
+            }
+            const int key0 = p.q.k_begin + t * C::kKeys;
+            if (active && key0 <= seen_last) {
+#pragma unroll 1
+                for (int block = 0; block < 2; ++block) {
+                    if (key0 + 32 * block + 31 <= seen_first) take_keys<C, false>(w, now, block, key0 + 32 * block, a.scale_log2, lane);
+                    else if (key0 + 32 * block <= seen_last) take_keys<C, true>(w, now, block, key0 + 32 * block, a.scale_log2, lane);
+                }
+            }
+            return ++t < p.t1;
+        };
+        while (step(buf0, buf1) && step(buf1, buf0)) {}
+    }
+    w.l = row_sum<C::kRows>(w.l);
+    if (active && first + li < n_packed)
+        hand_over<C>(a, p, wave * C::kRows + li, h == 0, w.m * kLn2, w.l, [&](auto put) {
+#pragma unroll
+            for (int b = 0; b < R::kBlocks; ++b)
+#pragma unroll
+                for (int g = 0; g < C::kRows / 16 * C::kRows / 16; ++g) put(R::kBlock * b + 8 * g + 4 * h, f32x4{w.acc[b][4 * g], w.acc[b][4 * g + 1], w.acc[b][4 * g + 2], w.acc[b][4 * g + 3]});
+        });
+}
+
 // Items of a share, one after the other.
 template <class C, class Run>
 __device__ __forceinline__ void walk(const Args& a, int share, const Line& line, Run run) {
@@ -469,7 +801,7 @@ __device__ __forceinline__ void walk(const Args& a, int share, const Line& line,
         const Seq q = sequence<C::kOp>(a, s);
         const int tiles = row_tiles_of<C>(a, q);
         const long long head_units = units_before<C>(a, q, tiles);
-        int hk = seq_start < line.lo ? (int)((line.lo - seq_start) / head_units) : 0;
+        int hk = seq_start < line.lo && head_units > 0 ? (int)quotient(line.lo - seq_start, head_units) : 0;
         if (tiles > 0)
             for (; hk < a.H_stream; ++hk) {
                 const long long head_start = seq_start + hk * head_units;
@@ -499,12 +831,11 @@ __device__ __forceinline__ void walk(const Args& a, int share, const Line& line,
                     p.pieces = 1;
                     if (nk == 0 ? item < line.lo : p.t0 >= p.t1) continue;  // nothing of it is this share's
                     if (!p.whole) {
-                        p.share0 = share_of(line.total, line.shares, item + kItemCost);
-                        p.pieces = share_of(line.total, line.shares, item + kItemCost + nk - 1) - p.share0 + 1;
+                        p.share0 = line.share_of(item + kItemCost);
+                        p.pieces = line.share_of(item + kItemCost + nk - 1) - p.share0 + 1;
                         p.slot = 2 * share + (p.t0 == 0 ? 1 : 0);  // an item that begins here, or one that began before
                         if (C::kOp != kShared && p.t0 == 0 && threadIdx.x == 0) {
-                            const long long first = (long long)rt * C::kM, rows = min((long long)q.rows * a.G - first, (long long)C::kM);
-                            desc[1] = q.row0; desc[2] = hk; desc[3] = rt; desc[4] = (int)rows;
+                            desc[1] = q.row0; desc[2] = hk; desc[3] = rt; desc[4] = min(q.rows * a.G - rt * C::kM, C::kM);
                             desc[0] = p.pieces;
                         }
                     }
@@ -522,12 +853,32 @@ __device__ __forceinline__ int share_of_block(int block, int nb) {
 }
 
 template <class C>
-__global__ __launch_bounds__(kThreads, C::kPerSimd) void simple_kernel(Args a) {
+__global__ __launch_bounds__(C::kBlockThreads, 1) void simple_kernel(Args a) {
     __shared__ long long scratch[kThreads + kWaves];
     const int share = share_of_block(blockIdx.x, a.nb);
     const Line line = find_share<C>(a, share, scratch);
     walk<C>(a, share, line, [&](const Piece& p) { run_simple<C>(a, p); });
 }
+
+template <class C>
+__global__ __launch_bounds__(C::kBlockThreads, 2) void tiled_kernel(Args a) {  // (256 registers: two waves on a SIMD)
+    __shared__ __align__(1024) char buf0[C::kBuf];
+    __shared__ __align__(1024) char buf1[C::kBuf];
+    const int share = share_of_block(blockIdx.x, a.nb);
+    const Line line = find_share<C>(a, share, reinterpret_cast<long long*>(buf0));
+    walk<C>(a, share, line, [&](const Piece& p) { run_tiled<C>(a, p, buf0, buf1); });
+}
+
+template <class C>
+struct Kernel;
+template <int OP, int KH, int KT, int DV, class IN, class OUT>
+struct Kernel<Simple<OP, KH, KT, DV, IN, OUT>> {
+    static constexpr auto run = simple_kernel<Simple<OP, KH, KT, DV, IN, OUT>>;
+};
+template <int OP, int KH, int KT, int DV, class OUT>
+struct Kernel<Tiled<OP, KH, KT, DV, OUT>> {
+    static constexpr auto run = tiled_kernel<Tiled<OP, KH, KT, DV, OUT>>;
+};
 
 // Sums of a row's pieces, joined: a wave per row, D_v / 64 columns a lane.
 template <int DV>
@@ -577,7 +928,7 @@ __global__ __launch_bounds__(kThreads) void join_shares_kernel(Args a) {
             const size_t at = (size_t)(2 * (share + k) + (k == 0 ? 1 : 0)) * a.m_cap + r;
             sum.add(a.part_o + at * C::kDv, a.part_ml + at * 2, lane);
         }
-        const Place to = place_of(a, desc[1], desc[2], (long long)desc[3] * C::kM + r);
+        const Place to = place_of(a, desc[1], desc[2], desc[3] * C::kM + r);
         const size_t row = (size_t)to.row * a.H + to.head;
         sum.write((typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
     }
@@ -615,8 +966,8 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
             sum.add(a.row_o + k * C::kDv, a.row_ml + k * 2, lane);
             return;
         }
-        const long long packed = (long long)(call_row - q.row0) * a.G + head % a.G;
-        const int r = clamp_to((int)(packed % C::kM), 0, a.m_cap - 1);
+        const int packed = max(call_row - q.row0, 0) * a.G + head % a.G;
+        const int r = min(packed % C::kM, a.m_cap - 1);
         for (int j = 0; j < pieces; ++j) {
             const int share = clamp_to(share0 + j, 0, a.shares_cap - 1);
             const size_t at = (size_t)(2 * share + (j == 0 ? 1 : 0)) * a.m_cap + r;
@@ -687,12 +1038,12 @@ inline int compute_units() {
 
 template <class C>
 int launch(Args a, int max_workgroups, void* stream, const char* who) {
-    int nb = compute_units() * C::kPerSimd;
-    if (max_workgroups > 0) nb = std::min(nb, max_workgroups * C::kPerSimd);
+    int nb = compute_units() * C::kPerUnit;
+    if (max_workgroups > 0) nb = std::min(nb, max_workgroups * C::kPerUnit);
     a.nb = std::min(nb, kSharesCap);
     a.min_share = kItemCost + 1;
     hipStream_t s = (hipStream_t)stream;
-    hipLaunchKernelGGL((simple_kernel<C>), dim3(a.nb), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((Kernel<C>::run), dim3(a.nb), dim3(C::kBlockThreads), 0, s, a);
     int rc = check_launch(who);
     if (rc != FSR_OK) return rc;
     if (C::kOp == kShared) {

@@ -37,8 +37,8 @@ Layout layout(const fsr_attn_params* p, int& m_cap) {
 template <int D>
 int run(const Args& a, const fsr_attn_params* p, void* stream, const char* who) {
     if (p->dtype == FSR_F32) return launch<Simple<kShared, D, 0, D, float, float>>(a, p->max_workgroups, stream, who);
-    if (p->out_dtype == FSR_F32) return launch<Simple<kShared, D, 0, D, uint16_t, float>>(a, p->max_workgroups, stream, who);
-    return launch<Simple<kShared, D, 0, D, uint16_t, uint16_t>>(a, p->max_workgroups, stream, who);
+    if (p->out_dtype == FSR_F32) return launch<Tiled<kShared, D, 0, D, float>>(a, p->max_workgroups, stream, who);
+    return launch<Tiled<kShared, D, 0, D, uint16_t>>(a, p->max_workgroups, stream, who);
 }
 
 }  // namespace
@@ -79,8 +79,9 @@ extern "C" int fsr_verify_attention_shared(const void* q, const void* k_cache, c
     a.out = out; a.lse = lse;
     a.B = p->B; a.N_cap = p->N_cap; a.H = p->H_q; a.H_stream = p->H_kv; a.G = p->H_q / p->H_kv; a.n_groups = n_groups;
     a.P = p->P; a.max_pages = p->max_pages; a.n_pages = p->n_pages;
+    a.p_shift = (p->P & (p->P - 1)) == 0 ? __builtin_ctz((unsigned)p->P) : -1;
     a.page_slots = (uint32_t)(token_major ? p->P : p->P * p->H_kv);
-    a.head_stride = a.v_stride = token_major ? p->H_kv * row : row;
+    a.head_stride = a.v_stride = (uint32_t)(token_major ? p->H_kv * row : row);
     a.head_hk = a.v_hk = token_major ? row : p->P * row;
     a.scale = p->scale;
     a.scale_log2 = p->scale * kLog2e;
