@@ -3,7 +3,7 @@
 // paged cache before its attention (fsr_latent_append), come back as contiguous rows for the expanded form
 // (fsr_latent_gather), and are attended over directly by queries that have been taken into the latent's space
 // (fsr_latent_attention).
-#include "row_tiles.hpp"
+#include "latent_tiles.hpp"
 
 namespace fsr {
 namespace {
@@ -121,8 +121,8 @@ int rows_cap(const fsr_latent_params* p) { return (int)std::max(1LL, std::min((l
 template <int DL, int DR>
 int run(const Args& a, const fsr_latent_params* p, void* stream, const char* who) {
     if (p->dtype == FSR_F32) return launch<Simple<kLatent, DL, DR, DL, float, float>>(a, p->max_workgroups, stream, who);
-    if (p->out_dtype == FSR_F32) return launch<Tiled<kLatent, DL, DR, DL, float>>(a, p->max_workgroups, stream, who);
-    return launch<Tiled<kLatent, DL, DR, DL, uint16_t>>(a, p->max_workgroups, stream, who);
+    if (p->out_dtype == FSR_F32) return launch<Latent<DL, DR, float>>(a, p->max_workgroups, stream, who);
+    return launch<Latent<DL, DR, uint16_t>>(a, p->max_workgroups, stream, who);
 }
 
 }  // namespace

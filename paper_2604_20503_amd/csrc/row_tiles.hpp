@@ -38,6 +38,7 @@ constexpr int kItemCost = 2;       // key tiles that taking up an item is worth
 constexpr int kDescInts = 8;       // merge descriptor of a share
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kAhead = 40.0f;    // distance of a row's exponent reference from its largest score, in powers of two
 
 enum : int { kLatent = 0, kExpanded = 1, kShared = 2 };
 
@@ -471,31 +472,26 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// bf16: a workgroup takes 128 rows and 64 keys at a time through LDS.
+// bf16, heads of 64 and 128: a workgroup takes 128 rows, a wave 32 of them, and 64 keys at a time through LDS.
 //
-// Heads of 64 and 128: a wave takes 32 rows.  S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds, of 32
-// keys, the scores of one row (row = lane % 32, keys 8 (e / 4) + 4 (lane / 32) + e % 4 for e < 16), so that statistics of a row
-// take one exchange between the lane halves, and eight scores in a row are the operand of P^T for 16 keys, if V^T is read with
-// its keys in the same order: two transposing LDS reads of four keys each.  The queries stay in registers, scores and weights
-// never leave them.  K and V go from memory to LDS without passing through registers, the next tile while this one is computed.
+// S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds, of 32 keys, the scores of one row (row = lane % 32,
+// keys 8 (e / 4) + 4 (lane / 32) + e % 4 for e < 16), so that statistics of a row take one exchange between the lane halves, and
+// eight scores in a row are the operand of P^T for 16 keys, if V^T is read with its keys in the same order: two transposing LDS
+// reads of four keys each.  The queries stay in registers, scores and weights never leave them.  K and V go from memory to LDS
+// without passing through registers, the next tile while this one is computed.
 //
-// Latents: 32 rows of 512 sums and 576 query elements would take 400 of a lane's registers; a wave takes 16 rows, on
-// v_mfma_f32_16x16x32_bf16 (a lane: row lane % 16, keys 4 (lane / 16) + e of each 16), and a workgroup has eight waves.
-//
-// LDS rows are read across (16 bytes of each of 16 or 32 keys) and, for V^T, in blocks of 4 keys x 32 bytes; their 16-byte chunks
-// are permuted by row such that both reach all banks.
+// LDS rows are read across (16 bytes of each of 32 keys) and, for V^T, in blocks of 4 keys x 32 bytes; their 16-byte chunks are
+// permuted by row such that both reach all banks.
 // ---------------------------------------------------------------------------------------------------------------
 template <int OP, int KH, int KT, int DV, class OUT>
 struct Tiled {
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
-    static constexpr bool kAlias = OP == kLatent;     // values are the first part of the keys
     static constexpr bool kPair = sizeof(OUT) == 4;   // weights enter the second product as a pair of bf16
     static constexpr int kM = kTileRows, kKeys = 64;
-    static constexpr int kRows = kAlias ? 16 : 32;    // of a wave
-    static constexpr int kBlockThreads = kM / kRows * kWave, kWaves = kBlockThreads / kWave;
-    static constexpr int kPerUnit = 8 / kWaves;       // workgroups of a compute unit, two waves to a SIMD
-    static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kAlias ? 0 : kTailAt + kKeys * KT * 2;
-    static constexpr int kBuf = kTailAt + kKeys * KT * 2 + (kAlias ? 0 : kKeys * DV * 2);
+    static constexpr int kBlockThreads = kThreads, kWaves = row_tiles::kWaves;
+    static constexpr int kPerUnit = 2;                // workgroups of a compute unit, two waves to a SIMD
+    static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kTailAt + kKeys * KT * 2;
+    static constexpr int kBuf = kVAt + kKeys * DV * 2;
     typedef uint16_t In;
     typedef OUT Out;
 };
@@ -521,11 +517,18 @@ __device__ __forceinline__ void load_rows(const char* base, uint32_t stride, uin
     }
 }
 
+// The tile's loads, which this wave has issued, have arrived, and so have everyone's behind the barrier; nobody reads what has been
+// read in front of it any more.
+__device__ __forceinline__ void arrive() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 template <class C>
 __device__ __forceinline__ void load_tile(const Args& a, const Piece& p, uint32_t slot, char* buf, int wave, int lane) {
     load_rows<C::kHead / 8, C::kWaves>(a.k_head + (size_t)p.hk * a.head_hk, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
     if constexpr (C::kTail > 0) load_rows<C::kTail / 8, C::kWaves>(a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
-    if constexpr (!C::kAlias) load_rows<C::kDv / 8, C::kWaves>(a.v + (size_t)p.hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
+    if constexpr (C::kOp != kLatent) load_rows<C::kDv / 8, C::kWaves>(a.v + (size_t)p.hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
 }
 
 __device__ __forceinline__ float other_half(float x) {  // of the lane 32 further
@@ -536,134 +539,97 @@ __device__ __forceinline__ float other_half(float x) {  // of the lane 32 furthe
 
 // Kinds of elements of an operand: the finite ones, or 1 where an element is of the kind.
 enum : int { kFinite = 0, kUp = 1, kDown = 2, kNan = 3 };
-template <int KIND>
-__device__ __forceinline__ bf16x8 elements(s16x8 x) {
+__device__ __forceinline__ bf16x8 elements(s16x8 x, int kind) {
     s16x8 y;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const uint16_t b = (uint16_t)x[k];
+        const uint32_t b = (uint16_t)x[k];
         const bool odd = (b & 0x7f80u) == 0x7f80u;
-        if (KIND == kFinite) y[k] = (short)(odd ? 0 : b);
-        else y[k] = (short)((KIND == kNan ? odd && (b & 0x7fu) : b == (KIND == kUp ? 0x7f80u : 0xff80u)) ? 0x3f80 : 0);
+        const int is = !odd ? kFinite : b == 0x7f80u ? kUp : b == 0xff80u ? kDown : kNan;
+        y[k] = (short)(is != kind ? 0u : odd ? 0x3f80u : b);
     }
     return __builtin_bit_cast(bf16x8, y);
+}
+// Adds the value of the kind where it has weight.
+__device__ __forceinline__ void put_odd(f32x16& acc, const f32x16& weight, int kind) {
+    const float value = kind == kUp ? INFINITY : kind == kDown ? -INFINITY : __builtin_nanf("");
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] += weight[e] != 0.0f ? value : 0.0f;
+}
+
+__device__ __forceinline__ f32x16 product(bf16x8 x, bf16x8 y, f32x16 sum) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, sum, 0, 0, 0); }
+__device__ __forceinline__ f32x16 zeros() {
+    f32x16 x;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+    return x;
+}
+// Eight keys of 32 columns, one column a lane: four keys at each of two places.
+__device__ __forceinline__ s16x8 transposed(const char* four, const char* other_four) {
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)four), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)other_four);
+    return s16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+}
+__device__ __forceinline__ bool any_odd(s16x8 x) {  // an element that is not finite
+    bool odd = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) odd |= ((uint16_t)x[k] & 0x7f80u) == 0x7f80u;
+    return odd;
 }
 
 template <class C>
 struct Rows {
-    static constexpr int kStep = C::kRows == 16 ? 32 : 16;    // elements of a key that one instruction takes
-    static constexpr int kBlock = C::kRows == 16 ? 16 : 32;   // columns that one instruction makes
-    typedef std::conditional_t<C::kRows == 16, f32x4, f32x16> Acc;
-    static constexpr int kHeadSteps = C::kHead / kStep, kTailSteps = C::kTail / kStep, kBlocks = C::kDv / kBlock;
-    // 16-byte chunks by which an operand's places differ repeat after 16 (128 elements)
-    static constexpr int kOwnK = std::min(kHeadSteps, 128 / kStep), kOwnV = std::min(kBlocks, 128 / kBlock);
+    static constexpr int kHeadSteps = C::kHead / 16, kTailSteps = C::kTail / 16, kBlocks = C::kDv / 32;
+    // LDS offsets of a lane's operands repeat after 16 chunks (128 elements): the permutation changes the last four bits of a chunk's number
+    static constexpr int kOwnK = std::min(kHeadSteps, 8), kOwnV = std::min(kBlocks, 4);
     bf16x8 q[kHeadSteps + kTailSteps];
-    Acc acc[kBlocks];
+    f32x16 acc[kBlocks];
     float m, l;          // exponent reference (times log2(e)), sum of this lane's weights
     int seen;            // last key of the lane's row
-    // LDS offsets of the lane's operands, as far as the permutation of chunks makes them its own
     int k_at[kOwnK], tail_at[std::max(kTailSteps, 1)], v_at[kOwnV];
 
     __device__ __forceinline__ void place_operands(int lane) {
-        const int li = lane % C::kRows, h = lane / C::kRows;
-        constexpr int CH = C::kHead / 8, CT = C::kTail / 8, CV = C::kDv / 8, kPer = kStep / 8;
+        const int li = lane & 31, h = lane >> 5;
+        constexpr int CH = C::kHead / 8, CT = C::kTail / 8, CV = C::kDv / 8;
 #pragma unroll
-        for (int s = 0; s < kOwnK; ++s) k_at[s] = li * CH * 16 + (((kPer * s + h) ^ permutation<CH>(li)) << 4);
+        for (int s = 0; s < kOwnK; ++s) k_at[s] = li * CH * 16 + (((2 * s + h) ^ permutation<CH>(li)) << 4);
         if constexpr (CT > 0)
 #pragma unroll
-            for (int s = 0; s < kTailSteps; ++s) tail_at[s] = li * CT * 16 + (((kPer * s + h) ^ permutation<CT>(li)) << 4);
+            for (int s = 0; s < kTailSteps; ++s) tail_at[s] = li * CT * 16 + (((2 * s + h) ^ permutation<CT>(li)) << 4);
         // lane g of 16 fetches 8 bytes of key row g / 4 of four, for 16 columns
-        const int g = lane & 15, group = lane >> 4;
-        const int r = C::kRows == 16 ? 4 * group + (g >> 2) : 4 * h + (g >> 2), column = C::kRows == 16 ? 0 : 16 * (group & 1);
+        const int g = lane & 15, r = 4 * h + (g >> 2), column = lane & 16;
 #pragma unroll
-        for (int b = 0; b < kOwnV; ++b) v_at[b] = r * CV * 16 + (g & 1) * 8 + ((((kBlock * b + column) / 8 + ((g & 3) >> 1)) ^ permutation<CV>(r)) << 4);
+        for (int b = 0; b < kOwnV; ++b) v_at[b] = r * CV * 16 + (g & 1) * 8 + ((((32 * b + column) / 8 + ((g & 3) >> 1)) ^ permutation<CV>(r)) << 4);
     }
 };
-
-__device__ __forceinline__ f32x16 product(bf16x8 x, bf16x8 y, f32x16 sum) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, sum, 0, 0, 0); }
-__device__ __forceinline__ f32x4 product(bf16x8 x, bf16x8 y, f32x4 sum) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, sum, 0, 0, 0); }
-
-template <int KIND, int N, class Acc>
-__device__ __forceinline__ void take_kind(Acc& acc, const s16x8 (&v)[N], const bf16x8 (&weights)[N], float value) {
-    Acc t;
-#pragma unroll
-    for (int e = 0; e < (int)(sizeof(Acc) / 4); ++e) t[e] = 0.0f;
-#pragma unroll
-    for (int s = 0; s < N; ++s) t = product(elements<KIND>(v[s]), weights[s], t);
-#pragma unroll
-    for (int e = 0; e < (int)(sizeof(Acc) / 4); ++e) acc[e] += t[e] != 0.0f ? value : 0.0f;
-}
-
-// The largest, or the sum, of a row's values over the lanes that hold it.
-template <int ROWS>
-__device__ __forceinline__ float row_max(float x) {
-    if constexpr (ROWS == 16) x = fmaxf(x, __shfl_xor(x, 16, kWave));
-    return fmaxf(x, other_half(x));
-}
-template <int ROWS>
-__device__ __forceinline__ float row_sum(float x) {
-    if constexpr (ROWS == 16) x += __shfl_xor(x, 16, kWave);
-    return x + other_half(x);
-}
 
 // 32 keys of the tile in `buf`.
 template <class C, bool MASKED>
 __device__ __forceinline__ void take_keys(Rows<C>& w, const char* buf, int block, int key0, float scale_log2, int lane) {
     typedef Rows<C> R;
-    constexpr int kParts = C::kRows == 16 ? 2 : 1;                       // instructions' worth of keys among the 32
-    constexpr int kScores = 32 * C::kRows / kWave, kEach = kScores / kParts;  // scores of a lane: 8 or 16
-    constexpr int kKeysPart = 32 / kParts, kSteps = C::kRows == 16 ? 1 : 2;  // steps of the second product
-    const int h = lane / C::kRows;
-    typename R::Acc part[kParts];
+    const int h = lane >> 5;
+    f32x16 z = zeros();
     {
-        constexpr int CH = C::kHead / 8;
+        const char* row = buf + C::kHeadAt + block * 32 * C::kHead * 2;
 #pragma unroll
-        for (int u = 0; u < kParts; ++u)
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) part[u][e] = 0.0f;
-        const char* row = buf + C::kHeadAt + block * 32 * CH * 16;
-#pragma unroll
-        for (int s = 0; s < R::kHeadSteps; ++s)  // (the permutation concerns the last bits of a chunk's number only)
-#pragma unroll
-            for (int u = 0; u < kParts; ++u) {
-                const bf16x8 k = *reinterpret_cast<const bf16x8*>(row + u * kKeysPart * CH * 16 + w.k_at[s % R::kOwnK] + (s / R::kOwnK) * 256);
-                part[u] = product(k, w.q[s], part[u]);
-            }
+        for (int s = 0; s < R::kHeadSteps; ++s) z = product(*reinterpret_cast<const bf16x8*>(row + w.k_at[s % R::kOwnK] + (s / R::kOwnK) * 256), w.q[s], z);
     }
     if constexpr (C::kTail > 0) {
-        constexpr int CH = C::kTail / 8;
-        const char* row = buf + C::kTailAt + block * 32 * CH * 16;
+        const char* row = buf + C::kTailAt + block * 32 * C::kTail * 2;
 #pragma unroll
-        for (int s = 0; s < R::kTailSteps; ++s)
-#pragma unroll
-            for (int u = 0; u < kParts; ++u) {
-                const bf16x8 k = *reinterpret_cast<const bf16x8*>(row + u * kKeysPart * CH * 16 + w.tail_at[s]);
-                part[u] = product(k, w.q[R::kHeadSteps + s], part[u]);
-            }
+        for (int s = 0; s < R::kTailSteps; ++s) z = product(*reinterpret_cast<const bf16x8*>(row + w.tail_at[s]), w.q[R::kHeadSteps + s], z);
     }
-    float z[kScores];  // key (e / kEach) * kKeysPart + 8 ((e % kEach) / 4) + 4 h + e % 4
-#pragma unroll
-    for (int e = 0; e < kScores; ++e) z[e] = part[e / kEach][e % kEach];
-    bool careful = false;  // the tile holds values that are not finite, in front of rows that do not see them
     if constexpr (MASKED) {
-        if constexpr (C::kAlias) {  // such a value is in the key, too, and has made its scores infinite or NaN
-            float sum = 0.0f;
 #pragma unroll
-            for (int e = 0; e < kScores; ++e) sum += z[e] - z[e];
-            careful = __any(sum != 0.0f);
-        }
-#pragma unroll
-        for (int e = 0; e < kScores; ++e)
-            z[e] = key0 + (e / kEach) * kKeysPart + 8 * (e % kEach >> 2) + 4 * h + (e & 3) <= w.seen ? z[e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) z[e] = key0 + 8 * (e >> 2) + 4 * h + (e & 3) <= w.seen ? z[e] : -INFINITY;
     }
     float top = fmaxf(z[0], z[1]);
 #pragma unroll
-    for (int e = 2; e < kScores; ++e) top = fmaxf(top, z[e]);
-    top = row_max<C::kRows>(top) * scale_log2;
-    // The reference follows the largest score only where that is more than a factor of 2^8 ahead of it: weights up to 2^8 lose
-    // nothing, and the accumulators are rescaled a few times per row instead of a few times per tile.
-    if (__any(top > w.m + 8.0f)) {
-        const float m = top > w.m + 8.0f ? top : w.m;
+    for (int e = 2; e < 16; ++e) top = fmaxf(top, z[e]);
+    top = fmaxf(top, other_half(top)) * scale_log2;
+    // The reference keeps a distance above the largest score and is moved only when a score overtakes it: weights stay below one,
+    // lose nothing (they are floating-point numbers) and the accumulators are rescaled a few times per row, not per tile.
+    if (__any(top > w.m)) {
+        const float m = top > w.m ? top + kAhead : w.m;
         const float alpha = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - m);
         w.m = m;
         w.l *= alpha;
@@ -673,56 +639,45 @@ __device__ __forceinline__ void take_keys(Rows<C>& w, const char* buf, int block
     const float m = w.m == -INFINITY ? 0.0f : w.m;
     float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < kScores; ++e) {
+    for (int e = 0; e < 16; ++e) {
         z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -m));
         sum += z[e];
     }
     w.l += sum;
-    bf16x8 hi[kSteps], lo[kSteps];
+    bf16x8 hi[2], lo[2];
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             hi[s][e] = (__bf16)z[8 * s + e];
             if constexpr (C::kPair) lo[s][e] = (__bf16)(z[8 * s + e] - (float)hi[s][e]);
         }
-    constexpr int CH = C::kDv / 8, kApart = C::kRows == 16 ? 16 : 8;  // key rows between an operand's two halves
-    const char* row = buf + C::kVAt + block * 32 * CH * 16;
+    const char* row = buf + C::kVAt + block * 32 * C::kDv * 2;
 #pragma unroll
     for (int b = 0; b < R::kBlocks; ++b) {
-        s16x8 v[kSteps];
+        s16x8 v[2];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const char* at = row + 16 * s * CH * 16 + w.v_at[b % R::kOwnV] + (b / R::kOwnV) * 256;
-            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + kApart * CH * 16));
-            v[s] = s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        for (int s = 0; s < 2; ++s) {
+            const char* at = row + 16 * s * C::kDv * 2 + w.v_at[b % R::kOwnV] + (b / R::kOwnV) * 256;
+            v[s] = transposed(at, at + 8 * C::kDv * 2);
         }
         if constexpr (MASKED) {
-            if constexpr (!C::kAlias) {
-                bool odd = false;
-#pragma unroll
-                for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) odd |= ((uint16_t)v[s][k] & 0x7f80u) == 0x7f80u;
-                careful = __any(odd);
-            }
-            if (careful) {
+            if (__any(any_odd(v[0]) | any_odd(v[1]))) {
                 // a value that is not finite must not meet the zero weight of a row that does not see it: each kind is
                 // multiplied as 1 and takes its place only in rows that give it weight
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    w.acc[b] = product(elements<kFinite>(v[s]), hi[s], w.acc[b]);
-                    if constexpr (C::kPair) w.acc[b] = product(elements<kFinite>(v[s]), lo[s], w.acc[b]);
+                for (int s = 0; s < 2; ++s) {
+                    w.acc[b] = product(elements(v[s], kFinite), hi[s], w.acc[b]);
+                    if constexpr (C::kPair) w.acc[b] = product(elements(v[s], kFinite), lo[s], w.acc[b]);
                 }
-                take_kind<kUp>(w.acc[b], v, hi, INFINITY);
-                take_kind<kDown>(w.acc[b], v, hi, -INFINITY);
-                take_kind<kNan>(w.acc[b], v, hi, __builtin_nanf(""));
+#pragma unroll 1
+                for (int kind = kUp; kind <= kNan; ++kind)
+                    put_odd(w.acc[b], product(elements(v[1], kind), hi[1], product(elements(v[0], kind), hi[0], zeros())), kind);
                 continue;
             }
         }
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
+        for (int s = 0; s < 2; ++s) {
             const bf16x8 x = __builtin_bit_cast(bf16x8, v[s]);
             if constexpr (C::kPair) w.acc[b] = product(x, lo[s], w.acc[b]);
             w.acc[b] = product(x, hi[s], w.acc[b]);
@@ -732,8 +687,8 @@ __device__ __forceinline__ void take_keys(Rows<C>& w, const char* buf, int block
 
 template <class C>
 __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* buf0, char* buf1) {
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), li = lane % C::kRows, h = lane / C::kRows;
-    const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + wave * C::kRows;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), li = lane & 31, h = lane >> 5;
+    const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + wave * 32;
     const bool active = first < n_packed;  // a wave without rows helps to load
     typedef Rows<C> R;
     R w;
@@ -742,19 +697,17 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
     w.seen = -1;
     w.place_operands(lane);
 #pragma unroll
-    for (int b = 0; b < R::kBlocks; ++b)
-#pragma unroll
-        for (int e = 0; e < (int)(sizeof(typename R::Acc) / 4); ++e) w.acc[b][e] = 0.0f;
+    for (int b = 0; b < R::kBlocks; ++b) w.acc[b] = zeros();
     int seen_first = 0, seen_last = 0;  // by the wave's first and last row
     if (active) {
         const int r = min(first + li, n_packed - 1);
         const Place at = place_of(a, p.q.row0, p.hk, r);
         const uint16_t* qp = (const uint16_t*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
 #pragma unroll
-        for (int s = 0; s < C::kDk / R::kStep; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(qp + R::kStep * s + 8 * h);
+        for (int s = 0; s < C::kDk / 16; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * h);
         w.seen = last_key(a, p.q, r);
         seen_first = last_key(a, p.q, first);
-        seen_last = last_key(a, p.q, min(first + C::kRows - 1, n_packed - 1));
+        seen_last = last_key(a, p.q, min(first + 31, n_packed - 1));
     }
     auto find = [&](int t) { return find_key<C::kOp>(a, p.q, min(p.q.k_begin + t * C::kKeys + lane, p.q.k_end - 1)); };
     __syncthreads();  // nobody reads the buffers any more
@@ -762,8 +715,8 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
         int t = p.t0;
         load_tile<C>(a, p, slot_of<C::kOp>(a, find(t)), buf0, wave, lane);
         Where next = find(min(t + 1, p.t1 - 1));
-        auto step = [&](char* now, char* then) {
-            __syncthreads();  // the tile has arrived, and nobody reads the other buffer any more
+        auto step = [&](char* now, char* then) __attribute__((always_inline)) {
+            arrive();  // (and nobody reads the other buffer any more)
             if (t + 1 < p.t1) {
                 load_tile<C>(a, p, slot_of<C::kOp>(a, next), then, wave, lane);
                 next = find(min(t + 2, p.t1 - 1));
@@ -780,13 +733,13 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
         };
         while (step(buf0, buf1) && step(buf1, buf0)) {}
     }
-    w.l = row_sum<C::kRows>(w.l);
+    w.l += other_half(w.l);
     if (active && first + li < n_packed)
-        hand_over<C>(a, p, wave * C::kRows + li, h == 0, w.m * kLn2, w.l, [&](auto put) {
+        hand_over<C>(a, p, wave * 32 + li, h == 0, w.m * kLn2, w.l, [&](auto put) {
 #pragma unroll
             for (int b = 0; b < R::kBlocks; ++b)
 #pragma unroll
-                for (int g = 0; g < C::kRows / 16 * C::kRows / 16; ++g) put(R::kBlock * b + 8 * g + 4 * h, f32x4{w.acc[b][4 * g], w.acc[b][4 * g + 1], w.acc[b][4 * g + 2], w.acc[b][4 * g + 3]});
+                for (int g = 0; g < 4; ++g) put(32 * b + 8 * g + 4 * h, f32x4{w.acc[b][4 * g], w.acc[b][4 * g + 1], w.acc[b][4 * g + 2], w.acc[b][4 * g + 3]});
         });
 }
 
