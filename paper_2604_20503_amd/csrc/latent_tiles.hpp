@@ -58,122 +58,181 @@ struct LatentRows {
     }
 };
 
+// Scores of the wave's 32 keys.
 template <class C>
-__device__ __forceinline__ void write_weights(const LatentRows<C>& w, char* p, const float (&z)[16]) {
+__device__ __forceinline__ f32x16 scores_of(const LatentRows<C>& w, const char* buf) {
+    typedef LatentRows<C> R;
+    f32x16 scores = zeros();
+    first_product<R::kHeadSteps + R::kTailSteps>(scores, [&](int s) __attribute__((always_inline)) {
+        return *reinterpret_cast<const bf16x8*>(s < R::kHeadSteps ? buf + C::kHeadAt + w.k_at[s % 8] + (s / 8) * 256 : buf + C::kTailAt + w.tail_at[s - R::kHeadSteps]);
+    }, w.q);
+    return scores;
+}
+
+__device__ __forceinline__ float largest(const f32x16& z) {
+    float top = fmaxf(z[0], z[1]);
+#pragma unroll
+    for (int e = 2; e < 16; ++e) top = fmaxf(top, z[e]);
+    return fmaxf(top, other_half(top));
+}
+
+// Weights of the scores, their sum added to the lane's.
+__device__ __forceinline__ float weights_of(f32x16& z, float m, float scale_log2) {
+    const float use = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -use));
+        sum += z[e];
+    }
+    return sum;
+}
+
+template <class C>
+__device__ __forceinline__ void write_weights(const LatentRows<C>& w, char* p, const f32x16& z) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
         *reinterpret_cast<u32x2*>(p + w.p_write[k]) = u32x2{bf16_bits(z[4 * k]) | (bf16_bits(z[4 * k + 1]) << 16), bf16_bits(z[4 * k + 2]) | (bf16_bits(z[4 * k + 3]) << 16)};
 }
+__device__ __forceinline__ void take_bf16_off(f32x16& z) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] -= (float)(__bf16)z[e];
+}
+
+// Operand of the second product: keys 16 s + 8 h .. of columns 32 b .. of the wave's half.  (Keys 4 .. 7 of eight: the permutation of
+// their rows differs in the bit that tells apart blocks b and b ^ 2.)
+template <class C>
+__device__ __forceinline__ s16x8 values_of(const LatentRows<C>& w, const char* buf, int s, int b) {
+    constexpr int kRow = C::kHead * 2;
+    const char* at = buf + C::kHeadAt + 16 * s * kRow + (b / 4) * 256;
+    return transposed(at + w.v_at[b % 4], at + 4 * kRow + w.v_at[(b % 4) ^ 2]);
+}
 
 // acc += V^T P^T for the wave's half of the columns.
 template <class C>
-__device__ __forceinline__ void second_product(LatentRows<C>& w, const char* buf, const char* p, bool careful) {
+__device__ __forceinline__ void second_product(LatentRows<C>& w, const char* buf, const char* p) {
     typedef LatentRows<C> R;
-    constexpr int kRow = C::kHead * 2;
     bf16x8 weights[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) weights[s] = *reinterpret_cast<const bf16x8*>(p + w.p_read[s]);
-    // (keys 4 .. 7 of eight: the permutation of their rows differs in the bit that tells apart blocks b and b ^ 2)
-    auto values = [&](int s, int b) __attribute__((always_inline)) {
-        const char* at = buf + C::kHeadAt + 16 * s * kRow + (b / 4) * 256;
-        return transposed(at + w.v_at[b % 4], at + 4 * kRow + w.v_at[(b % 4) ^ 2]);
-    };
-    if (!careful) {
+    constexpr int kBlocks = R::kBlocks, kSteps = 4 * kBlocks, kAheadSteps = 6;
+    s16x8 v[kAheadSteps];
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+    for (int k = 0; k < kAheadSteps; ++k) v[k] = values_of<C>(w, buf, k / kBlocks, k % kBlocks);
 #pragma unroll
-            for (int b = 0; b < R::kBlocks; ++b) w.acc[b] = product(__builtin_bit_cast(bf16x8, values(s, b)), weights[s], w.acc[b]);
-        return;
+    for (int k = 0; k < kSteps; ++k) {
+        __builtin_amdgcn_sched_barrier(0);
+        w.acc[k % kBlocks] = product(__builtin_bit_cast(bf16x8, v[k % kAheadSteps]), weights[k / kBlocks], w.acc[k % kBlocks]);
+        if (k + kAheadSteps < kSteps) v[k % kAheadSteps] = values_of<C>(w, buf, (k + kAheadSteps) / kBlocks, (k + kAheadSteps) % kBlocks);
     }
-    // values that are not finite among masked ones: see take_keys
+    __builtin_amdgcn_sched_barrier(0);
+}
+// The same where values are not finite among masked ones: such a value must not meet the zero weight of a row that does not see it.
+// Each kind is multiplied as 1 and takes its place only in rows that give it weight.
+template <class C>
+__device__ __forceinline__ void second_product_carefully(LatentRows<C>& w, const char* buf, const char* p) {
+    typedef LatentRows<C> R;
+    bf16x8 weights[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) weights[s] = *reinterpret_cast<const bf16x8*>(p + w.p_read[s]);
 #pragma unroll
     for (int b = 0; b < R::kBlocks; ++b) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) w.acc[b] = product(elements(values(s, b), kFinite), weights[s], w.acc[b]);
+        for (int s = 0; s < 4; ++s) w.acc[b] = product(elements(values_of<C>(w, buf, s, b), kFinite), weights[s], w.acc[b]);
 #pragma unroll 1
         for (int kind = kUp; kind <= kNan; ++kind) {
             f32x16 t = zeros();
 #pragma unroll
-            for (int s = 0; s < 4; ++s) t = product(elements(values(s, b), kind), weights[s], t);
+            for (int s = 0; s < 4; ++s) t = product(elements(values_of<C>(w, buf, s, b), kind), weights[s], t);
             put_odd(w.acc[b], t, kind);
         }
     }
 }
 
-// One tile of 64 keys from `key0` on.  All waves pass the same barriers; those of rows that see none of the keys (not `live`) do no more.
+// A tile of 64 keys that every row sees whole.  True: a score is ahead of its row's reference, and nothing has been added.  All waves
+// pass the same barriers; those without rows (not `live`) do no more.
 template <class C>
-__device__ __forceinline__ void take_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, int key0, bool live, bool masked, float scale_log2, int lane,
-                                          int wave) {
-    typedef LatentRows<C> R;
-    const int li = lane & 31, h = lane >> 5, part = wave & 1;
+__device__ __forceinline__ bool take_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, bool live, float scale_log2, int lane, int wave) {
     char* p = reinterpret_cast<char*>(sh.p);
-    float z[16], x[16], sum = 0.0f, top = -INFINITY;
-    auto weigh = [&]() __attribute__((always_inline)) {
-        const float m = w.m == -INFINITY ? 0.0f : w.m;
-        sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -m));
-            sum += x[e];
-        }
-        write_weights<C>(w, p, x);
-    };
-    int flags = 0;
+    f32x16 z;
+    float sum = 0.0f;
+    bool ahead = false;
     if (live) {
-        f32x16 scores = zeros();
-#pragma unroll
-        for (int s = 0; s < R::kHeadSteps; ++s)
-            scores = product(*reinterpret_cast<const bf16x8*>(buf + C::kHeadAt + w.k_at[s % 8] + (s / 8) * 256), w.q[s], scores);
-#pragma unroll
-        for (int s = 0; s < R::kTailSteps; ++s)
-            scores = product(*reinterpret_cast<const bf16x8*>(buf + C::kTailAt + w.tail_at[s]), w.q[R::kHeadSteps + s], scores);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) z[e] = scores[e];
-        if (masked) {
-            float odd = 0.0f;  // a value that is not finite is in its key, too, and has made the key's scores infinite or NaN
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                odd += z[e] - z[e];
-                z[e] = key0 + 32 * part + 8 * (e >> 2) + 4 * h + (e & 3) <= w.seen ? z[e] : -INFINITY;
-            }
-            if (__any(odd != 0.0f)) flags = 2;
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, z[e]);
-        top = fmaxf(top, other_half(top)) * scale_log2;
-        if (__any(top > w.m)) flags |= 1;
-        weigh();
+        z = scores_of<C>(w, buf);
+        ahead = __any(largest(z) * scale_log2 > w.m);
+        sum = weights_of(z, w.m, scale_log2);
+        write_weights<C>(w, p, z);
     }
-    if (lane == 0) sh.flags[wave] = flags;
+    if (lane == 0) sh.flags[wave] = ahead;
     __syncthreads();
-    const int rows01 = uniform(sh.flags[0] | sh.flags[1]), rows23 = uniform(sh.flags[2] | sh.flags[3]);
-    if ((rows01 | rows23) & 1) {  // some row's reference moves
-        if (h == 0) sh.top[wave][li] = top;
-        __syncthreads();
-        if (live) {
-            const float both = fmaxf(sh.top[wave & 2][li], sh.top[wave | 1][li]), old = w.m;
-            if (both > old) w.m = both + kAhead;
-            const float alpha = w.m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - w.m);
-            w.l *= alpha;
-#pragma unroll
-            for (int b = 0; b < R::kBlocks; ++b) w.acc[b] *= alpha;
-            weigh();
-        }
-        __syncthreads();
+    if (uniform(sh.flags[0] | sh.flags[1] | sh.flags[2] | sh.flags[3])) return true;
+    if (live) {
+        w.l += sum;
+        second_product<C>(w, buf, p);
     }
-    w.l += sum;
-    const bool careful = ((wave & 2 ? rows23 : rows01) & 2) != 0;
-    if (live) second_product<C>(w, buf, p, careful);
     if constexpr (C::kPair) {
         __syncthreads();
         if (live) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] -= (float)(__bf16)x[e];
-            write_weights<C>(w, p, x);
+            take_bf16_off(z);
+            write_weights<C>(w, p, z);
         }
         __syncthreads();
-        // (a weight's rest has no infinite values to meet that its leading part has not met: they are left out)
-        if (live) second_product<C>(w, buf, p, careful);
+        if (live) second_product<C>(w, buf, p);
+    }
+    return false;
+}
+
+// Any tile: some keys may be masked, references move if they have to.  (Rows that see none of its keys give zero weights.)
+template <class C>
+__device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, int key0, bool live, float scale_log2, int lane, int wave) {
+    const int li = lane & 31, h = lane >> 5, part = wave & 1;
+    char* p = reinterpret_cast<char*>(sh.p);
+    f32x16 z;
+    float top = -INFINITY;
+    int odd_scores = 0;
+    if (live) {
+        z = scores_of<C>(w, buf);
+        float odd = 0.0f;  // a value that is not finite is in its key, too, and has made the key's scores infinite or NaN
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            odd += z[e] - z[e];
+            z[e] = key0 + 32 * part + 8 * (e >> 2) + 4 * h + (e & 3) <= w.seen ? z[e] : -INFINITY;
+        }
+        odd_scores = __any(odd != 0.0f);
+        top = largest(z) * scale_log2;
+    }
+    if (h == 0) sh.top[wave][li] = top;
+    if (lane == 0) sh.flags[wave] = odd_scores;
+    __syncthreads();
+    const bool careful = uniform(sh.flags[wave & 2] | sh.flags[wave | 1]);
+    if (live) {
+        const float both = fmaxf(sh.top[wave & 2][li], sh.top[wave | 1][li]), old = w.m;
+        if (both > old) w.m = both + kAhead;
+        if (__any(both > old)) {
+            const float alpha = w.m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - w.m);
+            w.l *= alpha;
+#pragma unroll
+            for (int b = 0; b < LatentRows<C>::kBlocks; ++b) w.acc[b] *= alpha;
+        }
+        w.l += weights_of(z, w.m, scale_log2);
+        write_weights<C>(w, p, z);
+    }
+    __syncthreads();
+    if (live) {
+        if (careful) second_product_carefully<C>(w, buf, p);
+        else second_product<C>(w, buf, p);
+    }
+    if constexpr (C::kPair) {  // (where a weight's first part has met a value that is not finite, its rest has nothing to add)
+        __syncthreads();
+        if (live) {
+            take_bf16_off(z);
+            write_weights<C>(w, p, z);
+        }
+        __syncthreads();
+        if (live) {
+            if (careful) second_product_carefully<C>(w, buf, p);
+            else second_product<C>(w, buf, p);
+        }
     }
 }
 
@@ -182,7 +241,7 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
     typedef LatentRows<C> R;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), li = lane & 31, h = lane >> 5, part = wave & 1;
     const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + (wave >> 1) * 32;
-    const bool active = first < n_packed;  // a wave without rows helps to load
+    const bool live = first < n_packed;  // a wave without rows helps to load
     R w;
     w.m = -INFINITY;
     w.l = 0.0f;
@@ -196,36 +255,53 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
         load_tile<C>(a, p, slot_of<C::kOp>(a, find(t)), buf0, wave, lane);
         next = find(min(t + 1, p.t1 - 1));
     }
-    int seen_first = 0, seen_last = -1;  // by the wave's first and last row
-    if (active) {
+    if (live) {
         const int r = min(first + li, n_packed - 1);
         const Place at = place_of(a, p.q.row0, p.hk, r);
         const uint16_t* qp = (const uint16_t*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
 #pragma unroll
         for (int s = 0; s < C::kDk / 16; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * h);
         w.seen = last_key(a, p.q, r);
-        seen_first = last_key(a, p.q, first);
-        seen_last = last_key(a, p.q, min(first + 31, n_packed - 1));
     }
+    const int all_see = last_key(a, p.q, p.rt * C::kM);  // the tile's first row, and with it every row
 #pragma unroll
     for (int b = 0; b < R::kBlocks; ++b) w.acc[b] = zeros();
-    auto step = [&](char* now, char* then) __attribute__((always_inline)) {
+    auto begin = [&](char* then) __attribute__((always_inline)) {
         arrive();  // (and nobody reads the other buffer any more)
         if (t + 1 < p.t1) {
             load_tile<C>(a, p, slot_of<C::kOp>(a, next), then, wave, lane);
             next = find(min(t + 2, p.t1 - 1));
         }
-        const int key0 = p.q.k_begin + t * C::kKeys;
-        take_tile<C>(w, now, sh, key0, key0 <= seen_last, key0 + C::kKeys - 1 > seen_first, a.scale_log2, lane, wave);
-        return ++t < p.t1;
     };
-    if (t < p.t1)
-        while (step(buf0, buf1) && step(buf1, buf0)) {}
+    auto whole = [&] { return t < p.t1 && p.q.k_begin + t * C::kKeys + C::kKeys - 1 <= all_see; };
+    bool begun = false;
+    while (t < p.t1) {
+        // the first tile, tiles with masked keys, tiles where a reference moves
+        char* now = (t - p.t0) & 1 ? buf1 : buf0;
+        if (!begun) begin((t - p.t0) & 1 ? buf0 : buf1);
+        take_any_tile<C>(w, now, sh, p.q.k_begin + t * C::kKeys, live, a.scale_log2, lane, wave);
+        begun = false;
+        ++t;
+        // all the others: here the sums are the matrix instructions' alone, and stay in the accumulation registers
+        if ((t - p.t0) & 1) {
+            while (whole()) {
+                begin(buf0);
+                begun = take_tile<C>(w, buf1, sh, live, a.scale_log2, lane, wave);
+                if (begun) break;
+                ++t;
+                if (!whole()) break;
+                begin(buf1);
+                begun = take_tile<C>(w, buf0, sh, live, a.scale_log2, lane, wave);
+                if (begun) break;
+                ++t;
+            }
+        }
+    }
     w.l += other_half(w.l);
     __syncthreads();
     if (h == 0) sh.top[wave][li] = w.l;
     __syncthreads();
-    if (active && first + li < n_packed)
+    if (live && first + li < n_packed)
         hand_over<C>(a, p, (wave >> 1) * 32 + li, h == 0 && part == 0, w.m * kLn2, sh.top[wave & 2][li] + sh.top[wave | 1][li], [&](auto put) {
 #pragma unroll
             for (int b = 0; b < R::kBlocks; ++b)
