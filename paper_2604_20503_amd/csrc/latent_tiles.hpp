@@ -14,14 +14,71 @@
 namespace fsr {
 namespace row_tiles {
 
-template <int KH, int KT, class OUT>
+// PAGES16: pages hold a multiple of 16 tokens.
+template <int KH, int KT, class OUT, bool PAGES16>
 struct Latent {
     static constexpr int kOp = kLatent, kHead = KH, kTail = KT, kDk = KH + KT, kDv = KH;
-    static constexpr bool kPair = sizeof(OUT) == 4;
+    static constexpr bool kPair = sizeof(OUT) == 4, kPages16 = PAGES16;
     static constexpr int kM = 64, kKeys = 64, kBlockThreads = 256, kWaves = 4, kPerUnit = 1;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kBuf = kTailAt + kKeys * KT * 2;
     typedef uint16_t In;
     typedef OUT Out;
+};
+
+// A wave's loads of a tile: rows 16 wave .. 16 wave + 15.  Where they lie is fetched a tile ahead.
+//
+// A wave that has a SIMD to itself issues an instruction every 4 cycles, eight to a product; of the 18 loads, each with an address and a
+// place in LDS of its own, as little as possible is to be computed.  16 consecutive keys of a page are 16 consecutive rows: one page
+// number for all of the wave's rows, and addresses that are a scalar plus a lane's constant.
+template <class C>
+struct LatentLoads {
+    typedef RowLoads<C::kHead / 8, C::kWaves> Head;
+    typedef RowLoads<C::kTail / 8, C::kWaves> Tail;
+    static constexpr int kEach = Head::kEach + Tail::kEach;
+    int page, place;      // pages of 16: of the wave's first row (place: behind that row of the page); else of the lane's key
+    Buffer from;          // the wave's rows
+    uint32_t slot;
+    int head_xor, head_add, tail_at;
+
+    __device__ __forceinline__ void place_lane(const Args& a, int lane) {
+        constexpr int CH = C::kHead / 8, CT = C::kTail / 8;
+        head_xor = ((lane % CH) ^ permutation<CH>(lane / CH)) << 4;
+        head_add = (lane / CH) * (int)a.head_stride;
+        tail_at = (lane / CT) * (int)a.head_stride + C::kHead * 2 + (((lane % CT) ^ permutation<CT>(lane / CT)) << 4);
+    }
+    __device__ __forceinline__ void find(const Args& a, const Piece& p, int t, int wave, int lane) {
+        if constexpr (C::kPages16) {
+            const int key = min(t * C::kKeys + 16 * wave, (p.q.k_end - 1) & ~15);
+            const int pg = a.p_shift >= 0 ? key >> a.p_shift : (int)((uint32_t)key / (uint32_t)a.P);
+            page = a.bt[(size_t)p.q.table * a.max_pages + pg];
+            place = key - pg * a.P;
+        } else {
+            const Where x = find_key<kLatent>(a, p.q, min(t * C::kKeys + lane, p.q.k_end - 1));
+            page = x.page;
+            place = (int)x.place;
+        }
+    }
+    // The loads to come are those of the tile that has been found.
+    __device__ __forceinline__ void take(const Args& a) {
+        if constexpr (C::kPages16)
+            from = buffer_at(a.k_head + ((uint64_t)(uint32_t)clamp_to(uniform(page), 0, a.n_pages - 1) * a.page_slots + uniform(place)) * a.head_stride, 16 * a.head_stride);
+        else slot = slot_of<kLatent>(a, Where{page, (uint32_t)place});
+    }
+    __device__ __forceinline__ void issue(int i, const Args& a, char* buf, int wave, int lane) const {
+        if constexpr (C::kPages16) {
+            if (i < Head::kEach) {
+                const int k = i * Head::kRows;
+                to_lds(from, (head_xor ^ ((k & 7) << 5)) + head_add, k * (int)a.head_stride, buf + C::kHeadAt + (16 * wave + k) * C::kHead * 2);
+            } else {
+                const int k = (i - Head::kEach) * Tail::kRows;
+                to_lds(from, tail_at, k * (int)a.head_stride, buf + C::kTailAt + (16 * wave + k) * C::kTail * 2);
+            }
+        } else if (i < Head::kEach) {
+            Head::issue(i, a.k_head, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
+        } else {
+            Tail::issue(i - Head::kEach, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
+        }
+    }
 };
 
 struct LatentShared {     // what the waves of a workgroup tell each other
@@ -59,14 +116,12 @@ struct LatentRows {
 };
 
 // Scores of the wave's 32 keys.
-template <class C>
-__device__ __forceinline__ f32x16 scores_of(const LatentRows<C>& w, const char* buf) {
+template <class C, class Beside>
+__device__ __forceinline__ f32x16 scores_of(const LatentRows<C>& w, const char* buf, Beside beside) {
     typedef LatentRows<C> R;
-    f32x16 scores = zeros();
-    first_product<R::kHeadSteps + R::kTailSteps>(scores, [&](int s) __attribute__((always_inline)) {
+    return first_product<R::kHeadSteps + R::kTailSteps>([&](int s) __attribute__((always_inline)) {
         return *reinterpret_cast<const bf16x8*>(s < R::kHeadSteps ? buf + C::kHeadAt + w.k_at[s % 8] + (s / 8) * 256 : buf + C::kTailAt + w.tail_at[s - R::kHeadSteps]);
-    }, w.q);
-    return scores;
+    }, w.q, beside);
 }
 
 __device__ __forceinline__ float largest(const f32x16& z) {
@@ -79,20 +134,16 @@ __device__ __forceinline__ float largest(const f32x16& z) {
 // Weights of the scores, their sum added to the lane's.
 __device__ __forceinline__ float weights_of(f32x16& z, float m, float scale_log2) {
     const float use = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -use));
-        sum += z[e];
-    }
-    return sum;
+    for (int e = 0; e < 16; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -use));
+    return (((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]))) + (((z[8] + z[9]) + (z[10] + z[11])) + ((z[12] + z[13]) + (z[14] + z[15])));
 }
 
 template <class C>
 __device__ __forceinline__ void write_weights(const LatentRows<C>& w, char* p, const f32x16& z) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-        *reinterpret_cast<u32x2*>(p + w.p_write[k]) = u32x2{bf16_bits(z[4 * k]) | (bf16_bits(z[4 * k + 1]) << 16), bf16_bits(z[4 * k + 2]) | (bf16_bits(z[4 * k + 3]) << 16)};
+        *reinterpret_cast<u32x2*>(p + w.p_write[k]) = u32x2{bf16_pair(z[4 * k], z[4 * k + 1]), bf16_pair(z[4 * k + 2], z[4 * k + 3])};
 }
 __device__ __forceinline__ void take_bf16_off(f32x16& z) {
 #pragma unroll
@@ -115,17 +166,12 @@ __device__ __forceinline__ void second_product(LatentRows<C>& w, const char* buf
     bf16x8 weights[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) weights[s] = *reinterpret_cast<const bf16x8*>(p + w.p_read[s]);
-    constexpr int kBlocks = R::kBlocks, kSteps = 4 * kBlocks, kAheadSteps = 6;
-    s16x8 v[kAheadSteps];
-#pragma unroll
-    for (int k = 0; k < kAheadSteps; ++k) v[k] = values_of<C>(w, buf, k / kBlocks, k % kBlocks);
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-        __builtin_amdgcn_sched_barrier(0);
-        w.acc[k % kBlocks] = product(__builtin_bit_cast(bf16x8, v[k % kAheadSteps]), weights[k / kBlocks], w.acc[k % kBlocks]);
-        if (k + kAheadSteps < kSteps) v[k % kAheadSteps] = values_of<C>(w, buf, (k + kAheadSteps) / kBlocks, (k + kAheadSteps) % kBlocks);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    constexpr int kBlocks = R::kBlocks;
+    in_turn<4 * kBlocks, 6, s16x8>([&](int k) __attribute__((always_inline)) { return values_of<C>(w, buf, k / kBlocks, k % kBlocks); },
+                                   [&](int k, s16x8 v) __attribute__((always_inline)) {
+                                       w.acc[k % kBlocks] = product(__builtin_bit_cast(bf16x8, v), weights[k / kBlocks], w.acc[k % kBlocks]);
+                                   },
+                                   [](int) {});
 }
 // The same where values are not finite among masked ones: such a value must not meet the zero weight of a row that does not see it.
 // Each kind is multiplied as 1 and takes its place only in rows that give it weight.
@@ -151,32 +197,40 @@ __device__ __forceinline__ void second_product_carefully(LatentRows<C>& w, const
 
 // A tile of 64 keys that every row sees whole.  True: a score is ahead of its row's reference, and nothing has been added.  All waves
 // pass the same barriers; those without rows (not `live`) do no more.
-template <class C>
-__device__ __forceinline__ bool take_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, bool live, float scale_log2, int lane, int wave) {
+// beside(i) issues the wave's load i of the next tile: between the products, whose issue leaves time for it.
+template <class C, class Beside>
+__device__ __forceinline__ bool take_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, bool live, float scale_log2, int lane, int wave, Beside beside) {
+    constexpr int kLoads = LatentLoads<C>::kEach, kSteps = LatentRows<C>::kHeadSteps + LatentRows<C>::kTailSteps;
+    static_assert(2 * kLoads <= kSteps, "a load beside every other product");
     char* p = reinterpret_cast<char*>(sh.p);
     f32x16 z;
     float sum = 0.0f;
     bool ahead = false;
     if (live) {
-        z = scores_of<C>(w, buf);
+        z = scores_of<C>(w, buf, [&](int s) __attribute__((always_inline)) {
+            if (s % 2 == 0 && s / 2 < kLoads) beside(s / 2);
+        });
         ahead = __any(largest(z) * scale_log2 > w.m);
         sum = weights_of(z, w.m, scale_log2);
         write_weights<C>(w, p, z);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) beside(i);
     }
     if (lane == 0) sh.flags[wave] = ahead;
-    __syncthreads();
+    lds_barrier();
     if (uniform(sh.flags[0] | sh.flags[1] | sh.flags[2] | sh.flags[3])) return true;
     if (live) {
         w.l += sum;
         second_product<C>(w, buf, p);
     }
     if constexpr (C::kPair) {
-        __syncthreads();
+        lds_barrier();
         if (live) {
             take_bf16_off(z);
             write_weights<C>(w, p, z);
         }
-        __syncthreads();
+        lds_barrier();
         if (live) second_product<C>(w, buf, p);
     }
     return false;
@@ -191,7 +245,7 @@ __device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf,
     float top = -INFINITY;
     int odd_scores = 0;
     if (live) {
-        z = scores_of<C>(w, buf);
+        z = scores_of<C>(w, buf, [](int) {});
         float odd = 0.0f;  // a value that is not finite is in its key, too, and has made the key's scores infinite or NaN
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -203,7 +257,7 @@ __device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf,
     }
     if (h == 0) sh.top[wave][li] = top;
     if (lane == 0) sh.flags[wave] = odd_scores;
-    __syncthreads();
+    lds_barrier();
     const bool careful = uniform(sh.flags[wave & 2] | sh.flags[wave | 1]);
     if (live) {
         const float both = fmaxf(sh.top[wave & 2][li], sh.top[wave | 1][li]), old = w.m;
@@ -217,18 +271,18 @@ __device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf,
         w.l += weights_of(z, w.m, scale_log2);
         write_weights<C>(w, p, z);
     }
-    __syncthreads();
+    lds_barrier();
     if (live) {
         if (careful) second_product_carefully<C>(w, buf, p);
         else second_product<C>(w, buf, p);
     }
     if constexpr (C::kPair) {  // (where a weight's first part has met a value that is not finite, its rest has nothing to add)
-        __syncthreads();
+        lds_barrier();
         if (live) {
             take_bf16_off(z);
             write_weights<C>(w, p, z);
         }
-        __syncthreads();
+        lds_barrier();
         if (live) {
             if (careful) second_product_carefully<C>(w, buf, p);
             else second_product<C>(w, buf, p);
@@ -247,13 +301,19 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
     w.l = 0.0f;
     w.seen = -1;
     w.place_operands(lane, wave >> 1, part);
-    auto find = [&](int t) { return find_key<C::kOp>(a, p.q, min(p.q.k_begin + t * C::kKeys + lane, p.q.k_end - 1)); };
+    LatentLoads<C> loads;
+    loads.place_lane(a, lane);
     __syncthreads();  // nobody reads the buffers any more
     int t = p.t0;
-    Where next{};
+    auto load_all = [&](char* to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LatentLoads<C>::kEach; ++i) loads.issue(i, a, to, wave, lane);
+    };
     if (t < p.t1) {
-        load_tile<C>(a, p, slot_of<C::kOp>(a, find(t)), buf0, wave, lane);
-        next = find(min(t + 1, p.t1 - 1));
+        loads.find(a, p, t, wave, lane);
+        loads.take(a);
+        loads.find(a, p, min(t + 1, p.t1 - 1), wave, lane);
+        load_all(buf0);
     }
     if (live) {
         const int r = min(first + li, n_packed - 1);
@@ -266,39 +326,39 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
     const int all_see = last_key(a, p.q, p.rt * C::kM);  // the tile's first row, and with it every row
 #pragma unroll
     for (int b = 0; b < R::kBlocks; ++b) w.acc[b] = zeros();
-    auto begin = [&](char* then) __attribute__((always_inline)) {
-        arrive();  // (and nobody reads the other buffer any more)
-        if (t + 1 < p.t1) {
-            load_tile<C>(a, p, slot_of<C::kOp>(a, next), then, wave, lane);
-            next = find(min(t + 2, p.t1 - 1));
-        }
-    };
     auto whole = [&] { return t < p.t1 && p.q.k_begin + t * C::kKeys + C::kKeys - 1 <= all_see; };
-    bool begun = false;
+    // A tile of the fast loop; false: a reference moves, and the tile is still to be added (the next one's loads are under way).
+    auto step = [&](const char* now, char* then) __attribute__((always_inline)) {
+        arrive();  // (and nobody reads the other buffer any more)
+        loads.take(a);
+        loads.find(a, p, min(t + 2, p.t1 - 1), wave, lane);  // (behind the last tile this one is loaded again: a load too many costs less than asking)
+        const bool ahead = take_tile<C>(w, now, sh, live, a.scale_log2, lane, wave, [&](int i) __attribute__((always_inline)) { loads.issue(i, a, then, wave, lane); });
+        t += !ahead;
+        return !ahead;
+    };
+    bool loaded = false;  // the next tile's loads have been issued
     while (t < p.t1) {
         // the first tile, tiles with masked keys, tiles where a reference moves
-        char* now = (t - p.t0) & 1 ? buf1 : buf0;
-        if (!begun) begin((t - p.t0) & 1 ? buf0 : buf1);
-        take_any_tile<C>(w, now, sh, p.q.k_begin + t * C::kKeys, live, a.scale_log2, lane, wave);
-        begun = false;
+        const bool odd = (t - p.t0) & 1;
+        if (!loaded) {
+            arrive();
+            loads.take(a);
+            loads.find(a, p, min(t + 2, p.t1 - 1), wave, lane);
+            load_all(odd ? buf0 : buf1);
+        }
+        loaded = false;
+        take_any_tile<C>(w, odd ? buf1 : buf0, sh, p.q.k_begin + t * C::kKeys, live, a.scale_log2, lane, wave);
         ++t;
         // all the others: here the sums are the matrix instructions' alone, and stay in the accumulation registers
-        if ((t - p.t0) & 1) {
+        if (!odd)
             while (whole()) {
-                begin(buf0);
-                begun = take_tile<C>(w, buf1, sh, live, a.scale_log2, lane, wave);
-                if (begun) break;
-                ++t;
+                if (!step(buf1, buf0)) { loaded = true; break; }
                 if (!whole()) break;
-                begin(buf1);
-                begun = take_tile<C>(w, buf0, sh, live, a.scale_log2, lane, wave);
-                if (begun) break;
-                ++t;
+                if (!step(buf0, buf1)) { loaded = true; break; }
             }
-        }
     }
     w.l += other_half(w.l);
-    __syncthreads();
+    arrive();  // (the load too many has its place until it has come)
     if (h == 0) sh.top[wave][li] = w.l;
     __syncthreads();
     if (live && first + li < n_packed)
@@ -320,9 +380,9 @@ __global__ __launch_bounds__(C::kBlockThreads, 1) void latent_kernel(Args a) {
     const Line line = find_share<C>(a, share, reinterpret_cast<long long*>(buf0));
     walk<C>(a, share, line, [&](const Piece& p) { run_latent<C>(a, p, buf0, buf1, sh); });
 }
-template <int KH, int KT, class OUT>
-struct Kernel<Latent<KH, KT, OUT>> {
-    static constexpr auto run = latent_kernel<Latent<KH, KT, OUT>>;
+template <int KH, int KT, class OUT, bool PAGES16>
+struct Kernel<Latent<KH, KT, OUT, PAGES16>> {
+    static constexpr auto run = latent_kernel<Latent<KH, KT, OUT, PAGES16>>;
 };
 
 }  // namespace row_tiles

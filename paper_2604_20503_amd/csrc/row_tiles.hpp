@@ -289,11 +289,14 @@ __device__ __forceinline__ uint32_t slot_of(const Args& a, Where w) {  // (insid
 }
 
 __device__ __forceinline__ uint32_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((__attribute__((ext_vector_type(2))) float){x, y}, __attribute__((ext_vector_type(2))) __bf16));
+}
 
 // D_v columns of a row: out of the accumulators of one lane, four neighbouring columns at a time.
 __device__ __forceinline__ void store4(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 __device__ __forceinline__ void store4(uint16_t* p, f32x4 x) {
-    *reinterpret_cast<u32x2*>(p) = u32x2{bf16_bits(x[0]) | (bf16_bits(x[1]) << 16), bf16_bits(x[2]) | (bf16_bits(x[3]) << 16)};
+    *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
 }
 
 // Logarithm of exp(m) * l, -inf without any weight.
@@ -504,31 +507,54 @@ __device__ __forceinline__ void to_lds(const char* from, char* to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// A wave's part of 64 rows of CH chunks: rows (wave * kEach + i) * kRows ..; lane k of the wave holds the slot of row k.
+// The same by a buffer descriptor, a lane's offset and a common one.  (Not only fewer instructions: behind a load in the other form the
+// compiler takes every wait for an LDS read to be one for all of them.)
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_at(const char* base, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000); }
+__device__ __forceinline__ void to_lds(Buffer from, int lane_at, int at, char* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_at, at, 0, 0);
+}
+
+// A wave's part of 64 rows of CH chunks: load `i` of kEach takes rows (wave * kEach + i) * kRows ..; lane k of the wave holds the slot of row k.
 template <int CH, int WAVES>
-__device__ __forceinline__ void load_rows(const char* base, uint32_t stride, uint32_t slot, char* to, int wave, int lane) {
-    constexpr int kRows = 64 / CH, kLoads = 64 / kRows, kEach = (kLoads + WAVES - 1) / WAVES;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        if (kLoads % WAVES != 0 && wave * kEach + i >= kLoads) break;
+struct RowLoads {
+    static constexpr int kRows = 64 / CH, kLoads = 64 / kRows, kEach = (kLoads + WAVES - 1) / WAVES;
+    static __device__ __forceinline__ void issue(int i, const char* base, uint32_t stride, uint32_t slot, char* to, int wave, int lane) {
+        if (kLoads % WAVES != 0 && wave * kEach + i >= kLoads) return;
         const int row0 = (wave * kEach + i) * kRows, row = row0 + lane / CH;
         const uint32_t at = kRows == 1 ? (uint32_t)__builtin_amdgcn_readlane((int)slot, row0) : (uint32_t)__shfl((int)slot, row, kWave);
         to_lds(base + (uint64_t)at * stride + (((lane % CH) ^ permutation<CH>(row)) << 4), to + row0 * CH * 16);
     }
-}
+};
 
 // The tile's loads, which this wave has issued, have arrived, and so have everyone's behind the barrier; nobody reads what has been
 // read in front of it any more.
 __device__ __forceinline__ void arrive() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __syncthreads();
 }
 
+// A barrier for what waves hand each other through LDS: loads that are on their way there stay so.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// A wave's loads of a tile, one after the other.
+template <class C>
+struct TileLoads {
+    typedef RowLoads<C::kHead / 8, C::kWaves> Head;
+    typedef RowLoads<C::kTail / 8 ? C::kTail / 8 : 1, C::kWaves> Tail;
+    typedef RowLoads<C::kDv / 8, C::kWaves> Value;
+    static constexpr int kTails = C::kTail > 0 ? Tail::kEach : 0, kValues = C::kOp != kLatent ? Value::kEach : 0;
+    static constexpr int kEach = Head::kEach + kTails + kValues;
+    static __device__ __forceinline__ void issue(int i, const Args& a, int hk, uint32_t slot, char* buf, int wave, int lane) {
+        if (i < Head::kEach) Head::issue(i, a.k_head + (size_t)hk * a.head_hk, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
+        else if (i < Head::kEach + kTails) Tail::issue(i - Head::kEach, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
+        else if constexpr (kValues > 0) Value::issue(i - Head::kEach - kTails, a.v + (size_t)hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
+    }
+};
 template <class C>
 __device__ __forceinline__ void load_tile(const Args& a, const Piece& p, uint32_t slot, char* buf, int wave, int lane) {
-    load_rows<C::kHead / 8, C::kWaves>(a.k_head + (size_t)p.hk * a.head_hk, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
-    if constexpr (C::kTail > 0) load_rows<C::kTail / 8, C::kWaves>(a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
-    if constexpr (C::kOp != kLatent) load_rows<C::kDv / 8, C::kWaves>(a.v + (size_t)p.hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
+#pragma unroll
+    for (int i = 0; i < TileLoads<C>::kEach; ++i) TileLoads<C>::issue(i, a, p.hk, slot, buf, wave, lane);
 }
 
 __device__ __forceinline__ float other_half(float x) {  // of the lane 32 further
@@ -576,21 +602,29 @@ __device__ __forceinline__ void reads_ahead() {
     }
     __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
-// sum += key(s) q[s] over N steps, the operands fetched eight steps ahead.  (Left to itself the compiler saves registers and waits for
-// every operand: 36 steps took 6000 cycles instead of 1200.)
-template <int N, class Key>
-__device__ __forceinline__ void first_product(f32x16& sum, Key key, const bf16x8* q) {
-    constexpr int kAheadSteps = N < 8 ? N : 8;
-    bf16x8 k[kAheadSteps];
+// N products in order: product(k, operand k), operands by read(k) AHEAD products before they are needed, and beside(k) in between.  (Left to
+// itself the compiler saves registers and waits for every operand: 36 steps took 6000 cycles instead of 1300.)
+template <int N, int AHEAD, class Operand, class Read, class Product, class Beside>
+__device__ __forceinline__ void in_turn(Read read, Product product, Beside beside) {
+    constexpr int A = N < AHEAD ? N : AHEAD;
+    Operand x[A];
 #pragma unroll
-    for (int s = 0; s < kAheadSteps; ++s) k[s] = key(s);
+    for (int k = 0; k < A; ++k) x[k] = read(k);
 #pragma unroll
-    for (int s = 0; s < N; ++s) {
+    for (int k = 0; k < N; ++k) {
         __builtin_amdgcn_sched_barrier(0);
-        sum = product(k[s % kAheadSteps], q[s], sum);
-        if (s + kAheadSteps < N) k[s % kAheadSteps] = key(s + kAheadSteps);
+        product(k, x[k % A]);
+        if (k + A < N) x[k % A] = read(k + A);
+        beside(k);
     }
     __builtin_amdgcn_sched_barrier(0);
+}
+// Sum of key(s) q[s] over N steps.
+template <int N, class Key, class Beside>
+__device__ __forceinline__ f32x16 first_product(Key key, const bf16x8* q, Beside beside) {
+    f32x16 sum = zeros();
+    in_turn<N, 8, bf16x8>(key, [&](int s, bf16x8 k) __attribute__((always_inline)) { sum = product(k, q[s], sum); }, beside);
+    return sum;
 }
 // Eight keys of 32 columns, one column a lane: four keys at each of two places.
 __device__ __forceinline__ s16x8 transposed(const char* four, const char* other_four) {
