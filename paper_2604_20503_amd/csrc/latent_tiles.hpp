@@ -64,26 +64,27 @@ struct LatentLoads {
             from = buffer_at(a.k_head + ((uint64_t)(uint32_t)clamp_to(uniform(page), 0, a.n_pages - 1) * a.page_slots + uniform(place)) * a.head_stride, 16 * a.head_stride);
         else slot = slot_of<kLatent>(a, Where{page, (uint32_t)place});
     }
-    __device__ __forceinline__ void issue(int i, const Args& a, char* buf, int wave, int lane) const {
-        if constexpr (C::kPages16) {
-            if (i < Head::kEach) {
-                const int k = i * Head::kRows;
-                to_lds(from, (head_xor ^ ((k & 7) << 5)) + head_add, k * (int)a.head_stride, buf + C::kHeadAt + (16 * wave + k) * C::kHead * 2);
-            } else {
-                const int k = (i - Head::kEach) * Tail::kRows;
-                to_lds(from, tail_at, k * (int)a.head_stride, buf + C::kTailAt + (16 * wave + k) * C::kTail * 2);
-            }
-        } else if (i < Head::kEach) {
-            Head::issue(i, a.k_head, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
+    // Load i of 16 rows that follow each other in memory.
+    __device__ __forceinline__ void issue_rows(int i, Buffer rows, int stride, char* buf, int wave) const {
+        if (i < Head::kEach) {
+            const int k = i * Head::kRows;
+            to_lds(rows, (head_xor ^ ((k & 7) << 5)) + head_add, k * stride, buf + C::kHeadAt + (16 * wave + k) * C::kHead * 2);
         } else {
-            Tail::issue(i - Head::kEach, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
+            const int k = (i - Head::kEach) * Tail::kRows;
+            to_lds(rows, tail_at, k * stride, buf + C::kTailAt + (16 * wave + k) * C::kTail * 2);
         }
+    }
+    __device__ __forceinline__ void issue(int i, const Args& a, char* buf, int wave, int lane) const {
+        if constexpr (C::kPages16) issue_rows(i, from, (int)a.head_stride, buf, wave);
+        else if (i < Head::kEach) Head::issue(i, a.k_head, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
+        else Tail::issue(i - Head::kEach, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
     }
 };
 
 struct LatentShared {     // what the waves of a workgroup tell each other
     uint16_t p[64][64];   // weights [row][key], 16-byte chunks of a row permuted
     float top[4][32];     // largest score of a row among a wave's keys; at the end its sum of weights
+    float m[2][32];       // at the end: the scores that the rows' weights refer to
     int flags[4];         // by wave: 1: a score is ahead of its reference, 2: scores that are not finite among masked ones
 };
 
@@ -303,27 +304,32 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
     w.place_operands(lane, wave >> 1, part);
     LatentLoads<C> loads;
     loads.place_lane(a, lane);
-    __syncthreads();  // nobody reads the buffers any more
+    if (live) w.seen = last_key(a, p.q, min(first + li, n_packed - 1));
+    const int all_see = last_key(a, p.q, p.rt * C::kM);  // the tile's first row, and with it every row
     int t = p.t0;
     auto load_all = [&](char* to) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LatentLoads<C>::kEach; ++i) loads.issue(i, a, to, wave, lane);
     };
+    __syncthreads();  // nobody reads the buffers any more
     if (t < p.t1) {
         loads.find(a, p, t, wave, lane);
+        // the queries, 64 rows that follow each other and have a key's shape, come by way of the other buffer
+        const size_t row0 = (size_t)p.q.row0 * a.H + p.rt * C::kM + 16 * wave, rows = (size_t)a.N_cap * a.H;
+        const int stride = (int)a.head_stride;
+        const Buffer queries = buffer_at((const char*)a.q + min(row0, rows - 1) * stride, row0 < rows ? (uint32_t)min(rows - row0, (size_t)16) * stride : 0u);
+#pragma unroll
+        for (int i = 0; i < LatentLoads<C>::kEach; ++i) loads.issue_rows(i, queries, stride, buf1, wave);
         loads.take(a);
         loads.find(a, p, min(t + 1, p.t1 - 1), wave, lane);
         load_all(buf0);
-    }
-    if (live) {
-        const int r = min(first + li, n_packed - 1);
-        const Place at = place_of(a, p.q.row0, p.hk, r);
-        const uint16_t* qp = (const uint16_t*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
+        arrive();
+        const int other = ((wave >> 1) - part) * 32;  // from the wave's keys to its rows
 #pragma unroll
-        for (int s = 0; s < C::kDk / 16; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * h);
-        w.seen = last_key(a, p.q, r);
+        for (int s = 0; s < R::kHeadSteps; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(buf1 + C::kHeadAt + other * C::kHead * 2 + w.k_at[s % 8] + (s / 8) * 256);
+#pragma unroll
+        for (int s = 0; s < R::kTailSteps; ++s) w.q[R::kHeadSteps + s] = *reinterpret_cast<const bf16x8*>(buf1 + C::kTailAt + other * C::kTail * 2 + w.tail_at[s]);
     }
-    const int all_see = last_key(a, p.q, p.rt * C::kM);  // the tile's first row, and with it every row
 #pragma unroll
     for (int b = 0; b < R::kBlocks; ++b) w.acc[b] = zeros();
     auto whole = [&] { return t < p.t1 && p.q.k_begin + t * C::kKeys + C::kKeys - 1 <= all_see; };
@@ -357,18 +363,43 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
                 if (!step(buf0, buf1)) { loaded = true; break; }
             }
     }
+    // The sums leave by way of LDS, row by row: from the accumulators a store would touch 32 rows.  (16-byte chunks permuted by row, so
+    // that eight rows' writes of one column reach all banks.)
     w.l += other_half(w.l);
     arrive();  // (the load too many has its place until it has come)
     if (h == 0) sh.top[wave][li] = w.l;
+    if (h == 0 && part == 0) sh.m[wave >> 1][li] = w.m * kLn2;
+    constexpr int kRowBytes = C::kDv * 4;
+    static_assert(32 * kRowBytes <= C::kBuf, "32 rows' sums fit into a buffer");
+    auto place = [&](int row, int chunk) { return (row < 32 ? buf0 : buf1) + (row & 31) * kRowBytes + ((chunk ^ (row & 7)) << 4); };
+#pragma unroll
+    for (int b = 0; b < R::kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f32x4*>(place((wave >> 1) * 32 + li, part * (C::kDv / 8) + 8 * b + 2 * g + h)) =
+                f32x4{w.acc[b][4 * g], w.acc[b][4 * g + 1], w.acc[b][4 * g + 2], w.acc[b][4 * g + 3]};
     __syncthreads();
-    if (live && first + li < n_packed)
-        hand_over<C>(a, p, (wave >> 1) * 32 + li, h == 0 && part == 0, w.m * kLn2, sh.top[wave & 2][li] + sh.top[wave | 1][li], [&](auto put) {
+    const int rows = min(n_packed - p.rt * C::kM, C::kM);
+    for (int r = wave; r < rows; r += C::kWaves) {
+        const float l = sh.top[r >> 5 << 1][r & 31] + sh.top[(r >> 5 << 1) | 1][r & 31], m = sh.m[r >> 5][r & 31];
+        const Target<C> to = target_of<C>(a, p, r, lane == 0);
+        const float inv = to.out ? inverse(l) : 1.0f;
 #pragma unroll
-            for (int b = 0; b < R::kBlocks; ++b)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    put(part * (C::kDv / 2) + 32 * b + 8 * g + 4 * h, f32x4{w.acc[b][4 * g], w.acc[b][4 * g + 1], w.acc[b][4 * g + 2], w.acc[b][4 * g + 3]});
-        });
+        for (int k = 0; k < C::kDv / 4 / 64; ++k) {
+            const int chunk = k * 64 + lane;
+            const f32x4 x = *reinterpret_cast<const f32x4*>(place(r, chunk));
+            if (to.out) store4(to.out + 4 * chunk, x * inv);
+            else store4(to.sums + 4 * chunk, x);
+        }
+        if (lane == 0) {
+            if (!to.out) {
+                to.ml[0] = m;
+                to.ml[1] = l;
+            } else if (to.lse) {
+                *to.lse = log_sum(m, l);
+            }
+        }
+    }
 }
 
 template <class C>

@@ -303,44 +303,55 @@ __device__ __forceinline__ void store4(uint16_t* p, f32x4 x) {
 __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2; }
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-// Result of a row's share of the keys: sums o[4] at columns d .. d + 3 (called for all of the lane's columns), the score m that the
-// weights refer to (-inf: no key), their sum l.
-template <class C, class ForEach4>
-__device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_tile, bool first_lane, float m, float l, ForEach4 each) {
+// Where the result of a row's share of the keys goes.
+template <class C>
+struct Target {
+    typename C::Out* out;  // the result (kDv values and, if wanted, lse), or
+    float* lse;
+    float* sums;           // the sums of weighted values, not divided, with the score that the weights refer to and their sum
+    float* ml;
+};
+// For row r_tile of the piece; `first_lane` says (in a batch behind prefixes) where the row's parts are to be found.
+template <class C>
+__device__ __forceinline__ Target<C> target_of(const Args& a, const Piece& p, int r_tile, bool first_lane) {
     const Place at = place_of(a, p.q.row0, p.hk, p.rt * C::kM + r_tile);
     const size_t row = (size_t)at.row * a.H + at.head;
     const bool prefix = C::kOp == kShared && p.q.base == 1 << 30;
     const bool joined = C::kOp == kShared && (prefix || p.q.k_begin > 0);  // two items make the row
     if (p.whole && !joined) {
-        using Out = typename C::Out;
-        Out* out = (Out*)a.out + row * C::kDv;
-        const float inv = inverse(l);
-        each([&](int d, f32x4 x) { store4(out + d, x * inv); });
-        if (first_lane && a.lse) a.lse[row] = log_sum(m, l);
         if (C::kOp == kShared && first_lane) {
             const size_t n = (size_t)a.N_cap * a.H;
             a.refs[2 * (n + row)] = -1;  // nothing is left to be joined
         }
-        return;
+        return Target<C>{(typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, nullptr, nullptr};
     }
-    float *o, *ml;
+    if (C::kOp == kShared && first_lane && p.t0 == 0) {  // whoever begins the item says where its pieces are
+        const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
+        a.refs[2 * k] = p.whole ? 0 : p.pieces;
+        a.refs[2 * k + 1] = p.share0;
+    }
     if (p.whole) {
         const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
-        o = a.row_o + k * C::kDv;
-        ml = a.row_ml + k * 2;
-    } else {
-        const size_t k = (size_t)p.slot * a.m_cap + r_tile;
-        o = a.part_o + k * C::kDv;
-        ml = a.part_ml + k * 2;
+        return Target<C>{nullptr, nullptr, a.row_o + k * C::kDv, a.row_ml + k * 2};
     }
-    each([&](int d, f32x4 x) { store4(o + d, x); });
-    if (first_lane) {
-        ml[0] = m;
-        ml[1] = l;
-        if (C::kOp == kShared && p.t0 == 0) {  // whoever begins the item says where its pieces are
-            const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
-            a.refs[2 * k] = p.whole ? 0 : p.pieces;
-            a.refs[2 * k + 1] = p.share0;
+    const size_t k = (size_t)p.slot * a.m_cap + r_tile;
+    return Target<C>{nullptr, nullptr, a.part_o + k * C::kDv, a.part_ml + k * 2};
+}
+
+// Result of a row's share of the keys: sums o[4] at columns d .. d + 3 (called for all of the lane's columns), the score m that the
+// weights refer to (-inf: no key), their sum l.
+template <class C, class ForEach4>
+__device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_tile, bool first_lane, float m, float l, ForEach4 each) {
+    const Target<C> to = target_of<C>(a, p, r_tile, first_lane);
+    if (to.out) {
+        const float inv = inverse(l);
+        each([&](int d, f32x4 x) { store4(to.out + d, x * inv); });
+        if (first_lane && to.lse) *to.lse = log_sum(m, l);
+    } else {
+        each([&](int d, f32x4 x) { store4(to.sums + d, x); });
+        if (first_lane) {
+            to.ml[0] = m;
+            to.ml[1] = l;
         }
     }
 }
