@@ -116,6 +116,23 @@ struct LatentRows {
     }
 };
 
+// The sums' place is the accumulation registers.  Where something else than a product touches them, once in many tiles, the compiler would
+// otherwise take them to the other registers for all of the loop around it, 256 moves a tile.  change(x) is applied to every element; the
+// wait states are those behind a product of 8 passes, and in front of the next.
+template <class Change>
+__device__ __forceinline__ void change_sums(f32x16& acc, Change change) {
+    asm volatile("s_nop 15\n\ts_nop 7" : "+a"(acc));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        float x, y = acc[e];
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(y));
+        x = change(x, e);
+        asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(y) : "v"(x));
+        acc[e] = y;
+    }
+    asm volatile("s_nop 7" : "+a"(acc));
+}
+
 // Scores of the wave's 32 keys.
 template <class C, class Beside>
 __device__ __forceinline__ f32x16 scores_of(const LatentRows<C>& w, const char* buf, Beside beside) {
@@ -191,7 +208,8 @@ __device__ __forceinline__ void second_product_carefully(LatentRows<C>& w, const
             f32x16 t = zeros();
 #pragma unroll
             for (int s = 0; s < 4; ++s) t = product(elements(values_of<C>(w, buf, s, b), kind), weights[s], t);
-            put_odd(w.acc[b], t, kind);
+            const float value = odd_value(kind);
+            change_sums(w.acc[b], [&](float x, int e) { return t[e] != 0.0f ? x + value : x; });
         }
     }
 }
@@ -263,11 +281,11 @@ __device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf,
     if (live) {
         const float both = fmaxf(sh.top[wave & 2][li], sh.top[wave | 1][li]), old = w.m;
         if (both > old) w.m = both + kAhead;
-        if (__any(both > old)) {
-            const float alpha = w.m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - w.m);
+        if (__any(both > old && old > -INFINITY)) {
+            const float alpha = w.m == -INFINITY || old == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - w.m);
             w.l *= alpha;
 #pragma unroll
-            for (int b = 0; b < LatentRows<C>::kBlocks; ++b) w.acc[b] *= alpha;
+            for (int b = 0; b < LatentRows<C>::kBlocks; ++b) change_sums(w.acc[b], [&](float x, int) { return x * alpha; });
         }
         w.l += weights_of(z, w.m, scale_log2);
         write_weights<C>(w, p, z);
@@ -330,8 +348,12 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
 #pragma unroll
         for (int s = 0; s < R::kTailSteps; ++s) w.q[R::kHeadSteps + s] = *reinterpret_cast<const bf16x8*>(buf1 + C::kTailAt + other * C::kTail * 2 + w.tail_at[s]);
     }
+    u32x4 none = {0, 0, 0, 0};
 #pragma unroll
-    for (int b = 0; b < R::kBlocks; ++b) w.acc[b] = zeros();
+    for (int b = 0; b < R::kBlocks; ++b) {  // zeros by a product each: one instruction where 16 registers would be set
+        asm volatile("" : "+v"(none));
+        w.acc[b] = product(__builtin_bit_cast(bf16x8, none), __builtin_bit_cast(bf16x8, none), zeros());
+    }
     auto whole = [&] { return t < p.t1 && p.q.k_begin + t * C::kKeys + C::kKeys - 1 <= all_see; };
     // A tile of the fast loop; false: a reference moves, and the tile is still to be added (the next one's loads are under way).
     auto step = [&](const char* now, char* then) __attribute__((always_inline)) {
@@ -380,26 +402,125 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
                 f32x4{w.acc[b][4 * g], w.acc[b][4 * g + 1], w.acc[b][4 * g + 2], w.acc[b][4 * g + 3]};
     __syncthreads();
     const int rows = min(n_packed - p.rt * C::kM, C::kM);
+    const size_t row0 = (size_t)p.q.row0 * a.H + p.rt * C::kM, slot0 = (size_t)p.slot * a.m_cap;  // (a request's rows follow each other)
+#pragma unroll 1
     for (int r = wave; r < rows; r += C::kWaves) {
         const float l = sh.top[r >> 5 << 1][r & 31] + sh.top[(r >> 5 << 1) | 1][r & 31], m = sh.m[r >> 5][r & 31];
-        const Target<C> to = target_of<C>(a, p, r, lane == 0);
-        const float inv = to.out ? inverse(l) : 1.0f;
+        f32x4 x[C::kDv / 256];
 #pragma unroll
-        for (int k = 0; k < C::kDv / 4 / 64; ++k) {
-            const int chunk = k * 64 + lane;
-            const f32x4 x = *reinterpret_cast<const f32x4*>(place(r, chunk));
-            if (to.out) store4(to.out + 4 * chunk, x * inv);
-            else store4(to.sums + 4 * chunk, x);
-        }
-        if (lane == 0) {
-            if (!to.out) {
-                to.ml[0] = m;
-                to.ml[1] = l;
-            } else if (to.lse) {
-                *to.lse = log_sum(m, l);
-            }
+        for (int k = 0; k < C::kDv / 256; ++k) x[k] = *reinterpret_cast<const f32x4*>(place(r, k * 64 + lane));
+        if (p.whole) {
+            const float inv = inverse(l);
+#pragma unroll
+            for (int k = 0; k < C::kDv / 256; ++k) store4((typename C::Out*)a.out + (row0 + r) * C::kDv + 4 * (k * 64 + lane), x[k] * inv);
+            if (lane == 0 && a.lse) a.lse[row0 + r] = log_sum(m, l);
+        } else {
+#pragma unroll
+            for (int k = 0; k < C::kDv / 256; ++k) store4(a.part_o + (slot0 + r) * C::kDv + 4 * (k * 64 + lane), x[k]);
+            if (lane < 2) a.part_ml[2 * (slot0 + r) + lane] = lane ? l : m;
         }
     }
+}
+
+// Even pieces: where a batch has no more row tiles than there are workgroups, every item is cut into pieces of about the same length,
+// as long as makes one piece for each workgroup: half the sums of a cut line, each workgroup takes up one piece, and pieces of the same
+// keys, row tile by row tile, are neighbours (and share a die's cache).  The length is the shortest of 64 candidates, one per lane, from
+// an equal share of all key tiles upwards, for which the pieces do not outnumber the workgroups.  False: the line is cut instead.
+constexpr int kEvenRequests = 256;
+struct EvenScratch {
+    int tiles[kEvenRequests], row_tiles[kEvenRequests];
+    int counts[4][kWave];
+    int sums[8];
+    int piece[8];
+};
+template <class C>
+__device__ __forceinline__ bool even_piece(const Args& a, int share, EvenScratch& x, Piece& p, bool& mine) {
+    static_assert(C::kBlockThreads == kEvenRequests && C::kWaves == 4, "a request per thread");
+    if (a.B > kEvenRequests) return false;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    Seq q{};
+    int nk = 0, nrt = 0;
+    if (tid < a.B) {
+        q = sequence<C::kOp>(a, tid);
+        nrt = row_tiles_of<C>(a, q);
+        nk = nrt ? key_tiles<C>(a, q, 0) : 0;
+    }
+    x.tiles[tid] = nk;
+    x.row_tiles[tid] = nrt;
+    const int tiles = wave_sum_i(min(nk, 1 << 20) * min(nrt, 1 << 10)), items = wave_sum_i(nrt);
+    if (lane == 0) {
+        x.sums[wave] = tiles;
+        x.sums[4 + wave] = items;
+    }
+    __syncthreads();
+    const int n_items = uniform((x.sums[4] + x.sums[5]) + (x.sums[6] + x.sums[7]));
+    if (n_items > a.nb || n_items == 0) return false;
+    const int shortest = max(1, ceil_div(uniform((x.sums[0] + x.sums[1]) + (x.sums[2] + x.sums[3])), a.nb));
+    const int length = lane == 63 ? 1 << 24 : shortest + ((shortest * lane + 15) >> 4);
+    const float inv = 1.0f / (float)length;
+    auto pieces_of = [&](int tiles, int length, float inv) {  // ceil(tiles / length), at least 1
+        int n = max((int)((float)tiles * inv), 1);
+        n += n * length < tiles;
+        return n + (n * length < tiles);
+    };
+    int count = 0;
+#pragma unroll 1
+    for (int i = wave; i < a.B; i += 4) count += x.row_tiles[i] * pieces_of(x.tiles[i], length, inv);
+    x.counts[wave][lane] = count;
+    __syncthreads();
+    count = (x.counts[0][lane] + x.counts[1][lane]) + (x.counts[2][lane] + x.counts[3][lane]);
+    const int pick = __ffsll((unsigned long long)__ballot(count <= a.nb)) - 1;  // (lane 63 cuts nothing)
+    const int chosen = __builtin_amdgcn_readlane(length, pick);
+    if (chosen > shortest + (shortest >> 2) + 3) return false;  // lengths too uneven for that
+    const int pieces = nrt ? pieces_of(nk, chosen, 1.0f / (float)chosen) : 0;
+    int upto = wave_inclusive_scan_dpp(nrt * pieces);
+    if (lane == 63) x.sums[wave] = upto;
+    __syncthreads();
+    for (int k = 0; k < wave; ++k) upto += x.sums[k];
+    const int begin = upto - nrt * pieces;
+    if (tid == 0) x.piece[0] = 0;
+    __syncthreads();
+    if (share >= begin && share < upto) {
+        x.piece[0] = pieces;
+        x.piece[1] = share - begin;
+        x.piece[2] = q.row0;
+        x.piece[3] = q.rows;
+        x.piece[4] = q.k_end;
+        x.piece[5] = q.base;
+        x.piece[6] = tid;
+        x.piece[7] = nk;
+    }
+    __syncthreads();
+    int32_t* desc = a.desc + (size_t)share * kDescInts;
+    p.pieces = uniform(x.piece[0]);
+    mine = p.pieces > 0;
+    if (!mine) {
+        if (tid == 0) desc[0] = 0;
+        return true;
+    }
+    p.q.row0 = uniform(x.piece[2]);
+    p.q.rows = uniform(x.piece[3]);
+    p.q.k_begin = 0;
+    p.q.k_end = uniform(x.piece[4]);
+    p.q.base = uniform(x.piece[5]);
+    p.q.table = uniform(x.piece[6]);
+    p.q.first = 0;
+    const int at = uniform(x.piece[1]), all = uniform(x.piece[7]), tiles_of_rows = row_tiles_of<C>(a, p.q);
+    const int which = (int)((uint32_t)at / (uint32_t)tiles_of_rows), each = (int)((uint32_t)all / (uint32_t)p.pieces), longer = all - each * p.pieces;
+    p.hk = 0;
+    p.rt = at - which * tiles_of_rows;
+    p.t0 = which * each + min(which, longer);
+    p.t1 = p.t0 + each + (which < longer);
+    p.whole = p.pieces == 1;
+    p.slot = 2 * share;
+    p.share0 = share;
+    if (tid == 0) {
+        const bool first = which == 0 && !p.whole;
+        desc[1] = p.q.row0; desc[2] = 0; desc[3] = p.rt; desc[4] = min(p.q.rows * a.G - p.rt * C::kM, C::kM);
+        desc[5] = p.slot; desc[6] = p.slot + 2 * tiles_of_rows; desc[7] = 2 * tiles_of_rows;
+        desc[0] = first ? p.pieces : 0;
+    }
+    return true;
 }
 
 template <class C>
@@ -408,8 +529,15 @@ __global__ __launch_bounds__(C::kBlockThreads, 1) void latent_kernel(Args a) {
     __shared__ __align__(1024) char buf1[C::kBuf];
     __shared__ __align__(1024) LatentShared sh;
     const int share = share_of_block(blockIdx.x, a.nb);
-    const Line line = find_share<C>(a, share, reinterpret_cast<long long*>(buf0));
-    walk<C>(a, share, line, [&](const Piece& p) { run_latent<C>(a, p, buf0, buf1, sh); });
+    Piece p;
+    Walk<C> walk;
+    bool more = false;
+    const bool even = even_piece<C>(a, share, *reinterpret_cast<EvenScratch*>(buf1), p, more);
+    if (!even) walk.begin(a, share, find_share<C>(a, share, reinterpret_cast<long long*>(buf0)));
+    while (even ? more : walk.next(a, share, p)) {
+        run_latent<C>(a, p, buf0, buf1, sh);
+        more = false;
+    }
 }
 template <int KH, int KT, class OUT, bool PAGES16>
 struct Kernel<Latent<KH, KT, OUT, PAGES16>> {

@@ -587,9 +587,10 @@ __device__ __forceinline__ bf16x8 elements(s16x8 x, int kind) {
     }
     return __builtin_bit_cast(bf16x8, y);
 }
+__device__ __forceinline__ float odd_value(int kind) { return kind == kUp ? INFINITY : kind == kDown ? -INFINITY : __builtin_nanf(""); }
 // Adds the value of the kind where it has weight.
 __device__ __forceinline__ void put_odd(f32x16& acc, const f32x16& weight, int kind) {
-    const float value = kind == kUp ? INFINITY : kind == kDown ? -INFINITY : __builtin_nanf("");
+    const float value = odd_value(kind);
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] += weight[e] != 0.0f ? value : 0.0f;
 }
@@ -816,61 +817,85 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
         });
 }
 
-// Items of a share, one after the other.
-template <class C, class Run>
-__device__ __forceinline__ void walk(const Args& a, int share, const Line& line, Run run) {
-    int32_t* desc = a.desc + (size_t)share * kDescInts;
-    if (C::kOp != kShared && threadIdx.x == 0) desc[0] = 0;
-    const int n = n_sequences<C::kOp>(a);
-    long long seq_start = line.seq_start;
-    for (int s = line.seq; s < n && seq_start < line.hi; ++s) {
-        const Seq q = sequence<C::kOp>(a, s);
-        const int tiles = row_tiles_of<C>(a, q);
-        const long long head_units = units_before<C>(a, q, tiles);
-        int hk = seq_start < line.lo && head_units > 0 ? (int)quotient(line.lo - seq_start, head_units) : 0;
-        if (tiles > 0)
-            for (; hk < a.H_stream; ++hk) {
-                const long long head_start = seq_start + hk * head_units;
-                if (head_start >= line.hi) break;
-                int rt = 0;
-                if (head_start < line.lo) {  // the row tile that holds unit lo
+// The pieces of a share of the line, one after the other.
+template <class C>
+struct Walk {
+    Line line;
+    Seq q;
+    long long seq_start, head_units;
+    int s, hk, rt, tiles;
+    bool inside;  // q is sequence s
+
+    __device__ __forceinline__ void begin(const Args& a, int share, const Line& l) {
+        line = l;
+        s = l.seq;
+        seq_start = l.seq_start;
+        inside = false;
+        if (C::kOp != kShared && threadIdx.x == 0) a.desc[(size_t)share * kDescInts] = 0;
+    }
+    __device__ __forceinline__ bool next(const Args& a, int share, Piece& p) {
+        const int n = n_sequences<C::kOp>(a);
+        for (;;) {
+            if (!inside) {
+                if (s >= n || seq_start >= line.hi) return false;
+                q = sequence<C::kOp>(a, s);
+                tiles = row_tiles_of<C>(a, q);
+                head_units = units_before<C>(a, q, tiles);
+                hk = rt = 0;
+                if (tiles == 0) {
+                    ++s;
+                    continue;
+                }
+                if (seq_start < line.lo) {  // the stream head and the row tile that hold unit lo
+                    hk = (int)quotient(line.lo - seq_start, head_units);
+                    const long long head_start = seq_start + hk * head_units;
                     int last = tiles - 1;
                     while (rt < last) {
                         const int mid = (rt + last + 1) >> 1;
                         if (head_start + units_before<C>(a, q, mid) <= line.lo) rt = mid; else last = mid - 1;
                     }
                 }
-                for (; rt < tiles; ++rt) {
-                    const long long item = head_start + units_before<C>(a, q, rt);
-                    if (item >= line.hi) break;
-                    Piece p;
-                    p.q = q;
-                    p.hk = hk;
-                    p.rt = rt;
-                    const int nk = key_tiles<C>(a, q, rt);
-                    const long long t0 = line.lo - item - kItemCost, t1 = line.hi - item - kItemCost;
-                    p.t0 = t0 > 0 ? (int)min(t0, (long long)nk) : 0;
-                    p.t1 = t1 > 0 ? (int)min(t1, (long long)nk) : 0;
-                    p.whole = p.t0 == 0 && p.t1 == nk;
-                    p.slot = 0;
-                    p.share0 = share;
-                    p.pieces = 1;
-                    if (nk == 0 ? item < line.lo : p.t0 >= p.t1) continue;  // nothing of it is this share's
-                    if (!p.whole) {
-                        p.share0 = line.share_of(item + kItemCost);
-                        p.pieces = line.share_of(item + kItemCost + nk - 1) - p.share0 + 1;
-                        p.slot = 2 * share + (p.t0 == 0 ? 1 : 0);  // an item that begins here, or one that began before
-                        if (C::kOp != kShared && p.t0 == 0 && threadIdx.x == 0) {
-                            desc[1] = q.row0; desc[2] = hk; desc[3] = rt; desc[4] = min(q.rows * a.G - rt * C::kM, C::kM);
-                            desc[0] = p.pieces;
-                        }
-                    }
-                    run(p);
+                inside = true;
+            }
+            if (rt == tiles) {
+                rt = 0;
+                ++hk;
+            }
+            if (hk == a.H_stream) {
+                seq_start += head_units * a.H_stream;
+                ++s;
+                inside = false;
+                continue;
+            }
+            const long long item = seq_start + hk * head_units + units_before<C>(a, q, rt);
+            if (item >= line.hi) return false;
+            p.q = q;
+            p.hk = hk;
+            p.rt = rt++;
+            const int nk = key_tiles<C>(a, q, p.rt);
+            const long long t0 = line.lo - item - kItemCost, t1 = line.hi - item - kItemCost;
+            p.t0 = t0 > 0 ? (int)min(t0, (long long)nk) : 0;
+            p.t1 = t1 > 0 ? (int)min(t1, (long long)nk) : 0;
+            if (nk == 0 ? item < line.lo : p.t0 >= p.t1) continue;  // nothing of it is this share's
+            p.whole = p.t0 == 0 && p.t1 == nk;
+            p.slot = 0;
+            p.share0 = share;
+            p.pieces = 1;
+            if (!p.whole) {
+                p.share0 = line.share_of(item + kItemCost);
+                p.pieces = line.share_of(item + kItemCost + nk - 1) - p.share0 + 1;
+                p.slot = 2 * share + (p.t0 == 0 ? 1 : 0);  // an item that begins here, or one that began before
+                if (C::kOp != kShared && p.t0 == 0 && threadIdx.x == 0) {
+                    int32_t* desc = a.desc + (size_t)share * kDescInts;
+                    desc[1] = q.row0; desc[2] = hk; desc[3] = p.rt; desc[4] = min(q.rows * a.G - p.rt * C::kM, C::kM);
+                    desc[5] = p.slot; desc[6] = p.slot + 1; desc[7] = 2;  // the first piece's slot, the second's, and from there on
+                    desc[0] = p.pieces;
                 }
             }
-        seq_start += head_units * a.H_stream;
+            return true;
+        }
     }
-}
+};
 
 // Neighbouring shares read the same keys: they go to the same one of the 8 dies (workgroups are dealt to them in turn).
 __device__ __forceinline__ int share_of_block(int block, int nb) {
@@ -883,7 +908,10 @@ __global__ __launch_bounds__(C::kBlockThreads, 1) void simple_kernel(Args a) {
     __shared__ long long scratch[kThreads + kWaves];
     const int share = share_of_block(blockIdx.x, a.nb);
     const Line line = find_share<C>(a, share, scratch);
-    walk<C>(a, share, line, [&](const Piece& p) { run_simple<C>(a, p); });
+    Walk<C> walk;
+    walk.begin(a, share, line);
+    Piece p;
+    while (walk.next(a, share, p)) run_simple<C>(a, p);
 }
 
 template <class C>
@@ -892,7 +920,10 @@ __global__ __launch_bounds__(C::kBlockThreads, 2) void tiled_kernel(Args a) {  /
     __shared__ __align__(1024) char buf1[C::kBuf];
     const int share = share_of_block(blockIdx.x, a.nb);
     const Line line = find_share<C>(a, share, reinterpret_cast<long long*>(buf0));
-    walk<C>(a, share, line, [&](const Piece& p) { run_tiled<C>(a, p, buf0, buf1); });
+    Walk<C> walk;
+    walk.begin(a, share, line);
+    Piece p;
+    while (walk.next(a, share, p)) run_tiled<C>(a, p, buf0, buf1);
 }
 
 template <class C>
@@ -906,57 +937,75 @@ struct Kernel<Tiled<OP, KH, KT, DV, OUT>> {
     static constexpr auto run = tiled_kernel<Tiled<OP, KH, KT, DV, OUT>>;
 };
 
-// Sums of a row's pieces, joined: a wave per row, D_v / 64 columns a lane.
-template <int DV>
-struct Joined {
-    float o[DV / 64];
-    float m = -INFINITY, l = 0.0f;
-    __device__ __forceinline__ Joined() {
-#pragma unroll
-        for (int k = 0; k < DV / 64; ++k) o[k] = 0.0f;
-    }
-    __device__ __forceinline__ void add(const float* po, const float* ml, int lane) {
-        const float pm = ml[0], pl = ml[1];
-        if (pl == 0.0f) return;  // no visible key
-        float x[DV / 64];
-#pragma unroll
-        for (int k = 0; k < DV / 64; ++k) x[k] = po[lane * (DV / 64) + k];
-        const float m_new = fmaxf(m, pm);
-        const float use = m_new == -INFINITY ? 0.0f : m_new;
-        const float wa = __builtin_amdgcn_exp2f((m - use) * kLog2e), wb = __builtin_amdgcn_exp2f((pm - use) * kLog2e);
-#pragma unroll
-        for (int k = 0; k < DV / 64; ++k) o[k] = o[k] * wa + x[k] * wb;
-        l = l * wa + pl * wb;
-        m = m_new;
-    }
-    template <class Out>
-    __device__ __forceinline__ void write(Out* out, float* lse, int lane) const {
-        const float inv = inverse(l);
-#pragma unroll
-        for (int k = 0; k < DV / 64; ++k) {
-            if constexpr (sizeof(Out) == 2) out[lane * (DV / 64) + k] = (uint16_t)bf16_bits(o[k] * inv);
-            else out[lane * (DV / 64) + k] = o[k] * inv;
-        }
-        if (lse && lane == 0) *lse = log_sum(m, l);
-    }
+// A row's result out of the sums of its `pieces`: a wave per row.  source(k) says where piece k has its sums and its (score, sum of weights).
+// The statistics of 64 pieces are fetched at once, a piece a lane, and then the sums one behind the other without waiting.
+struct Source {
+    const float* sums;
+    const float* ml;
 };
+template <class C, class SourceOf>
+__device__ __forceinline__ void join(int pieces, SourceOf source, typename C::Out* out, float* lse, int lane) {
+    constexpr int kColumns = C::kDv / 64, kVector = kColumns < 4 ? kColumns : 4, kVectors = kColumns / kVector;
+    float o[kColumns], m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kColumns; ++c) o[c] = 0.0f;
+    for (int first = 0; first < pieces; first += kWave) {
+        const int n = min(pieces - first, kWave);
+        const Source mine = source(first + min(lane, n - 1));
+        float pm = mine.ml[0], pl = mine.ml[1];
+        if (lane >= n || pl == 0.0f) pm = -INFINITY, pl = 0.0f;  // (a piece without a visible key)
+        const float m_new = fmaxf(m, wave_max(pm)), use = m_new == -INFINITY ? 0.0f : m_new;
+        const float before = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((m - use) * kLog2e);
+        const float w = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((pm - use) * kLog2e);
+        float sum = w * pl;
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, kWave);
+        l = l * before + sum;
+        m = m_new;
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) o[c] *= before;
+        const uint32_t lo = (uint32_t)(uintptr_t)mine.sums, hi = (uint32_t)((uintptr_t)mine.sums >> 32);
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+            const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k));
+            const float* x = (const float*)(((uintptr_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, k) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, k));
+#pragma unroll
+            for (int v = 0; v < kVectors; ++v) {
+                float y[kVector];
+                __builtin_memcpy(y, x + v * 64 * kVector + lane * kVector, sizeof y);
+#pragma unroll
+                for (int c = 0; c < kVector; ++c) o[v * kVector + c] = fmaf(wk, y[c], o[v * kVector + c]);
+            }
+        }
+    }
+    const float inv = inverse(l);
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+        typename C::Out y[kVector];
+#pragma unroll
+        for (int c = 0; c < kVector; ++c) {
+            if constexpr (sizeof(typename C::Out) == 2) y[c] = (uint16_t)bf16_bits(o[v * kVector + c] * inv);
+            else y[c] = o[v * kVector + c] * inv;
+        }
+        __builtin_memcpy(out + v * 64 * kVector + lane * kVector, y, sizeof y);
+    }
+    if (lse && lane == 0) *lse = log_sum(m, l);
+}
 
-// Joins the items that begin in a share and go on behind it.  blockIdx.x: share, blockIdx.y: rows of the tile, kWaves at a time.
+// Joins the item of which a share has the first piece and others have more.  blockIdx.x: share, blockIdx.y: rows of the tile, kWaves at a time.
 template <class C>
 __global__ __launch_bounds__(kThreads) void join_shares_kernel(Args a) {
     const int32_t* desc = a.desc + (size_t)blockIdx.x * kDescInts;
     const int pieces = desc[0];
     if (pieces <= 0) return;
-    const int lane = threadIdx.x & 63, share = blockIdx.x;
-    for (int r = blockIdx.y * kWaves + (threadIdx.x >> 6); r < desc[4]; r += gridDim.y * kWaves) {
-        Joined<C::kDv> sum;
-        for (int k = 0; k < pieces; ++k) {
-            const size_t at = (size_t)(2 * (share + k) + (k == 0 ? 1 : 0)) * a.m_cap + r;
-            sum.add(a.part_o + at * C::kDv, a.part_ml + at * 2, lane);
-        }
+    const int lane = threadIdx.x & 63, first = desc[5], second = desc[6], step = desc[7];
+    for (int r = blockIdx.y * kWaves + uniform(threadIdx.x >> 6); r < desc[4]; r += gridDim.y * kWaves) {
         const Place to = place_of(a, desc[1], desc[2], desc[3] * C::kM + r);
         const size_t row = (size_t)to.row * a.H + to.head;
-        sum.write((typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
+        join<C>(pieces, [&](int k) {
+            const size_t at = (size_t)(k == 0 ? first : second + (k - 1) * step) * a.m_cap + r;
+            return Source{a.part_o + at * C::kDv, a.part_ml + at * 2};
+        }, (typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
     }
 }
 
@@ -965,13 +1014,13 @@ template <class C>
 __global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
     const int lane = threadIdx.x & 63;
     const size_t n = (size_t)a.N_cap * a.H;
-    const size_t row = (size_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    const size_t row = (size_t)blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
     const int i0 = clamp_to(a.cu_groups[0], 0, a.B), i1 = clamp_to(a.cu_groups[a.n_groups], 0, a.B);
     const int call_row = (int)(row / a.H), head = (int)(row - (size_t)call_row * a.H);
     if (row >= n || call_row < a.cu_q[i0] || call_row >= a.cu_q[i1]) return;
     const int own = a.refs[2 * (n + row)];
     if (own < 0) return;  // no prefix, and whole: written already
-    // the rows of the tile that held it: by its request for its own keys, by its group for the prefix
+    // the row's request, and that one's group
     int lo = i0, hi = i1;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -982,27 +1031,23 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
         const int mid = (g0 + g1) >> 1;
         if (a.cu_groups[mid] <= lo) g0 = mid; else g1 = mid;
     }
-    Joined<C::kDv> sum;
-    auto take = [&](int part, int seq) {
-        const Seq q = sequence<C::kOp>(a, seq);
-        if (part == 0 && q.k_end == 0) return;
+    int pieces[2], share0[2], place[2];
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+        const Seq q = sequence<C::kOp>(a, part ? a.n_groups + lo : g0);
         const size_t k = part * n + row;
-        const int pieces = clamp_to(a.refs[2 * k], 0, a.shares_cap), share0 = a.refs[2 * k + 1];
-        if (pieces == 0) {
-            sum.add(a.row_o + k * C::kDv, a.row_ml + k * 2, lane);
-            return;
-        }
-        const int packed = max(call_row - q.row0, 0) * a.G + head % a.G;
-        const int r = min(packed % C::kM, a.m_cap - 1);
-        for (int j = 0; j < pieces; ++j) {
-            const int share = clamp_to(share0 + j, 0, a.shares_cap - 1);
-            const size_t at = (size_t)(2 * share + (j == 0 ? 1 : 0)) * a.m_cap + r;
-            sum.add(a.part_o + at * C::kDv, a.part_ml + at * 2, lane);
-        }
-    };
-    take(0, g0);
-    take(1, a.n_groups + lo);
-    sum.write((typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
+        pieces[part] = part == 0 && q.k_end == 0 ? -1 : clamp_to(a.refs[2 * k], 0, a.shares_cap);
+        share0[part] = a.refs[2 * k + 1];
+        place[part] = min((max(call_row - q.row0, 0) * a.G + head % a.G) % C::kM, a.m_cap - 1);
+    }
+    const int n0 = pieces[0] < 0 ? 0 : max(pieces[0], 1), n1 = max(pieces[1], 1);  // (no pieces: the whole in row_o)
+    join<C>(n0 + n1, [&](int k) {
+        const int part = k < n0 ? 0 : 1, j = part ? k - n0 : k;
+        if (pieces[part] <= 0) return Source{a.row_o + (part * n + row) * C::kDv, a.row_ml + (part * n + row) * 2};
+        const int share = clamp_to(share0[part] + j, 0, a.shares_cap - 1);
+        const size_t at = (size_t)(2 * share + (j == 0 ? 1 : 0)) * a.m_cap + place[part];
+        return Source{a.part_o + at * C::kDv, a.part_ml + at * 2};
+    }, (typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -1076,7 +1121,7 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
         const size_t rows = (size_t)a.N_cap * a.H;
         hipLaunchKernelGGL((join_rows_kernel<C>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
     } else {
-        hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.nb, std::max(1, a.m_cap / 16)), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.nb, (a.m_cap + kWaves - 1) / kWaves), dim3(kThreads), 0, s, a);
     }
     return check_launch(who);
 }
