@@ -64,18 +64,16 @@ struct LatentLoads {
             from = buffer_at(a.k_head + ((uint64_t)(uint32_t)clamp_to(uniform(page), 0, a.n_pages - 1) * a.page_slots + uniform(place)) * a.head_stride, 16 * a.head_stride);
         else slot = slot_of<kLatent>(a, Where{page, (uint32_t)place});
     }
-    // Load i of 16 rows that follow each other in memory.
+    // Load i of 16 rows that follow each other in memory.  ENDS: some may be behind the last row (then all of the offset is the lane's: that
+    // is what is held against the descriptor).
+    template <bool ENDS>
     __device__ __forceinline__ void issue_rows(int i, Buffer rows, int stride, char* buf, int wave) const {
-        if (i < Head::kEach) {
-            const int k = i * Head::kRows;
-            to_lds(rows, (head_xor ^ ((k & 7) << 5)) + head_add, k * stride, buf + C::kHeadAt + (16 * wave + k) * C::kHead * 2);
-        } else {
-            const int k = (i - Head::kEach) * Tail::kRows;
-            to_lds(rows, tail_at, k * stride, buf + C::kTailAt + (16 * wave + k) * C::kTail * 2);
-        }
+        const bool head = i < Head::kEach;
+        const int k = head ? i * Head::kRows : (i - Head::kEach) * Tail::kRows, lane_at = head ? (head_xor ^ ((k & 7) << 5)) + head_add : tail_at;
+        to_lds(rows, ENDS ? lane_at + k * stride : lane_at, ENDS ? 0 : k * stride, buf + (head ? C::kHeadAt + (16 * wave + k) * C::kHead * 2 : C::kTailAt + (16 * wave + k) * C::kTail * 2));
     }
     __device__ __forceinline__ void issue(int i, const Args& a, char* buf, int wave, int lane) const {
-        if constexpr (C::kPages16) issue_rows(i, from, (int)a.head_stride, buf, wave);
+        if constexpr (C::kPages16) issue_rows<false>(i, from, (int)a.head_stride, buf, wave);
         else if (i < Head::kEach) Head::issue(i, a.k_head, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
         else Tail::issue(i - Head::kEach, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
     }
@@ -140,21 +138,6 @@ __device__ __forceinline__ f32x16 scores_of(const LatentRows<C>& w, const char* 
     return first_product<R::kHeadSteps + R::kTailSteps>([&](int s) __attribute__((always_inline)) {
         return *reinterpret_cast<const bf16x8*>(s < R::kHeadSteps ? buf + C::kHeadAt + w.k_at[s % 8] + (s / 8) * 256 : buf + C::kTailAt + w.tail_at[s - R::kHeadSteps]);
     }, w.q, beside);
-}
-
-__device__ __forceinline__ float largest(const f32x16& z) {
-    float top = fmaxf(z[0], z[1]);
-#pragma unroll
-    for (int e = 2; e < 16; ++e) top = fmaxf(top, z[e]);
-    return fmaxf(top, other_half(top));
-}
-
-// Weights of the scores, their sum added to the lane's.
-__device__ __forceinline__ float weights_of(f32x16& z, float m, float scale_log2) {
-    const float use = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -use));
-    return (((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]))) + (((z[8] + z[9]) + (z[10] + z[11])) + ((z[12] + z[13]) + (z[14] + z[15])));
 }
 
 template <class C>
@@ -337,7 +320,7 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
         const int stride = (int)a.head_stride;
         const Buffer queries = buffer_at((const char*)a.q + min(row0, rows - 1) * stride, row0 < rows ? (uint32_t)min(rows - row0, (size_t)16) * stride : 0u);
 #pragma unroll
-        for (int i = 0; i < LatentLoads<C>::kEach; ++i) loads.issue_rows(i, queries, stride, buf1, wave);
+        for (int i = 0; i < LatentLoads<C>::kEach; ++i) loads.template issue_rows<true>(i, queries, stride, buf1, wave);
         loads.take(a);
         loads.find(a, p, min(t + 1, p.t1 - 1), wave, lane);
         load_all(buf0);

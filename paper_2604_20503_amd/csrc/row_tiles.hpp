@@ -72,7 +72,8 @@ struct Args {
 
 struct Seq {
     int row0, rows;      // call rows
-    int k_begin, k_end;  // keys
+    int k_begin, k_end;  // keys (tiles begin at k_begin)
+    int k_first;         // the first one that is seen
     int base;            // packed row r sees keys up to base + r / G
     int table;           // row of the block table
     uint32_t first;      // expanded: slot of the first key
@@ -91,6 +92,7 @@ template <int OP>
 __device__ __forceinline__ Seq sequence(const Args& a, int s) {
     Seq q;
     q.first = 0;
+    q.k_first = 0;
     if constexpr (OP == kExpanded) {
         q.row0 = clamp_to(a.cu_q[s], 0, a.N_cap);
         q.rows = clamp_to(a.cu_q[s + 1], q.row0, a.N_cap) - q.row0;
@@ -126,10 +128,11 @@ __device__ __forceinline__ Seq sequence(const Args& a, int s) {
             if (a.cu_groups[mid] <= i) lo = mid; else hi = mid;
         }
         const bool in = a.cu_groups[lo] <= i && i < a.cu_groups[lo + 1];
-        q.k_begin = in ? clamp_to(a.prefix[lo], 0, cap) : 0;
+        q.k_first = in ? clamp_to(a.prefix[lo], 0, cap) : 0;
+        q.k_begin = q.k_first & ~15;  // (16 rows of a tile lie in one page, if pages hold a multiple of 16 tokens)
         if (!in) q.rows = 0;  // requests outside the groups have no output
     }
-    const int c = clamp_to(a.ctx[i], q.k_begin, cap);
+    const int c = clamp_to(a.ctx[i], q.k_first, cap);
     q.base = c;
     q.k_end = min(c + min(q.rows, cap), cap);
     q.table = i;
@@ -148,7 +151,7 @@ template <class C>
 __device__ __forceinline__ int key_tiles(const Args& a, const Seq& q, int rt) {
     int end = q.k_end;
     if constexpr (C::kOp == kExpanded) end = min(end, q.base + min(q.rows, (rt + 1) * C::kM));  // (G = 1) the last row's last key
-    return end > q.k_begin ? ceil_div(end - q.k_begin, C::kKeys) : 0;
+    return end > q.k_first ? ceil_div(end - q.k_begin, C::kKeys) : 0;
 }
 
 // Units of the line in front of row tile rt of a stream head.
@@ -317,7 +320,7 @@ __device__ __forceinline__ Target<C> target_of(const Args& a, const Piece& p, in
     const Place at = place_of(a, p.q.row0, p.hk, p.rt * C::kM + r_tile);
     const size_t row = (size_t)at.row * a.H + at.head;
     const bool prefix = C::kOp == kShared && p.q.base == 1 << 30;
-    const bool joined = C::kOp == kShared && (prefix || p.q.k_begin > 0);  // two items make the row
+    const bool joined = C::kOp == kShared && (prefix || p.q.k_first > 0);  // two items make the row
     if (p.whole && !joined) {
         if (C::kOp == kShared && first_lane) {
             const size_t n = (size_t)a.N_cap * a.H;
@@ -425,7 +428,7 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int key = kb + 4 * lg + e;
-            z[e] = key <= seen && key < k_last ? z[e] : -INFINITY;
+            z[e] = key >= p.q.k_first && key <= seen && key < k_last ? z[e] : -INFINITY;
             top = fmaxf(top, z[e]);
         }
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
@@ -440,7 +443,7 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
         m = m_new;
 #pragma unroll
         for (int b = 0; b < C::kDv / 16; ++b) acc[b] *= alpha;
-        const bool masked = __any(kb + 15 > seen || kb + 15 >= k_last);
+        const bool masked = __any(kb + 15 > seen || kb + 15 >= k_last || kb < p.q.k_first);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const uint32_t vs = (uint32_t)__shfl((int)slot, 4 * lg + e, kWave);
@@ -497,8 +500,10 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
 // LDS rows are read across (16 bytes of each of 32 keys) and, for V^T, in blocks of 4 keys x 32 bytes; their 16-byte chunks are
 // permuted by row such that both reach all banks.
 // ---------------------------------------------------------------------------------------------------------------
-template <int OP, int KH, int KT, int DV, class OUT>
+// PAGES16: 16 keys from a multiple of 16 on are 16 rows that follow each other (no pages, or pages of a multiple of 16 tokens).
+template <int OP, int KH, int KT, int DV, class OUT, bool PAGES16>
 struct Tiled {
+    static constexpr bool kPages16 = PAGES16;
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
     static constexpr bool kPair = sizeof(OUT) == 4;   // weights enter the second product as a pair of bf16
     static constexpr int kM = kTileRows, kKeys = 64;
@@ -548,25 +553,65 @@ __device__ __forceinline__ void arrive() {
 // A barrier for what waves hand each other through LDS: loads that are on their way there stay so.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// A wave's loads of a tile, one after the other.
+// A wave's loads of a tile: of keys' first and second parts and of values, rows 16 wave .. 16 wave + 15 each.  Where they lie is fetched a
+// tile ahead.  Of rows that follow each other every load has a descriptor and two offsets; else a lane holds the slot of a row.
 template <class C>
 struct TileLoads {
-    typedef RowLoads<C::kHead / 8, C::kWaves> Head;
-    typedef RowLoads<C::kTail / 8 ? C::kTail / 8 : 1, C::kWaves> Tail;
-    typedef RowLoads<C::kDv / 8, C::kWaves> Value;
-    static constexpr int kTails = C::kTail > 0 ? Tail::kEach : 0, kValues = C::kOp != kLatent ? Value::kEach : 0;
-    static constexpr int kEach = Head::kEach + kTails + kValues;
-    static __device__ __forceinline__ void issue(int i, const Args& a, int hk, uint32_t slot, char* buf, int wave, int lane) {
-        if (i < Head::kEach) Head::issue(i, a.k_head + (size_t)hk * a.head_hk, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
-        else if (i < Head::kEach + kTails) Tail::issue(i - Head::kEach, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
-        else if constexpr (kValues > 0) Value::issue(i - Head::kEach - kTails, a.v + (size_t)hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
+    static constexpr int CH = C::kHead / 8, CT = C::kTail / 8, CV = C::kDv / 8;
+    typedef RowLoads<CH, C::kWaves> Head;
+    typedef RowLoads<CT ? CT : 1, C::kWaves> Tail;
+    typedef RowLoads<CV, C::kWaves> Value;
+    static constexpr int kTails = CT ? Tail::kEach : 0, kEach = Head::kEach + kTails + Value::kEach;
+    Where next;
+    uint32_t slot;
+    Buffer head, tail, value;
+    int head_xor, head_add, tail_at, value_xor, value_add;
+
+    __device__ __forceinline__ void place_lane(const Args& a, int lane) {
+        head_xor = ((lane % CH) ^ permutation<CH>(lane / CH)) << 4;
+        head_add = (lane / CH) * (int)a.head_stride;
+        if constexpr (CT > 0) tail_at = (lane / CT) * (int)a.tail_stride + (((lane % CT) ^ permutation<CT>(lane / CT)) << 4);
+        value_xor = ((lane % CV) ^ permutation<CV>(lane / CV)) << 4;
+        value_add = (lane / CV) * (int)a.v_stride;
+    }
+    __device__ __forceinline__ void find(const Args& a, const Piece& p, int t, int wave, int lane) {
+        const int key = p.q.k_begin + t * C::kKeys;
+        next = find_key<C::kOp>(a, p.q, C::kPages16 ? min(key + 16 * wave, (p.q.k_end - 1) & ~15) : min(key + lane, p.q.k_end - 1));
+    }
+    // The loads to come are those of the tile that has been found.
+    __device__ __forceinline__ void take(const Args& a, const Piece& p) {
+        slot = slot_of<C::kOp>(a, next);
+        if constexpr (C::kPages16) {
+            slot = (uint32_t)uniform((int)slot);
+            // (behind the last key there may be no row: a load from there is zeros)
+            const uint32_t rows = C::kOp == kExpanded ? min((uint32_t)a.T_cap - min(slot, (uint32_t)a.T_cap), 16u) : 16u;
+            auto at = [&](const char* base, uint32_t stride) { return buffer_at(base + (uint64_t)slot * stride, rows ? (rows - 1) * stride + stride : 0u); };
+            head = at(a.k_head + (size_t)p.hk * a.head_hk, a.head_stride);
+            if constexpr (CT > 0) tail = at(a.k_tail, a.tail_stride);
+            value = at(a.v + (size_t)p.hk * a.v_hk, a.v_stride);
+        }
+    }
+    // (Where rows may end inside the 16, in the expanded form, all of the offset is the lane's: that is what is held against the descriptor.)
+    static __device__ __forceinline__ void get(Buffer from, int lane_at, int at, char* to) {
+        if constexpr (C::kOp == kExpanded) to_lds(from, lane_at + at, 0, to);
+        else to_lds(from, lane_at, at, to);
+    }
+    __device__ __forceinline__ void issue(int i, const Args& a, const Piece& p, char* buf, int wave, int lane) const {
+        if (i < Head::kEach) {
+            const int k = i * Head::kRows;
+            if constexpr (C::kPages16) get(head, (head_xor ^ ((k & 7) << 5)) + head_add, k * (int)a.head_stride, buf + C::kHeadAt + (16 * wave + k) * C::kHead * 2);
+            else Head::issue(i, a.k_head + (size_t)p.hk * a.head_hk, a.head_stride, slot, buf + C::kHeadAt, wave, lane);
+        } else if (i < Head::kEach + kTails) {
+            const int j = i - Head::kEach, k = j * Tail::kRows;
+            if constexpr (C::kPages16) get(tail, tail_at, k * (int)a.tail_stride, buf + C::kTailAt + (16 * wave + k) * C::kTail * 2);
+            else Tail::issue(j, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
+        } else {
+            const int j = i - Head::kEach - kTails, k = j * Value::kRows;
+            if constexpr (C::kPages16) get(value, (value_xor ^ ((k & 7) << 5)) + value_add, k * (int)a.v_stride, buf + C::kVAt + (16 * wave + k) * C::kDv * 2);
+            else Value::issue(j, a.v + (size_t)p.hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
+        }
     }
 };
-template <class C>
-__device__ __forceinline__ void load_tile(const Args& a, const Piece& p, uint32_t slot, char* buf, int wave, int lane) {
-#pragma unroll
-    for (int i = 0; i < TileLoads<C>::kEach; ++i) TileLoads<C>::issue(i, a, p.hk, slot, buf, wave, lane);
-}
 
 __device__ __forceinline__ float other_half(float x) {  // of the lane 32 further
     const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
@@ -676,30 +721,87 @@ struct Rows {
     }
 };
 
-// 32 keys of the tile in `buf`.
-template <class C, bool MASKED>
-__device__ __forceinline__ void take_keys(Rows<C>& w, const char* buf, int block, int key0, float scale_log2, int lane) {
-    typedef Rows<C> R;
-    const int h = lane >> 5;
-    f32x16 z = zeros();
-    {
-        const char* row = buf + C::kHeadAt + block * 32 * C::kHead * 2;
-#pragma unroll
-        for (int s = 0; s < R::kHeadSteps; ++s) z = product(*reinterpret_cast<const bf16x8*>(row + w.k_at[s % R::kOwnK] + (s / R::kOwnK) * 256), w.q[s], z);
-    }
-    if constexpr (C::kTail > 0) {
-        const char* row = buf + C::kTailAt + block * 32 * C::kTail * 2;
-#pragma unroll
-        for (int s = 0; s < R::kTailSteps; ++s) z = product(*reinterpret_cast<const bf16x8*>(row + w.tail_at[s]), w.q[R::kHeadSteps + s], z);
-    }
-    if constexpr (MASKED) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) z[e] = key0 + 8 * (e >> 2) + 4 * h + (e & 3) <= w.seen ? z[e] : -INFINITY;
-    }
+__device__ __forceinline__ float sum_of(const f32x16& z) {
+    return (((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]))) + (((z[8] + z[9]) + (z[10] + z[11])) + ((z[12] + z[13]) + (z[14] + z[15])));
+}
+__device__ __forceinline__ float largest(const f32x16& z) {
     float top = fmaxf(z[0], z[1]);
 #pragma unroll
     for (int e = 2; e < 16; ++e) top = fmaxf(top, z[e]);
-    top = fmaxf(top, other_half(top)) * scale_log2;
+    return fmaxf(top, other_half(top));
+}
+// Weights of the scores; their sum.
+__device__ __forceinline__ float weights_of(f32x16& z, float m, float scale_log2) {
+    const float use = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -use));
+    return sum_of(z);
+}
+// Eight weights as an operand.
+__device__ __forceinline__ bf16x8 operand_of(const f32x16& z, int s) {
+    return __builtin_bit_cast(bf16x8, u32x4{bf16_pair(z[8 * s], z[8 * s + 1]), bf16_pair(z[8 * s + 2], z[8 * s + 3]), bf16_pair(z[8 * s + 4], z[8 * s + 5]),
+                                            bf16_pair(z[8 * s + 6], z[8 * s + 7])});
+}
+
+// Scores of 32 keys of the tile in `buf`; beside(s) is called between the products.
+template <class C, class Beside>
+__device__ __forceinline__ f32x16 scores_of(const Rows<C>& w, const char* buf, int block, Beside beside) {
+    typedef Rows<C> R;
+    const char *head = buf + C::kHeadAt + block * 32 * C::kHead * 2, *tail = buf + C::kTailAt + block * 32 * C::kTail * 2;
+    return first_product<R::kHeadSteps + R::kTailSteps>([&](int s) __attribute__((always_inline)) {
+        return *reinterpret_cast<const bf16x8*>(s < R::kHeadSteps ? head + w.k_at[s % R::kOwnK] + (s / R::kOwnK) * 256 : tail + w.tail_at[s < R::kHeadSteps ? 0 : s - R::kHeadSteps]);
+    }, w.q, beside);
+}
+template <class C>
+__device__ __forceinline__ s16x8 values_of(const Rows<C>& w, const char* buf, int block, int s, int b) {
+    const char* at = buf + C::kVAt + (block * 32 + 16 * s) * C::kDv * 2 + w.v_at[b % Rows<C>::kOwnV] + (b / Rows<C>::kOwnV) * 256;
+    return transposed(at, at + 8 * C::kDv * 2);
+}
+
+// A tile of 64 keys that every row of the wave sees whole.  True: a score is ahead of its row's reference, and nothing has been added.
+template <class C, class Beside>
+__device__ __forceinline__ bool take_tile(Rows<C>& w, const char* buf, float scale_log2, Beside beside) {
+    typedef Rows<C> R;
+    constexpr int kSteps = R::kHeadSteps + R::kTailSteps;
+    f32x16 z[2];
+    z[0] = scores_of<C>(w, buf, 0, [&](int s) __attribute__((always_inline)) { beside(s); });
+    z[1] = scores_of<C>(w, buf, 1, [&](int s) __attribute__((always_inline)) { beside(kSteps + s); });
+    if (__any(fmaxf(largest(z[0]), largest(z[1])) * scale_log2 > w.m)) return true;
+    w.l += weights_of(z[0], w.m, scale_log2);
+    w.l += weights_of(z[1], w.m, scale_log2);
+    bf16x8 hi[4], lo[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) hi[s] = operand_of(z[s / 2], s % 2);
+    if constexpr (C::kPair) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[s][e] -= (float)(__bf16)z[s][e];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) lo[s] = operand_of(z[s / 2], s % 2);
+    }
+    in_turn<4 * R::kBlocks, 6, s16x8>([&](int k) __attribute__((always_inline)) { return values_of<C>(w, buf, k / (2 * R::kBlocks), k / R::kBlocks % 2, k % R::kBlocks); },
+                                      [&](int k, s16x8 v) __attribute__((always_inline)) {
+                                          const int b = k % R::kBlocks, s = k / R::kBlocks;
+                                          w.acc[b] = product(__builtin_bit_cast(bf16x8, v), hi[s], w.acc[b]);
+                                          if constexpr (C::kPair) w.acc[b] = product(__builtin_bit_cast(bf16x8, v), lo[s], w.acc[b]);
+                                      },
+                                      [](int) {});
+    return false;
+}
+
+// 32 keys of any tile, from key0 on: some may be masked, references move if they have to.
+template <class C>
+__device__ __forceinline__ void take_any_keys(Rows<C>& w, const char* buf, int block, int key0, int k_first, float scale_log2, int lane) {
+    typedef Rows<C> R;
+    const int h = lane >> 5;
+    f32x16 z = scores_of<C>(w, buf, block, [](int) {});
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int key = key0 + 8 * (e >> 2) + 4 * h + (e & 3);
+        z[e] = key >= k_first && key <= w.seen ? z[e] : -INFINITY;
+    }
+    const float top = largest(z) * scale_log2;
     // The reference keeps a distance above the largest score and is moved only when a score overtakes it: weights stay below one,
     // lose nothing (they are floating-point numbers) and the accumulators are rescaled a few times per row, not per tile.
     if (__any(top > w.m)) {
@@ -710,51 +812,29 @@ __device__ __forceinline__ void take_keys(Rows<C>& w, const char* buf, int block
 #pragma unroll
         for (int b = 0; b < R::kBlocks; ++b) w.acc[b] *= alpha;
     }
-    const float m = w.m == -INFINITY ? 0.0f : w.m;
-    float sum = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -m));
-        sum += z[e];
-    }
-    w.l += sum;
+    w.l += weights_of(z, w.m, scale_log2);
     bf16x8 hi[2], lo[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int s = 0; s < 2; ++s) hi[s] = operand_of(z, s);
+    if constexpr (C::kPair) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            hi[s][e] = (__bf16)z[8 * s + e];
-            if constexpr (C::kPair) lo[s][e] = (__bf16)(z[8 * s + e] - (float)hi[s][e]);
-        }
-    const char* row = buf + C::kVAt + block * 32 * C::kDv * 2;
+        for (int e = 0; e < 16; ++e) z[e] -= (float)(__bf16)z[e];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) lo[s] = operand_of(z, s);
+    }
 #pragma unroll
     for (int b = 0; b < R::kBlocks; ++b) {
-        s16x8 v[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const char* at = row + 16 * s * C::kDv * 2 + w.v_at[b % R::kOwnV] + (b / R::kOwnV) * 256;
-            v[s] = transposed(at, at + 8 * C::kDv * 2);
-        }
-        if constexpr (MASKED) {
-            if (__any(any_odd(v[0]) | any_odd(v[1]))) {
-                // a value that is not finite must not meet the zero weight of a row that does not see it: each kind is
-                // multiplied as 1 and takes its place only in rows that give it weight
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    w.acc[b] = product(elements(v[s], kFinite), hi[s], w.acc[b]);
-                    if constexpr (C::kPair) w.acc[b] = product(elements(v[s], kFinite), lo[s], w.acc[b]);
-                }
+        const s16x8 v0 = values_of<C>(w, buf, block, 0, b), v1 = values_of<C>(w, buf, block, 1, b);
+        if (__any(any_odd(v0) | any_odd(v1))) {
+            // a value that is not finite must not meet the zero weight of a row that does not see it: each kind is
+            // multiplied as 1 and takes its place only in rows that give it weight
+            w.acc[b] = product(elements(v1, kFinite), hi[1], product(elements(v0, kFinite), hi[0], w.acc[b]));
+            if constexpr (C::kPair) w.acc[b] = product(elements(v1, kFinite), lo[1], product(elements(v0, kFinite), lo[0], w.acc[b]));
 #pragma unroll 1
-                for (int kind = kUp; kind <= kNan; ++kind)
-                    put_odd(w.acc[b], product(elements(v[1], kind), hi[1], product(elements(v[0], kind), hi[0], zeros())), kind);
-                continue;
-            }
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const bf16x8 x = __builtin_bit_cast(bf16x8, v[s]);
-            if constexpr (C::kPair) w.acc[b] = product(x, lo[s], w.acc[b]);
-            w.acc[b] = product(x, hi[s], w.acc[b]);
+            for (int kind = kUp; kind <= kNan; ++kind) put_odd(w.acc[b], product(elements(v1, kind), hi[1], product(elements(v0, kind), hi[0], zeros())), kind);
+        } else {
+            w.acc[b] = product(__builtin_bit_cast(bf16x8, v1), hi[1], product(__builtin_bit_cast(bf16x8, v0), hi[0], w.acc[b]));
+            if constexpr (C::kPair) w.acc[b] = product(__builtin_bit_cast(bf16x8, v1), lo[1], product(__builtin_bit_cast(bf16x8, v0), lo[0], w.acc[b]));
         }
     }
 }
@@ -783,29 +863,59 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
         seen_first = last_key(a, p.q, first);
         seen_last = last_key(a, p.q, min(first + 31, n_packed - 1));
     }
-    auto find = [&](int t) { return find_key<C::kOp>(a, p.q, min(p.q.k_begin + t * C::kKeys + lane, p.q.k_end - 1)); };
+    TileLoads<C> loads;
+    loads.place_lane(a, lane);
+    int t = p.t0;
+    auto load_all = [&](char* to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < TileLoads<C>::kEach; ++i) loads.issue(i, a, p, to, wave, lane);
+    };
     __syncthreads();  // nobody reads the buffers any more
-    if (p.t0 < p.t1) {
-        int t = p.t0;
-        load_tile<C>(a, p, slot_of<C::kOp>(a, find(t)), buf0, wave, lane);
-        Where next = find(min(t + 1, p.t1 - 1));
-        auto step = [&](char* now, char* then) __attribute__((always_inline)) {
+    if (t < p.t1) {
+        loads.find(a, p, t, wave, lane);
+        loads.take(a, p);
+        load_all(buf0);
+        loads.find(a, p, min(t + 1, p.t1 - 1), wave, lane);
+        auto whole = [&] { return active && t < p.t1 && p.q.k_begin + t * C::kKeys >= p.q.k_first && p.q.k_begin + t * C::kKeys + C::kKeys - 1 <= seen_first; };
+        // A tile of the fast loop; false: a reference moves, and the tile is still to be added (the next one's loads are under way).
+        auto step = [&](const char* now, char* then) __attribute__((always_inline)) {
             arrive();  // (and nobody reads the other buffer any more)
-            if (t + 1 < p.t1) {
-                load_tile<C>(a, p, slot_of<C::kOp>(a, next), then, wave, lane);
-                next = find(min(t + 2, p.t1 - 1));
-            }
-            const int key0 = p.q.k_begin + t * C::kKeys;
-            if (active && key0 <= seen_last) {
-#pragma unroll 1
-                for (int block = 0; block < 2; ++block) {
-                    if (key0 + 32 * block + 31 <= seen_first) take_keys<C, false>(w, now, block, key0 + 32 * block, a.scale_log2, lane);
-                    else if (key0 + 32 * block <= seen_last) take_keys<C, true>(w, now, block, key0 + 32 * block, a.scale_log2, lane);
-                }
-            }
-            return ++t < p.t1;
+            loads.take(a, p);
+            loads.find(a, p, min(t + 2, p.t1 - 1), wave, lane);  // (behind the last tile this one is loaded again: a load too many costs less than asking)
+            static_assert(TileLoads<C>::kEach <= 2 * (R::kHeadSteps + R::kTailSteps), "a load beside a product");
+            const bool ahead = take_tile<C>(w, now, a.scale_log2, [&](int i) __attribute__((always_inline)) {
+                if (i < TileLoads<C>::kEach) loads.issue(i, a, p, then, wave, lane);
+            });
+            t += !ahead;
+            return !ahead;
         };
-        while (step(buf0, buf1) && step(buf1, buf0)) {}
+        bool loaded = false;  // the next tile's loads have been issued
+        while (t < p.t1) {
+            // the first tile, tiles with masked keys, tiles where a reference moves; every wave goes its own way, one barrier to a tile
+            const bool odd = (t - p.t0) & 1;
+            if (!loaded) {
+                arrive();
+                loads.take(a, p);
+                loads.find(a, p, min(t + 2, p.t1 - 1), wave, lane);
+                load_all(odd ? buf0 : buf1);
+            }
+            loaded = false;
+            const int key0 = p.q.k_begin + t * C::kKeys;
+            if (active)
+#pragma unroll 1
+                for (int block = 0; block < 2; ++block)
+                    if (key0 + 32 * block <= seen_last) take_any_keys<C>(w, odd ? buf1 : buf0, block, key0 + 32 * block, p.q.k_first, a.scale_log2, lane);
+            ++t;
+            // all the others: here the sums are the products' alone (where something else may touch them, the compiler makes a second
+            // set and copies them in every tile)
+            if (!odd)
+                while (whole()) {
+                    if (!step(buf1, buf0)) { loaded = true; break; }
+                    if (!whole()) break;
+                    if (!step(buf0, buf1)) { loaded = true; break; }
+                }
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // the load too many has its place until it has come
     }
     w.l += other_half(w.l);
     if (active && first + li < n_packed)
@@ -932,9 +1042,9 @@ template <int OP, int KH, int KT, int DV, class IN, class OUT>
 struct Kernel<Simple<OP, KH, KT, DV, IN, OUT>> {
     static constexpr auto run = simple_kernel<Simple<OP, KH, KT, DV, IN, OUT>>;
 };
-template <int OP, int KH, int KT, int DV, class OUT>
-struct Kernel<Tiled<OP, KH, KT, DV, OUT>> {
-    static constexpr auto run = tiled_kernel<Tiled<OP, KH, KT, DV, OUT>>;
+template <int OP, int KH, int KT, int DV, class OUT, bool PAGES16>
+struct Kernel<Tiled<OP, KH, KT, DV, OUT, PAGES16>> {
+    static constexpr auto run = tiled_kernel<Tiled<OP, KH, KT, DV, OUT, PAGES16>>;
 };
 
 // A row's result out of the sums of its `pieces`: a wave per row.  source(k) says where piece k has its sums and its (score, sum of weights).
