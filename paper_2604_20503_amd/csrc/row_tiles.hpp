@@ -6,7 +6,7 @@
 // call row r / G, query head r % G of the stream head) and cut into tiles of M rows; an *item* is one tile with all its keys.
 //     z[r, t] = scale * q[r] . k[t],   o[r] = sum_t exp(z[r, t] - m) v[t] / sum_t exp(z[r, t] - m)
 //
-// Schedule: the key tiles of all items lie end to end on a line (every item with kItemCost units in front for taking it up),
+// Schedule: the key tiles of all items lie end to end on a line (every item with C::kItemCost units in front for taking it up),
 // and the line is cut into equal shares, one per workgroup of a persistent grid.  Lengths stay on the device: every workgroup
 // adds them up for itself.  An item inside one share is finished there; one that a share boundary cuts leaves unnormalised
 // fp32 sums of its pieces in the workspace, at most two per share, which a second launch adds in the order of the shares
@@ -34,7 +34,6 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 constexpr int kThreads = 256;      // of the kernels below, where a configuration does not say otherwise
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTileRows = 128;     // most rows of a tile
-constexpr int kItemCost = 2;       // key tiles that taking up an item is worth
 constexpr int kDescInts = 8;       // merge descriptor of a share
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -157,7 +156,7 @@ __device__ __forceinline__ int key_tiles(const Args& a, const Seq& q, int rt) {
 // Units of the line in front of row tile rt of a stream head.
 template <class C>
 __device__ __forceinline__ long long units_before(const Args& a, const Seq& q, int rt) {
-    if constexpr (C::kOp != kExpanded) return (long long)rt * (kItemCost + key_tiles<C>(a, q, 0));
+    if constexpr (C::kOp != kExpanded) return (long long)rt * (C::kItemCost + key_tiles<C>(a, q, 0));
     // expanded: key_tiles grows by M / kKeys per row tile from the first tile that sees a key, except that the last tile may
     // hold fewer rows (it is summed by itself)
     static_assert(C::kOp != kExpanded || C::kM % C::kKeys == 0, "whole key tiles per row tile");
@@ -169,8 +168,8 @@ __device__ __forceinline__ long long units_before(const Args& a, const Seq& q, i
     const int r0 = t0 >= -kStep + 1 ? 0 : min((-t0) / kStep, full);
     const long long m = full - r0;
     long long sum = m * t0 + (long long)kStep * (m * (r0 + 1) + m * (m - 1) / 2);
-    sum += (long long)kItemCost * full;
-    if (rt > full) sum += kItemCost + key_tiles<C>(a, q, n - 1);
+    sum += (long long)C::kItemCost * full;
+    if (rt > full) sum += C::kItemCost + key_tiles<C>(a, q, n - 1);
     return sum;
 }
 
@@ -204,7 +203,7 @@ __device__ __forceinline__ long long shfl_up64(long long v, int d) {
     return ((long long)hi << 32) | (uint32_t)lo;
 }
 
-// Adds up the line; `scratch`: LDS for C::kBlocC::kBlockThreads and one sum per wave.
+// Adds up the line; `scratch`: LDS for C::kBlockThreads sums and one sum per wave.
 template <class C>
 __device__ __forceinline__ Line find_share(const Args& a, int share, long long* scratch) {
     const int n = n_sequences<C::kOp>(a), tid = threadIdx.x;
@@ -368,6 +367,7 @@ template <int OP, int KH, int KT, int DV, class IN, class OUT>
 struct Simple {
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
     static constexpr int kM = 64, kKeys = 64, kBlockThreads = kThreads, kPerUnit = 1;  // (kPerUnit: workgroups of a compute unit)
+    static constexpr int kItemCost = 2;  // key tiles that taking up an item is worth
     typedef IN In;
     typedef OUT Out;
 };
@@ -509,6 +509,7 @@ struct Tiled {
     static constexpr int kM = kTileRows, kKeys = 64;
     static constexpr int kBlockThreads = kThreads, kWaves = row_tiles::kWaves;
     static constexpr int kPerUnit = 2;                // workgroups of a compute unit, two waves to a SIMD
+    static constexpr int kItemCost = 5;  // measured: 20000 cycles (loads that nothing hides, tiles with masked keys, sums on their way out) against 4000 a tile
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kTailAt + kKeys * KT * 2;
     static constexpr int kBuf = kVAt + kKeys * DV * 2;
     typedef uint16_t In;
@@ -758,35 +759,61 @@ __device__ __forceinline__ s16x8 values_of(const Rows<C>& w, const char* buf, in
     return transposed(at, at + 8 * C::kDv * 2);
 }
 
+// Weights of 32 keys, two at a time, as operands (a pair of them where results are fp32) and their sum.
+template <bool PAIR>
+struct Weights {
+    uint32_t hi[8], lo[PAIR ? 8 : 1];
+    float sum = 0.0f;
+    __device__ __forceinline__ void take(int k, const f32x16& z, float use, float scale_log2) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(z[2 * k], scale_log2, -use)), y = __builtin_amdgcn_exp2f(fmaf(z[2 * k + 1], scale_log2, -use));
+        sum += x + y;
+        hi[k] = bf16_pair(x, y);
+        if constexpr (PAIR) lo[k] = bf16_pair(x - __builtin_bit_cast(float, hi[k] << 16), y - __builtin_bit_cast(float, hi[k] & 0xffff0000u));
+    }
+    // Those of step s of n.
+    __device__ __forceinline__ void take_part(int s, int n, const f32x16& z, float use, float scale_log2) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k >= s * 8 / n && k < (s + 1) * 8 / n) take(k, z, use, scale_log2);
+    }
+    static __device__ __forceinline__ bf16x8 operand(const uint32_t* x, int s) { return __builtin_bit_cast(bf16x8, u32x4{x[4 * s], x[4 * s + 1], x[4 * s + 2], x[4 * s + 3]}); }
+};
+__device__ __forceinline__ float largest_of_lane(const f32x16& z) {
+    float top = fmaxf(z[0], z[1]);
+#pragma unroll
+    for (int e = 2; e < 16; ++e) top = fmaxf(top, z[e]);
+    return top;
+}
+
 // A tile of 64 keys that every row of the wave sees whole.  True: a score is ahead of its row's reference, and nothing has been added.
+// The weights of a half are computed beside the products of the other: a product takes 32 cycles, in which eight instructions can be issued.
 template <class C, class Beside>
 __device__ __forceinline__ bool take_tile(Rows<C>& w, const char* buf, float scale_log2, Beside beside) {
     typedef Rows<C> R;
-    constexpr int kSteps = R::kHeadSteps + R::kTailSteps;
-    f32x16 z[2];
-    z[0] = scores_of<C>(w, buf, 0, [&](int s) __attribute__((always_inline)) { beside(s); });
-    z[1] = scores_of<C>(w, buf, 1, [&](int s) __attribute__((always_inline)) { beside(kSteps + s); });
-    if (__any(fmaxf(largest(z[0]), largest(z[1])) * scale_log2 > w.m)) return true;
-    w.l += weights_of(z[0], w.m, scale_log2);
-    w.l += weights_of(z[1], w.m, scale_log2);
-    bf16x8 hi[4], lo[4];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) hi[s] = operand_of(z[s / 2], s % 2);
-    if constexpr (C::kPair) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) z[s][e] -= (float)(__bf16)z[s][e];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) lo[s] = operand_of(z[s / 2], s % 2);
-    }
-    in_turn<4 * R::kBlocks, 6, s16x8>([&](int k) __attribute__((always_inline)) { return values_of<C>(w, buf, k / (2 * R::kBlocks), k / R::kBlocks % 2, k % R::kBlocks); },
-                                      [&](int k, s16x8 v) __attribute__((always_inline)) {
-                                          const int b = k % R::kBlocks, s = k / R::kBlocks;
-                                          w.acc[b] = product(__builtin_bit_cast(bf16x8, v), hi[s], w.acc[b]);
-                                          if constexpr (C::kPair) w.acc[b] = product(__builtin_bit_cast(bf16x8, v), lo[s], w.acc[b]);
-                                      },
-                                      [](int) {});
+    typedef Weights<C::kPair> W;
+    constexpr int kSteps = R::kHeadSteps + R::kTailSteps, kProducts = 2 * R::kBlocks;
+    const float use = w.m == -INFINITY ? 0.0f : w.m;
+    W x0, x1;
+    const f32x16 z0 = scores_of<C>(w, buf, 0, [&](int s) __attribute__((always_inline)) { beside(s); });
+    float top = -INFINITY;
+    const f32x16 z1 = scores_of<C>(w, buf, 1, [&](int s) __attribute__((always_inline)) {
+        beside(kSteps + s);
+        if (s == 0) top = largest_of_lane(z0);
+        x0.take_part(s, kSteps, z0, use, scale_log2);
+    });
+    if (__any(fmaxf(top, largest_of_lane(z1)) * scale_log2 > w.m)) return true;
+    auto add = [&](int block, const W& x, auto between) __attribute__((always_inline)) {
+        in_turn<kProducts, 6, s16x8>([&](int k) __attribute__((always_inline)) { return values_of<C>(w, buf, block, k / R::kBlocks, k % R::kBlocks); },
+                                     [&](int k, s16x8 v) __attribute__((always_inline)) {
+                                         const int b = k % R::kBlocks, s = k / R::kBlocks;
+                                         w.acc[b] = product(__builtin_bit_cast(bf16x8, v), W::operand(x.hi, s), w.acc[b]);
+                                         if constexpr (C::kPair) w.acc[b] = product(__builtin_bit_cast(bf16x8, v), W::operand(x.lo, s), w.acc[b]);
+                                     },
+                                     between);
+    };
+    add(0, x0, [&](int k) __attribute__((always_inline)) { x1.take_part(k, kProducts, z1, use, scale_log2); });
+    w.l += x0.sum + x1.sum;
+    add(1, x1, [](int) {});
     return false;
 }
 
@@ -983,7 +1010,7 @@ struct Walk {
             p.hk = hk;
             p.rt = rt++;
             const int nk = key_tiles<C>(a, q, p.rt);
-            const long long t0 = line.lo - item - kItemCost, t1 = line.hi - item - kItemCost;
+            const long long t0 = line.lo - item - C::kItemCost, t1 = line.hi - item - C::kItemCost;
             p.t0 = t0 > 0 ? (int)min(t0, (long long)nk) : 0;
             p.t1 = t1 > 0 ? (int)min(t1, (long long)nk) : 0;
             if (nk == 0 ? item < line.lo : p.t0 >= p.t1) continue;  // nothing of it is this share's
@@ -992,8 +1019,8 @@ struct Walk {
             p.share0 = share;
             p.pieces = 1;
             if (!p.whole) {
-                p.share0 = line.share_of(item + kItemCost);
-                p.pieces = line.share_of(item + kItemCost + nk - 1) - p.share0 + 1;
+                p.share0 = line.share_of(item + C::kItemCost);
+                p.pieces = line.share_of(item + C::kItemCost + nk - 1) - p.share0 + 1;
                 p.slot = 2 * share + (p.t0 == 0 ? 1 : 0);  // an item that begins here, or one that began before
                 if (C::kOp != kShared && p.t0 == 0 && threadIdx.x == 0) {
                     int32_t* desc = a.desc + (size_t)share * kDescInts;
@@ -1222,7 +1249,7 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
     int nb = compute_units() * C::kPerUnit;
     if (max_workgroups > 0) nb = std::min(nb, max_workgroups * C::kPerUnit);
     a.nb = std::min(nb, kSharesCap);
-    a.min_share = kItemCost + 1;
+    a.min_share = C::kItemCost + 1;
     hipStream_t s = (hipStream_t)stream;
     hipLaunchKernelGGL((Kernel<C>::run), dim3(a.nb), dim3(C::kBlockThreads), 0, s, a);
     int rc = check_launch(who);
