@@ -37,6 +37,8 @@ constexpr int kTileRows = 128;     // most rows of a tile
 constexpr int kDescInts = 8;       // merge descriptor of a share
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kSharesCap = 512;
+constexpr int kRefPlace = 10, kRefPrefix = 1 << 24;  // fields of a reference to a row's parts
 constexpr float kAhead = 40.0f;    // distance of a row's exponent reference from its largest score, in powers of two
 
 enum : int { kLatent = 0, kExpanded = 1, kShared = 2 };
@@ -314,6 +316,7 @@ struct Target {
     float* ml;
 };
 // For row r_tile of the piece; `first_lane` says (in a batch behind prefixes) where the row's parts are to be found.
+static_assert(kSharesCap <= 1 << kRefPlace && kTileRows <= 1 << 10 && kRefPlace + 10 <= 24, "a reference is a share, a row of its tile and a bit");
 template <class C>
 __device__ __forceinline__ Target<C> target_of(const Args& a, const Piece& p, int r_tile, bool first_lane) {
     const Place at = place_of(a, p.q.row0, p.hk, p.rt * C::kM + r_tile);
@@ -330,7 +333,7 @@ __device__ __forceinline__ Target<C> target_of(const Args& a, const Piece& p, in
     if (C::kOp == kShared && first_lane && p.t0 == 0) {  // whoever begins the item says where its pieces are
         const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
         a.refs[2 * k] = p.whole ? 0 : p.pieces;
-        a.refs[2 * k + 1] = p.share0;
+        a.refs[2 * k + 1] = p.share0 | r_tile << kRefPlace | (prefix ? 0 : kRefPrefix);
     }
     if (p.whole) {
         const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
@@ -404,26 +407,44 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
     for (int b = 0; b < C::kDv / 16; ++b) acc[b] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
     const int k_first = p.q.k_begin + p.t0 * C::kKeys, k_last = min(p.q.k_begin + p.t1 * C::kKeys, p.q.k_end);
+    // Where the next 16 keys lie is fetched while these are multiplied; where there are registers for it (not in the latent form) their
+    // rows too, and these ones' values before their weights are known.
+    constexpr int kSteps = C::kDk / 16, kBlocks = C::kDv / 16;
+    constexpr bool kEarly = kSteps <= 12;
+    auto slot_at = [&](int kb) { return slot_of<C::kOp>(a, find_key<C::kOp>(a, p.q, min(kb + li, k_last - 1))); };
+    auto key_of = [&](uint32_t slot, int s) {
+        if (s < C::kHead / 16) return load4((const In*)(a.k_head + (size_t)slot * a.head_stride + (size_t)p.hk * a.head_hk) + 16 * s + 4 * lg);
+        return load4((const In*)(a.k_tail + (size_t)slot * a.tail_stride) + 16 * (s - C::kHead / 16) + 4 * lg);
+    };
+    auto value_of = [&](uint32_t slot, int e, int b) {
+        const uint32_t vs = (uint32_t)__shfl((int)slot, 4 * lg + e, kWave);
+        return widen(((const In*)(a.v + (size_t)vs * a.v_stride + (size_t)p.hk * a.v_hk))[16 * b + li]);
+    };
+    uint32_t slot = k_first < k_last ? slot_at(k_first) : 0;
+    f32x4 key[kEarly ? kSteps : 1];
+    if (kEarly && k_first < k_last)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) key[kEarly ? s : 0] = key_of(slot, s);
 #pragma unroll 1
     for (int kb = k_first; kb < k_last; kb += 16) {
-        const uint32_t slot = slot_of<C::kOp>(a, find_key<C::kOp>(a, p.q, min(kb + li, k_last - 1)));
-        const In* kh = (const In*)(a.k_head + (size_t)slot * a.head_stride + (size_t)p.hk * a.head_hk);
+        const uint32_t now = slot;
+        slot = slot_at(kb + 16);  // (behind the last key: that one's again)
+        float value[kEarly ? 4 : 1][kBlocks];
+        if constexpr (kEarly)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) value[e][b] = value_of(now, e, b);
         f32x4 z = {0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < C::kHead / 16; ++s) {
-            const f32x4 k4 = load4(kh + 16 * s + 4 * lg);
+        for (int s = 0; s < kSteps; ++s) {
+            const f32x4 k4 = kEarly ? key[kEarly ? s : 0] : key_of(now, s);
 #pragma unroll
             for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q[s][e], z, 0, 0, 0);
         }
-        if constexpr (C::kTail > 0) {
-            const In* kt = (const In*)(a.k_tail + (size_t)slot * a.tail_stride);
+        if constexpr (kEarly)
 #pragma unroll
-            for (int s = 0; s < C::kTail / 16; ++s) {
-                const f32x4 k4 = load4(kt + 16 * s + 4 * lg);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q[C::kHead / 16 + s][e], z, 0, 0, 0);
-            }
-        }
+            for (int s = 0; s < kSteps; ++s) key[s] = key_of(slot, s);
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -446,13 +467,11 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
         const bool masked = __any(kb + 15 > seen || kb + 15 >= k_last || kb < p.q.k_first);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t vs = (uint32_t)__shfl((int)slot, 4 * lg + e, kWave);
-            const In* vp = (const In*)(a.v + (size_t)vs * a.v_stride + (size_t)p.hk * a.v_hk);
-            float v[C::kDv / 16];
+            float v[kBlocks];
             uint32_t odd = 0;
 #pragma unroll
-            for (int b = 0; b < C::kDv / 16; ++b) {
-                v[b] = widen(vp[16 * b + li]);
+            for (int b = 0; b < kBlocks; ++b) {
+                v[b] = kEarly ? value[kEarly ? e : 0][b] : value_of(now, e, b);
                 odd |= (__builtin_bit_cast(uint32_t, v[b]) & 0x7f800000u) == 0x7f800000u;
             }
             if (!masked || !__any(odd)) {
@@ -802,6 +821,7 @@ __device__ __forceinline__ bool take_tile(Rows<C>& w, const char* buf, float sca
         x0.take_part(s, kSteps, z0, use, scale_log2);
     });
     if (__any(fmaxf(top, largest_of_lane(z1)) * scale_log2 > w.m)) return true;
+    __builtin_amdgcn_s_setprio(1);  // the wave beside this one on the SIMD, at its scores or weights, gives way: 4 % of a long prompt's time
     auto add = [&](int block, const W& x, auto between) __attribute__((always_inline)) {
         in_turn<kProducts, 6, s16x8>([&](int k) __attribute__((always_inline)) { return values_of<C>(w, buf, block, k / R::kBlocks, k % R::kBlocks); },
                                      [&](int k, s16x8 v) __attribute__((always_inline)) {
@@ -814,6 +834,7 @@ __device__ __forceinline__ bool take_tile(Rows<C>& w, const char* buf, float sca
     add(0, x0, [&](int k) __attribute__((always_inline)) { x1.take_part(k, kProducts, z1, use, scale_log2); });
     w.l += x0.sum + x1.sum;
     add(1, x1, [](int) {});
+    __builtin_amdgcn_s_setprio(0);
     return false;
 }
 
@@ -1152,31 +1173,16 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
     const int lane = threadIdx.x & 63;
     const size_t n = (size_t)a.N_cap * a.H;
     const size_t row = (size_t)blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
+    if (row >= n) return;
     const int i0 = clamp_to(a.cu_groups[0], 0, a.B), i1 = clamp_to(a.cu_groups[a.n_groups], 0, a.B);
     const int call_row = (int)(row / a.H), head = (int)(row - (size_t)call_row * a.H);
-    if (row >= n || call_row < a.cu_q[i0] || call_row >= a.cu_q[i1]) return;
-    const int own = a.refs[2 * (n + row)];
-    if (own < 0) return;  // no prefix, and whole: written already
-    // the row's request, and that one's group
-    int lo = i0, hi = i1;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.cu_q[mid] <= call_row) lo = mid; else hi = mid;
-    }
-    int g0 = 0, g1 = a.n_groups;
-    while (g1 - g0 > 1) {
-        const int mid = (g0 + g1) >> 1;
-        if (a.cu_groups[mid] <= lo) g0 = mid; else g1 = mid;
-    }
-    int pieces[2], share0[2], place[2];
-#pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        const Seq q = sequence<C::kOp>(a, part ? a.n_groups + lo : g0);
-        const size_t k = part * n + row;
-        pieces[part] = part == 0 && q.k_end == 0 ? -1 : clamp_to(a.refs[2 * k], 0, a.shares_cap);
-        share0[part] = a.refs[2 * k + 1];
-        place[part] = min((max(call_row - q.row0, 0) * a.G + head % a.G) % C::kM, a.m_cap - 1);
-    }
+    // (The references are read beside the bounds: what stands there for a row outside of them is not used.)
+    const u32x2 own = reinterpret_cast<const u32x2*>(a.refs)[n + row], common = reinterpret_cast<const u32x2*>(a.refs)[row];
+    if (call_row < a.cu_q[i0] || call_row >= a.cu_q[i1] || (int)own[0] < 0) return;  // (no prefix, and whole: written already)
+    const bool behind = own[1] & kRefPrefix;
+    const int pieces[2] = {behind ? clamp_to((int)common[0], 0, a.shares_cap) : -1, clamp_to((int)own[0], 0, a.shares_cap)};
+    const int share0[2] = {(int)(common[1] & ((1 << kRefPlace) - 1)), (int)(own[1] & ((1 << kRefPlace) - 1))};
+    const int place[2] = {min((int)(common[1] >> kRefPlace & 1023), a.m_cap - 1), min((int)(own[1] >> kRefPlace & 1023), a.m_cap - 1)};
     const int n0 = pieces[0] < 0 ? 0 : max(pieces[0], 1), n1 = max(pieces[1], 1);  // (no pieces: the whole in row_o)
     join<C>(n0 + n1, [&](int k) {
         const int part = k < n0 ? 0 : 1, j = part ? k - n0 : k;
@@ -1190,8 +1196,6 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
 // ---------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------
-constexpr int kSharesCap = 512;
-
 struct Layout {
     size_t part_o, part_ml, desc, row_o, row_ml, refs, total;
 };
@@ -1258,7 +1262,8 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
         const size_t rows = (size_t)a.N_cap * a.H;
         hipLaunchKernelGGL((join_rows_kernel<C>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
     } else {
-        hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.nb, (a.m_cap + kWaves - 1) / kWaves), dim3(kThreads), 0, s, a);
+        // 16 workgroups a share: one row a wave of a latent tile, two of a tile of heads; with 32 there the launching of workgroups took longer: 20 us, not 17.6
+        hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.nb, std::min(16, (a.m_cap + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
     }
     return check_launch(who);
 }
