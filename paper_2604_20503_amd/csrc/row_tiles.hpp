@@ -369,8 +369,9 @@ __device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_t
 template <int OP, int KH, int KT, int DV, class IN, class OUT>
 struct Simple {
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
-    static constexpr int kM = 64, kKeys = 64, kBlockThreads = kThreads, kPerUnit = 1;  // (kPerUnit: workgroups of a compute unit)
-    static constexpr int kItemCost = 2;  // key tiles that taking up an item is worth
+    static constexpr int kM = 64, kKeys = 32, kBlockThreads = kThreads, kPerUnit = 1;  // (kPerUnit: workgroups of a compute unit)
+    static constexpr int kItemCost = 2;  // key tiles that taking up an item is worth (measured: 14000 cycles against 7000)
+    static constexpr int kMinShare = 1;  // units of a share of a short line: a tile of its own costs less than waiting for a neighbour's
     typedef IN In;
     typedef OUT Out;
 };
@@ -529,6 +530,7 @@ struct Tiled {
     static constexpr int kBlockThreads = kThreads, kWaves = row_tiles::kWaves;
     static constexpr int kPerUnit = 2;                // workgroups of a compute unit, two waves to a SIMD
     static constexpr int kItemCost = 5;  // measured: 20000 cycles (loads that nothing hides, tiles with masked keys, sums on their way out) against 4000 a tile
+    static constexpr int kMinShare = kItemCost + 1;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kTailAt + kKeys * KT * 2;
     static constexpr int kBuf = kVAt + kKeys * DV * 2;
     typedef uint16_t In;
@@ -1253,7 +1255,7 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
     int nb = compute_units() * C::kPerUnit;
     if (max_workgroups > 0) nb = std::min(nb, max_workgroups * C::kPerUnit);
     a.nb = std::min(nb, kSharesCap);
-    a.min_share = C::kItemCost + 1;
+    a.min_share = C::kMinShare;
     hipStream_t s = (hipStream_t)stream;
     hipLaunchKernelGGL((Kernel<C>::run), dim3(a.nb), dim3(C::kBlockThreads), 0, s, a);
     int rc = check_launch(who);
