@@ -438,7 +438,11 @@ __device__ __forceinline__ bool even_piece(const Args& a, int share, EvenScratch
     __syncthreads();
     const int n_items = uniform((x.sums[4] + x.sums[5]) + (x.sums[6] + x.sums[7]));
     if (n_items > a.nb || n_items == 0) return false;
-    const int shortest = max(1, ceil_div(uniform((x.sums[0] + x.sums[1]) + (x.sums[2] + x.sums[3])), a.nb));
+    const int n_tiles = uniform((x.sums[0] + x.sums[1]) + (x.sums[2] + x.sums[3]));
+    // Where workgroups are plenty: a tile more of a piece takes 2 us, a piece more of a join a sixth of that.  Length l of t tiles costs
+    // 2 l + t / 3 l, least at sqrt(t / 6).  (8000 keys, 16 heads: 69 us in 126 pieces of one tile, 47 us in 27.)
+    const int cheapest = (int)(__builtin_amdgcn_sqrtf((float)n_tiles / (6.0f * n_items)) + 0.5f);
+    const int shortest = max(max(cheapest, 1), ceil_div(n_tiles, a.nb));
     const int length = lane == 63 ? 1 << 24 : shortest + ((shortest * lane + 15) >> 4);
     const float inv = 1.0f / (float)length;
     auto pieces_of = [&](int tiles, int length, float inv) {  // ceil(tiles / length), at least 1
