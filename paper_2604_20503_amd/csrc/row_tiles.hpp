@@ -333,7 +333,7 @@ __device__ __forceinline__ Target<C> target_of(const Args& a, const Piece& p, in
     if (C::kOp == kShared && first_lane && p.t0 == 0) {  // whoever begins the item says where its pieces are
         const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
         a.refs[2 * k] = p.whole ? 0 : p.pieces;
-        a.refs[2 * k + 1] = p.share0 | r_tile << kRefPlace | (prefix ? 0 : kRefPrefix);
+        a.refs[2 * k + 1] = p.share0 | r_tile << kRefPlace | (p.q.k_first > 0 ? kRefPrefix : 0);
     }
     if (p.whole) {
         const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
