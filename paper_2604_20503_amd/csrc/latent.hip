@@ -120,7 +120,7 @@ int rows_cap(const fsr_latent_params* p) { return (int)std::max(1LL, std::min((l
 
 template <int DL, int DR>
 int run(const Args& a, const fsr_latent_params* p, void* stream, const char* who) {
-    if (p->dtype == FSR_F32) return launch<Simple<kLatent, DL, DR, DL, float, float>>(a, p->max_workgroups, stream, who);
+    if (p->dtype == FSR_F32) return launch<Simple<kLatent, DL, DR, DL>>(a, p->max_workgroups, stream, who);
     const bool pages16 = p->P % 16 == 0;
     if (p->out_dtype == FSR_F32)
         return pages16 ? launch<Latent<DL, DR, float, true>>(a, p->max_workgroups, stream, who) : launch<Latent<DL, DR, float, false>>(a, p->max_workgroups, stream, who);

@@ -31,7 +31,7 @@ int rows_cap(const fsr_expanded_params* p) { return std::max(1, std::min(p->N_ca
 
 template <int DN, int DR, int DV>
 int run(const Args& a, const fsr_expanded_params* p, void* stream, const char* who) {
-    if (p->dtype == FSR_F32) return launch<Simple<kExpanded, DN, DR, DV, float, float>>(a, p->max_workgroups, stream, who);
+    if (p->dtype == FSR_F32) return launch<Simple<kExpanded, DN, DR, DV>>(a, p->max_workgroups, stream, who);
     if (p->out_dtype == FSR_F32) return launch<Tiled<kExpanded, DN, DR, DV, float, true>>(a, p->max_workgroups, stream, who);
     return launch<Tiled<kExpanded, DN, DR, DV, uint16_t, true>>(a, p->max_workgroups, stream, who);
 }

@@ -21,7 +21,6 @@ struct Latent {
     static constexpr bool kPair = sizeof(OUT) == 4, kPages16 = PAGES16;
     static constexpr int kM = 64, kKeys = 64, kBlockThreads = 256, kWaves = 4, kPerUnit = 1, kItemCost = 2, kMinShare = kItemCost + 1;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kBuf = kTailAt + kKeys * KT * 2;
-    typedef uint16_t In;
     typedef OUT Out;
 };
 

@@ -38,7 +38,7 @@ constexpr int kDescInts = 8;       // merge descriptor of a share
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kSharesCap = 512;
-constexpr int kRefPlace = 10, kRefPrefix = 1 << 24;  // fields of a reference to a row's parts
+constexpr int kRefPlace = 10, kRefPrefix = 1 << 24;  // fields of a reference to a part of a row: its place in the tile; there is a prefix before it
 constexpr float kAhead = 40.0f;    // distance of a row's exponent reference from its largest score, in powers of two
 
 enum : int { kLatent = 0, kExpanded = 1, kShared = 2 };
@@ -68,7 +68,7 @@ struct Args {
     int32_t* desc;    // [shares_cap][kDescInts]
     float* row_o;     // shared: [2][N_cap * H][D_v] sums of items that are whole: prefix, own
     float* row_ml;    // shared: [2][N_cap * H][2]
-    int32_t* refs;    // shared: [2][N_cap * H][2] pieces (0: in row_o) and first share of the item
+    int32_t* refs;    // shared: [2][N_cap * H][2] pieces of the item (0: in row_o; -1: done); its first share, the row's place in its tile, kRefPrefix
 };
 
 struct Seq {
@@ -366,24 +366,14 @@ __device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_t
 // on v_mfma_f32_16x16x4_f32; the accumulator layout of S^T (lane: keys 4 (lane / 16) + e, row lane % 16) is the operand
 // layout of P^T if step e of the second product takes keys 4 g + e of lane group g.
 // ---------------------------------------------------------------------------------------------------------------
-template <int OP, int KH, int KT, int DV, class IN, class OUT>
+template <int OP, int KH, int KT, int DV>
 struct Simple {
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
     static constexpr int kM = 64, kKeys = 32, kBlockThreads = kThreads, kPerUnit = 1;  // (kPerUnit: workgroups of a compute unit)
     static constexpr int kItemCost = 2;  // key tiles that taking up an item is worth (measured: 14000 cycles against 7000)
     static constexpr int kMinShare = 1;  // units of a share of a short line: a tile of its own costs less than waiting for a neighbour's
-    typedef IN In;
-    typedef OUT Out;
+    typedef float Out;
 };
-
-__device__ __forceinline__ float widen(float x) { return x; }
-__device__ __forceinline__ float widen(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
-__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
-__device__ __forceinline__ f32x4 load4(const uint16_t* p) {
-    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
-    const uint32_t lo = x[0], hi = x[1];
-    return f32x4{widen((uint16_t)lo), widen((uint16_t)(lo >> 16)), widen((uint16_t)hi), widen((uint16_t)(hi >> 16))};
-}
 
 // Last key that packed row r sees.
 __device__ __forceinline__ int last_key(const Args& a, const Seq& q, int r) {
@@ -392,16 +382,15 @@ __device__ __forceinline__ int last_key(const Args& a, const Seq& q, int r) {
 
 template <class C>
 __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
-    typedef typename C::In In;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lg = lane >> 4;
     const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + wave * 16;
     if (first >= n_packed) return;
     const int r = min(first + li, n_packed - 1);
     const Place at = place_of(a, p.q.row0, p.hk, r);
-    const In* qp = (const In*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
+    const float* qp = (const float*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
     f32x4 q[C::kDk / 16];
 #pragma unroll
-    for (int s = 0; s < C::kDk / 16; ++s) q[s] = load4(qp + 16 * s + 4 * lg);
+    for (int s = 0; s < C::kDk / 16; ++s) q[s] = *reinterpret_cast<const f32x4*>(qp + 16 * s + 4 * lg);
     const int seen = last_key(a, p.q, r);
     f32x4 acc[C::kDv / 16];
 #pragma unroll
@@ -414,12 +403,12 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
     constexpr bool kEarly = kSteps <= 12;
     auto slot_at = [&](int kb) { return slot_of<C::kOp>(a, find_key<C::kOp>(a, p.q, min(kb + li, k_last - 1))); };
     auto key_of = [&](uint32_t slot, int s) {
-        if (s < C::kHead / 16) return load4((const In*)(a.k_head + (size_t)slot * a.head_stride + (size_t)p.hk * a.head_hk) + 16 * s + 4 * lg);
-        return load4((const In*)(a.k_tail + (size_t)slot * a.tail_stride) + 16 * (s - C::kHead / 16) + 4 * lg);
+        const char* part = s < C::kHead / 16 ? a.k_head + (size_t)slot * a.head_stride + (size_t)p.hk * a.head_hk + 64 * s : a.k_tail + (size_t)slot * a.tail_stride + 64 * (s - C::kHead / 16);
+        return *reinterpret_cast<const f32x4*>(part + 16 * lg);
     };
     auto value_of = [&](uint32_t slot, int e, int b) {
         const uint32_t vs = (uint32_t)__shfl((int)slot, 4 * lg + e, kWave);
-        return widen(((const In*)(a.v + (size_t)vs * a.v_stride + (size_t)p.hk * a.v_hk))[16 * b + li]);
+        return ((const float*)(a.v + (size_t)vs * a.v_stride + (size_t)p.hk * a.v_hk))[16 * b + li];
     };
     uint32_t slot = k_first < k_last ? slot_at(k_first) : 0;
     f32x4 key[kEarly ? kSteps : 1];
@@ -520,6 +509,12 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
 // LDS rows are read across (16 bytes of each of 32 keys) and, for V^T, in blocks of 4 keys x 32 bytes; their 16-byte chunks are
 // permuted by row such that both reach all banks.
 // ---------------------------------------------------------------------------------------------------------------
+//
+// What bounds it: each of the four waves reads all keys and values of a tile, 128 KB with heads of 128 (160 KB with a second part of 64)
+// and 32 KB (40) to write, 1280 (1600) cycles of a compute unit's LDS against 1024 (1280) of its matrix cores and 900 of exponentials
+// and conversions.  Measured: 1775 cycles a tile where two workgroups share a unit; 2048 rows of 32 heads behind 6000 tokens of
+// context: 313 us, 941 TFLOP/s.  (64 rows a wave would halve what LDS delivers, but leave one wave to a SIMD.)
+//
 // PAGES16: 16 keys from a multiple of 16 on are 16 rows that follow each other (no pages, or pages of a multiple of 16 tokens).
 template <int OP, int KH, int KT, int DV, class OUT, bool PAGES16>
 struct Tiled {
@@ -533,7 +528,6 @@ struct Tiled {
     static constexpr int kMinShare = kItemCost + 1;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kTailAt + kKeys * KT * 2;
     static constexpr int kBuf = kVAt + kKeys * DV * 2;
-    typedef uint16_t In;
     typedef OUT Out;
 };
 
@@ -668,18 +662,6 @@ __device__ __forceinline__ f32x16 zeros() {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.0f;
     return x;
-}
-// Order of what stands before it in a block: products, each with `READS` LDS reads for the product `AHEAD` further on beside it.  (Left
-// to itself the compiler saves registers instead and waits for every operand.)
-template <int PRODUCTS, int READS, int AHEAD>
-__device__ __forceinline__ void reads_ahead() {
-    __builtin_amdgcn_sched_group_barrier(0x100, READS * AHEAD, 0);
-#pragma unroll
-    for (int k = 0; k < PRODUCTS - AHEAD; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 // N products in order: product(k, operand k), operands by read(k) AHEAD products before they are needed, and beside(k) in between.  (Left to
 // itself the compiler saves registers and waits for every operand: 36 steps took 6000 cycles instead of 1300.)
@@ -1088,9 +1070,9 @@ __global__ __launch_bounds__(C::kBlockThreads, 2) void tiled_kernel(Args a) {  /
 
 template <class C>
 struct Kernel;
-template <int OP, int KH, int KT, int DV, class IN, class OUT>
-struct Kernel<Simple<OP, KH, KT, DV, IN, OUT>> {
-    static constexpr auto run = simple_kernel<Simple<OP, KH, KT, DV, IN, OUT>>;
+template <int OP, int KH, int KT, int DV>
+struct Kernel<Simple<OP, KH, KT, DV>> {
+    static constexpr auto run = simple_kernel<Simple<OP, KH, KT, DV>>;
 };
 template <int OP, int KH, int KT, int DV, class OUT, bool PAGES16>
 struct Kernel<Tiled<OP, KH, KT, DV, OUT, PAGES16>> {

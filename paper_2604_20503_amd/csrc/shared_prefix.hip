@@ -36,7 +36,7 @@ Layout layout(const fsr_attn_params* p, int& m_cap) {
 
 template <int D>
 int run(const Args& a, const fsr_attn_params* p, void* stream, const char* who) {
-    if (p->dtype == FSR_F32) return launch<Simple<kShared, D, 0, D, float, float>>(a, p->max_workgroups, stream, who);
+    if (p->dtype == FSR_F32) return launch<Simple<kShared, D, 0, D>>(a, p->max_workgroups, stream, who);
     const bool pages16 = p->P % 16 == 0;
     if (p->out_dtype == FSR_F32)
         return pages16 ? launch<Tiled<kShared, D, 0, D, float, true>>(a, p->max_workgroups, stream, who) : launch<Tiled<kShared, D, 0, D, float, false>>(a, p->max_workgroups, stream, who);
