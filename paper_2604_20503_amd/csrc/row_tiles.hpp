@@ -1087,7 +1087,7 @@ struct Source {
 };
 template <class C, class SourceOf>
 __device__ __forceinline__ void join(int pieces, SourceOf source, typename C::Out* out, float* lse, int lane) {
-    constexpr int kColumns = C::kDv / 64, kVector = kColumns < 4 ? kColumns : 4, kVectors = kColumns / kVector, kBatch = kColumns < 4 ? 16 : 8;
+    constexpr int kColumns = C::kDv / 64, kVector = kColumns < 4 ? kColumns : 4, kVectors = kColumns / kVector;
     float o[kColumns], m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int c = 0; c < kColumns; ++c) o[c] = 0.0f;
@@ -1107,28 +1107,32 @@ __device__ __forceinline__ void join(int pieces, SourceOf source, typename C::Ou
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) o[c] *= before;
         const uint32_t lo = (uint32_t)(uintptr_t)mine.sums, hi = (uint32_t)((uintptr_t)mine.sums >> 32);
-        // (Batches by hand: left to itself the compiler fetches one piece, waits and fetches the next.  8000 keys, 128 heads, 126 pieces: 91 us, not 42.)
-#pragma unroll 1
-        for (int k0 = 0; k0 < n; k0 += kBatch) {
-            float y[kBatch][kColumns];
+        // The sums of `many` pieces at once.  (Left to itself the compiler fetches one piece, waits and fetches the next.  8000 keys, 128 heads,
+        // 126 pieces: 91 us, not 42; eight at once where there are three, the last one again and again, cost a long prompt 30 us, not 20.)
+        auto add = [&](int k0, auto many) __attribute__((always_inline)) {
+            float y[many.value][kColumns];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const int k = min(k0 + i, n - 1);
-                const uintptr_t at = ((uintptr_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, k) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, k);
+            for (int i = 0; i < many.value; ++i) {
+                const uintptr_t at = ((uintptr_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, k0 + i) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)lo, k0 + i);
                 typedef const __attribute__((address_space(1))) char global_char;
                 global_char* x = (global_char*)at;
 #pragma unroll
                 for (int v = 0; v < kVectors; ++v) __builtin_memcpy(y[i] + v * kVector, x + (v * 64 * kVector + lane * kVector) * 4, kVector * 4);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                if (i == 0) __builtin_amdgcn_sched_barrier(0);
-                const bool in = k0 + i < n;  // (else the last piece once more: sums that are not finite must not meet a zero)
-                const float wk = in ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(k0 + i, n - 1))) : 0.0f;
+            for (int i = 0; i < many.value; ++i) {
+                const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), k0 + i));
 #pragma unroll
-                for (int c = 0; c < kColumns; ++c) o[c] = fmaf(wk, in ? y[i][c] : 0.0f, o[c]);
+                for (int c = 0; c < kColumns; ++c) o[c] = fmaf(wk, y[i][c], o[c]);
             }
-        }
+        };
+        int k = 0;
+#pragma unroll 1
+        for (; n - k >= 8; k += 8) add(k, std::integral_constant<int, 8>());
+        if (n - k >= 4) add(k, std::integral_constant<int, 4>()), k += 4;
+        if (n - k >= 2) add(k, std::integral_constant<int, 2>()), k += 2;
+        if (n - k >= 1) add(k, std::integral_constant<int, 1>());
     }
     const float inv = inverse(l);
 #pragma unroll
