@@ -365,6 +365,8 @@ __device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_t
 // Products in fp32: every wave takes 16 rows of the tile, with operands straight from memory.  S^T = K Q^T and O^T = V^T P^T
 // on v_mfma_f32_16x16x4_f32; the accumulator layout of S^T (lane: keys 4 (lane / 16) + e, row lane % 16) is the operand
 // layout of P^T if step e of the second product takes keys 4 g + e of lane group g.
+// Bound by latency where calls are short: 8 requests behind 437 common keys take 11 us and 5 to join; at 16 rows a wave every wave fetches
+// its keys for itself, which the caches serve.
 // ---------------------------------------------------------------------------------------------------------------
 template <int OP, int KH, int KT, int DV>
 struct Simple {
@@ -513,7 +515,7 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
 // What bounds it: each of the four waves reads all keys and values of a tile, 128 KB with heads of 128 (160 KB with a second part of 64)
 // and 32 KB (40) to write, 1280 (1600) cycles of a compute unit's LDS against 1024 (1280) of its matrix cores and 900 of exponentials
 // and conversions.  Measured: 1775 cycles a tile where two workgroups share a unit; 2048 rows of 32 heads behind 6000 tokens of
-// context: 313 us, 941 TFLOP/s.  (64 rows a wave would halve what LDS delivers, but leave one wave to a SIMD.)
+// context: 326 us, 906 TFLOP/s (clocks differ: 313 on another card).  (64 rows a wave would halve what LDS delivers, but leave one wave to a SIMD.)
 //
 // PAGES16: 16 keys from a multiple of 16 on are 16 rows that follow each other (no pages, or pages of a multiple of 16 tokens).
 template <int OP, int KH, int KT, int DV, class OUT, bool PAGES16>

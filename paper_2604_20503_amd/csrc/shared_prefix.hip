@@ -3,6 +3,8 @@
 // and 128 packed rows, and their products are matrix-core sized, where request by request every one reads them again.  A
 // request's own tokens behind the prefix are a second sequence of the same launch; the two results of a row are joined by
 // their softmax statistics.
+// Measured: 64 requests of 2-9 rows behind 8192 common tokens and 64-1024 of their own, 32/8 heads of 128: 104 us; 192 requests in 4
+// groups, 64/8 heads: 506 us, 770 TFLOP/s.  Own contexts of few rows cost most for what they are: three of four waves only load.
 #include "row_tiles.hpp"
 
 namespace fsr {
