@@ -117,7 +117,7 @@ int check_attention(const fsr_latent_params* p, const char* who) {
     return FSR_OK;
 }
 
-int rows_cap(const fsr_latent_params* p) { return (int)std::max(1LL, std::min((long long)p->N_cap * p->H, (long long)kTileRows)); }
+int rows_cap(const fsr_latent_params* p) { return (int)std::max(1LL, std::min((long long)p->N_cap * p->H, 64LL)); }  // (both kernels' tiles)
 
 template <int DL, int DR>
 int run(const Args& a, const fsr_latent_params* p, void* stream, const char* who) {

@@ -6,8 +6,8 @@
 // LDS has to deliver per tile, keys once per two waves and values once per two waves, is 370 KB against 2176 cycles of the matrix
 // cores (2900 cycles at 128 bytes each); with 16 rows a wave it would be 626 KB.
 //
-// Measured: 4350 cycles a tile (scores 1660, weights 690, second product 1500, three barriers).  64 requests of 512-4096 keys, 1-4 rows, 128
-// heads: 268 us, 417 TFLOP/s; 32 of 1024-8192 keys, 16 heads: 86 us, 1.9 TB/s.
+// Measured: 4350 cycles a tile whose keys come from the cache (scores 1660, weights 690, second product 1500, three barriers).  64
+// requests of 512-4096 keys, 1-4 rows, 128 heads: 223-240 us, 496-462 TFLOP/s by card; 32 of 1024-8192 keys, 16 heads: 82 us, 2.0 TB/s.
 //
 // The exponent reference of a row has to be common to both waves.  It is kept kAhead powers of two above the largest score seen and
 // changed only in a tile where a score overtakes it, the first one for the most part, with two more barriers.
@@ -22,6 +22,9 @@ template <int KH, int KT, class OUT, bool PAGES16>
 struct Latent {
     static constexpr int kOp = kLatent, kHead = KH, kTail = KT, kDk = KH + KT, kDv = KH;
     static constexpr bool kPair = sizeof(OUT) == 4, kPages16 = PAGES16;
+    // Where row tiles outnumber the workgroups: even pieces in rounds (below), 272 -> 240 us for 64 requests of 128 heads, 418 -> 335 us with
+    // lengths of 100-8000.  Rows of 256 + 32 pass the cache at half the bytes: there the cut line stays, 92 us and not 99.
+    static constexpr bool kEven = KH >= 512;
     static constexpr int kM = 64, kKeys = 64, kBlockThreads = 256, kWaves = 4, kPerUnit = 1, kItemCost = 2, kMinShare = kItemCost + 1;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kBuf = kTailAt + kKeys * KT * 2;
     typedef OUT Out;
@@ -410,7 +413,9 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
 // Even pieces: where a batch has no more row tiles than there are workgroups, every item is cut into pieces of about the same length,
 // as long as makes one piece for each workgroup: half the sums of a cut line, each workgroup takes up one piece, and pieces of the same
 // keys, row tile by row tile, are neighbours (and share a die's cache).  The length is the shortest of 64 candidates, one per lane, from
-// an equal share of all key tiles upwards, for which the pieces do not outnumber the workgroups.  False: the line is cut instead.
+// an equal share of all key tiles upwards, for which the pieces do not outnumber the workgroups.  Where there are more row tiles, every
+// workgroup takes up to kEvenRounds pieces: taking one up costs 38000 cycles (7 tiles), but row tiles of a request that run at different
+// keys read these anew from behind the die's cache, 8000 cycles a tile and not 5300.  False: the line is cut instead.
 constexpr int kEvenRequests = 256;
 struct EvenScratch {
     int tiles[kEvenRequests], row_tiles[kEvenRequests];
@@ -419,7 +424,7 @@ struct EvenScratch {
     int piece[8];
 };
 template <class C>
-__device__ __forceinline__ bool even_piece(const Args& a, int share, EvenScratch& x, Piece& p, bool& mine) {
+__device__ __forceinline__ bool even_piece(const Args& a, int share, EvenScratch& x, Piece& p, bool& mine, int& rounds) {
     static_assert(C::kBlockThreads == kEvenRequests && C::kWaves == 4, "a request per thread");
     if (a.B > kEvenRequests) return false;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -439,12 +444,14 @@ __device__ __forceinline__ bool even_piece(const Args& a, int share, EvenScratch
     }
     __syncthreads();
     const int n_items = uniform((x.sums[4] + x.sums[5]) + (x.sums[6] + x.sums[7]));
-    if (n_items > a.nb || n_items == 0) return false;
+    const int most = n_items <= a.nb ? a.nb : a.even_cap;  // pieces
+    if (n_items > most || n_items == 0) return false;
+    rounds = most == a.nb ? 1 : kEvenRounds;
     const int n_tiles = uniform((x.sums[0] + x.sums[1]) + (x.sums[2] + x.sums[3]));
     // Where workgroups are plenty: a tile more of a piece takes 2 us, a piece more of a join a sixth of that.  Length l of t tiles costs
     // 2 l + t / 3 l, least at sqrt(t / 6).  (8000 keys, 16 heads: 69 us in 126 pieces of one tile, 47 us in 27.)
     const int cheapest = (int)(__builtin_amdgcn_sqrtf((float)n_tiles * __builtin_amdgcn_rcpf(6.0f * n_items)) + 0.5f);
-    const int shortest = max(max(cheapest, 1), ceil_div(n_tiles, a.nb));
+    const int shortest = max(max(cheapest, 1), ceil_div(n_tiles, most));
     const int length = lane == 63 ? 1 << 24 : shortest + ((shortest * lane + 15) >> 4);
     const float inv = 1.0f / (float)length;
     auto pieces_of = [&](int tiles, int length, float inv) {  // ceil(tiles / length), at least 1
@@ -458,7 +465,7 @@ __device__ __forceinline__ bool even_piece(const Args& a, int share, EvenScratch
     x.counts[wave][lane] = count;
     __syncthreads();
     count = (x.counts[0][lane] + x.counts[1][lane]) + (x.counts[2][lane] + x.counts[3][lane]);
-    const int pick = __ffsll((unsigned long long)__ballot(count <= a.nb)) - 1;  // (lane 63 cuts nothing)
+    const int pick = __ffsll((unsigned long long)__ballot(count <= most)) - 1;  // (lane 63 cuts nothing)
     const int chosen = __builtin_amdgcn_readlane(length, pick);
     if (chosen > shortest + (shortest >> 2) + 3) return false;  // lengths too uneven for that
     const int pieces = nrt ? pieces_of(nk, chosen, 1.0f / (float)chosen) : 0;
@@ -501,12 +508,12 @@ __device__ __forceinline__ bool even_piece(const Args& a, int share, EvenScratch
     p.t0 = which * each + min(which, longer);
     p.t1 = p.t0 + each + (which < longer);
     p.whole = p.pieces == 1;
-    p.slot = 2 * share;
+    p.slot = share;
     p.share0 = share;
     if (tid == 0) {
         const bool first = which == 0 && !p.whole;
         desc[1] = p.q.row0; desc[2] = 0; desc[3] = p.rt; desc[4] = min(p.q.rows * a.G - p.rt * C::kM, C::kM);
-        desc[5] = p.slot; desc[6] = p.slot + 2 * tiles_of_rows; desc[7] = 2 * tiles_of_rows;
+        desc[5] = p.slot; desc[6] = p.slot + tiles_of_rows; desc[7] = tiles_of_rows;
         desc[0] = first ? p.pieces : 0;
     }
     return true;
@@ -520,12 +527,19 @@ __global__ __launch_bounds__(C::kBlockThreads, 1) void latent_kernel(Args a) {
     const int share = share_of_block(blockIdx.x, a.nb);
     Piece p;
     Walk<C> walk;
-    bool more = false;
-    const bool even = even_piece<C>(a, share, *reinterpret_cast<EvenScratch*>(buf1), p, more);
-    if (!even) walk.begin(a, share, find_share<C>(a, share, reinterpret_cast<long long*>(buf0)));
-    while (even ? more : walk.next(a, share, p)) {
-        run_latent<C>(a, p, buf0, buf1, sh);
-        more = false;
+    bool more = false, even = true;
+    int round = 0, rounds = 1;
+    if (threadIdx.x == 0)
+        for (int k = share + a.nb; k < a.even_cap; k += a.nb) a.desc[(size_t)k * kDescInts] = 0;
+    for (;;) {
+        if (even) {
+            __syncthreads();  // nobody reads the buffers any more
+            even = even_piece<C>(a, share + round * a.nb, *reinterpret_cast<EvenScratch*>(buf1), p, more, rounds);
+            if (!even) walk.begin(a, share, find_share<C>(a, share, reinterpret_cast<long long*>(buf0)));
+        }
+        if (!even) more = walk.next(a, share, p);
+        if (more) run_latent<C>(a, p, buf0, buf1, sh);
+        if (even ? ++round == rounds : !more) break;
     }
 }
 template <int KH, int KT, class OUT, bool PAGES16>

@@ -38,6 +38,7 @@ constexpr int kDescInts = 8;       // merge descriptor of a share
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kSharesCap = 512;
+constexpr int kEvenRounds = 3;       // latent: most pieces of a workgroup in a batch that is cut evenly
 constexpr int kRefPlace = 10, kRefPrefix = 1 << 24;  // fields of a reference to a part of a row: its place in the tile; there is a prefix before it
 constexpr float kAhead = 40.0f;    // distance of a row's exponent reference from its largest score, in powers of two
 
@@ -63,9 +64,10 @@ struct Args {
     long long head_hk, v_hk;                // bytes from a stream head to the next
     float scale, scale_log2;  // softmax scale, and times log2(e)
     int nb, shares_cap, min_share, m_cap;
+    int even_cap;     // latent: most pieces of a batch that is cut evenly
     float* part_o;    // [2 * shares_cap][m_cap][D_v]
     float* part_ml;   // [2 * shares_cap][m_cap][2] score that the weights refer to, sum
-    int32_t* desc;    // [shares_cap][kDescInts]
+    int32_t* desc;    // [2 * shares_cap][kDescInts]
     float* row_o;     // shared: [2][N_cap * H][D_v] sums of items that are whole: prefix, own
     float* row_ml;    // shared: [2][N_cap * H][2]
     int32_t* refs;    // shared: [2][N_cap * H][2] pieces of the item (0: in row_o; -1: done); its first share, the row's place in its tile, kRefPrefix
@@ -373,6 +375,7 @@ struct Simple {
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
     static constexpr int kM = 64, kKeys = 32, kBlockThreads = kThreads, kPerUnit = 1;  // (kPerUnit: workgroups of a compute unit)
     static constexpr int kItemCost = 2;  // key tiles that taking up an item is worth (measured: 14000 cycles against 7000)
+    static constexpr bool kEven = false; // (even pieces)
     static constexpr int kMinShare = 1;  // units of a share of a short line: a tile of its own costs less than waiting for a neighbour's
     typedef float Out;
 };
@@ -528,6 +531,7 @@ struct Tiled {
     static constexpr int kPerUnit = 2;                // workgroups of a compute unit, two waves to a SIMD
     static constexpr int kItemCost = 5;  // measured: 20000 cycles (loads that nothing hides, tiles with masked keys, sums on their way out) against 4000 a tile
     static constexpr int kMinShare = kItemCost + 1;
+    static constexpr bool kEven = false;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kTailAt + kKeys * KT * 2;
     static constexpr int kBuf = kVAt + kKeys * DV * 2;
     typedef OUT Out;
@@ -1207,7 +1211,7 @@ inline Layout layout_of(int m_cap, int dv, long long rows, bool shared) {
     auto take = [&](size_t bytes) { const size_t p = at; at += align_up(bytes, 256); return p; };
     l.part_o = take((size_t)2 * kSharesCap * m_cap * dv * sizeof(float));
     l.part_ml = take((size_t)2 * kSharesCap * m_cap * 2 * sizeof(float));
-    l.desc = take((size_t)kSharesCap * kDescInts * sizeof(int32_t));
+    l.desc = take((size_t)2 * kSharesCap * kDescInts * sizeof(int32_t));
     if (shared) {
         l.row_o = take((size_t)2 * rows * dv * sizeof(float));
         l.row_ml = take((size_t)2 * rows * 2 * sizeof(float));
@@ -1254,6 +1258,9 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
     if (max_workgroups > 0) nb = std::min(nb, max_workgroups * C::kPerUnit);
     a.nb = std::min(nb, kSharesCap);
     a.min_share = C::kMinShare;
+    a.even_cap = a.nb;
+    // Items that may outnumber the workgroups are cut into pieces for several rounds.  (Else that many descriptors need not be looked at.)
+    if (C::kEven && kEvenRounds * a.nb <= 2 * kSharesCap && ((long long)a.N_cap * a.G + C::kM - 1) / C::kM + a.B > a.nb) a.even_cap = kEvenRounds * a.nb;
     hipStream_t s = (hipStream_t)stream;
     hipLaunchKernelGGL((Kernel<C>::run), dim3(a.nb), dim3(C::kBlockThreads), 0, s, a);
     int rc = check_launch(who);
@@ -1263,7 +1270,7 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
         hipLaunchKernelGGL((join_rows_kernel<C>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
     } else {
         // 16 workgroups a share: one row a wave of a latent tile, two of a tile of heads; with 32 there the launching of workgroups took longer: 20 us, not 17.6
-        hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.nb, std::min(16, (a.m_cap + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.even_cap, std::min(16, (a.m_cap + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
     }
     return check_launch(who);
 }

@@ -56,3 +56,12 @@ def test_expanded(fsr, rows, keys, dtype, out_dtype):
     b = expanded.Batch(1, rows, keys, 2, expanded.BIG, dtype)
     need = fsr.expanded_workspace_bytes(N_cap=b.q.shape[0], H=2, D_nope=128, D_rope=64, D_v=128, dtype=dtype, out_dtype=out_dtype)
     b.compare("used workspace", same_for_all(need, lambda ws: b.run(fsr, out_dtype, workspace=ws)))
+
+
+@pytest.mark.parametrize("rows,ctx", [([8, 7, 8, 8, 6, 8, 8, 7, 8, 8, 8, 8, 8, 5, 8, 8, 8, 8, 1, 8], range(5, 405, 20)), ([200], [70]), ([1] * 250 + [9], [3] * 250 + [300])])
+def test_more_row_tiles_than_workgroups(fsr, rows, ctx):
+    """Pieces in several rounds, a request of many row tiles, more requests than fit one round."""
+    announce(f"latent attention, row tiles in rounds: {rows} {list(ctx)}")
+    b = latent.Batch(2, list(ctx), rows, 128, 512, 64, 16, BF)
+    need = fsr.latent_workspace_bytes(N_cap=b.N, H=128, D_latent=512, D_rope=64, dtype=BF, out_dtype=BF)
+    latent.compare("rounds", b, same_for_all(need, lambda ws: latent.run(fsr, b, BF, workspace=ws)))
