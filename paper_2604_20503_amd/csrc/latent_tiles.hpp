@@ -88,7 +88,10 @@ struct LatentShared {     // what the waves of a workgroup tell each other
     uint16_t p[64][64];   // weights [row][key], 16-byte chunks of a row permuted
     float top[4][32];     // largest score of a row among a wave's keys; at the end its sum of weights
     float m[2][32];       // at the end: the scores that the rows' weights refer to
-    int flags[4];         // by wave: 1: a score is ahead of its reference, 2: scores that are not finite among masked ones
+    // By wave.  A tile that take_tile gives up is taken by take_any_tile without a barrier between: another wave may still be reading `ahead`
+    // when this one writes again, so that each has flags of its own.
+    int ahead[4];         // take_tile: a score is ahead of its reference
+    int odd[4];           // take_any_tile: scores that are not finite
 };
 
 template <class C>
@@ -224,9 +227,9 @@ __device__ __forceinline__ bool take_tile(LatentRows<C>& w, const char* buf, Lat
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) beside(i);
     }
-    if (lane == 0) sh.flags[wave] = ahead;
+    if (lane == 0) sh.ahead[wave] = ahead;
     lds_barrier();
-    if (uniform(sh.flags[0] | sh.flags[1] | sh.flags[2] | sh.flags[3])) return true;
+    if (uniform(sh.ahead[0] | sh.ahead[1] | sh.ahead[2] | sh.ahead[3])) return true;
     if (live) {
         w.l += sum;
         second_product<C>(w, buf, p);
@@ -263,9 +266,9 @@ __device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf,
         top = largest(z) * scale_log2;
     }
     if (h == 0) sh.top[wave][li] = top;
-    if (lane == 0) sh.flags[wave] = odd_scores;
+    if (lane == 0) sh.odd[wave] = odd_scores;
     lds_barrier();
-    const bool careful = uniform(sh.flags[wave & 2] | sh.flags[wave | 1]);
+    const bool careful = uniform(sh.odd[wave & 2] | sh.odd[wave | 1]);
     if (live) {
         const float both = fmaxf(sh.top[wave & 2][li], sh.top[wave | 1][li]), old = w.m;
         if (both > old) w.m = both + kAhead;
