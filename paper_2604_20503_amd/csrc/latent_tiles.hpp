@@ -86,12 +86,13 @@ struct LatentLoads {
 
 struct LatentShared {     // what the waves of a workgroup tell each other
     uint16_t p[64][64];   // weights [row][key], 16-byte chunks of a row permuted
-    float top[4][32];     // largest score of a row among a wave's keys; at the end its sum of weights
-    float m[2][32];       // at the end: the scores that the rows' weights refer to
+    float top[4][32];     // largest product of a row among a wave's keys; at the end its sum of weights
+    Reference of[2][32];  // at the end: what the rows' weights refer to
     // By wave.  A tile that take_tile gives up is taken by take_any_tile without a barrier between: another wave may still be reading `ahead`
     // when this one writes again, so that each has flags of its own.
     int ahead[4];         // take_tile: a score is ahead of its reference
     int odd[4];           // take_any_tile: scores that are not finite
+    int far[4];           // take_any_tile: references that are no powers of two
 };
 
 template <class C>
@@ -99,7 +100,8 @@ struct LatentRows {
     static constexpr int kHeadSteps = C::kHead / 16, kTailSteps = C::kTail / 16, kBlocks = C::kDv / 64;  // (half the columns)
     bf16x8 q[kHeadSteps + kTailSteps];
     f32x16 acc[kBlocks];
-    float m, l;
+    Reference of;
+    float l;
     int seen;
     int k_at[8], tail_at[kTailSteps], v_at[4], p_write[4], p_read[4];
 
@@ -205,8 +207,8 @@ __device__ __forceinline__ void second_product_carefully(LatentRows<C>& w, const
     }
 }
 
-// A tile of 64 keys that every row sees whole.  True: a score is ahead of its row's reference, and nothing has been added.  All waves
-// pass the same barriers; those without rows (not `live`) do no more.
+// A tile of 64 keys that every row sees whole, by references in powers of two.  True: a score is ahead of its row's reference, and nothing
+// has been added.  All waves pass the same barriers; those without rows (not `live`) do no more.
 // beside(i) issues the wave's load i of the next tile: between the products, whose issue leaves time for it.
 template <class C, class Beside>
 __device__ __forceinline__ bool take_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, bool live, float scale_log2, int lane, int wave, Beside beside) {
@@ -220,8 +222,8 @@ __device__ __forceinline__ bool take_tile(LatentRows<C>& w, const char* buf, Lat
         z = scores_of<C>(w, buf, [&](int s) __attribute__((always_inline)) {
             if (s % 2 == 0 && s / 2 < kLoads) beside(s / 2);
         });
-        ahead = __any(largest(z) * scale_log2 > w.m);
-        sum = weights_of(z, w.m, scale_log2);
+        ahead = __any(largest(z) * scale_log2 > w.of.log2);
+        sum = weights_of(z, Reference{0.0f, w.of.log2}, scale_log2);
         write_weights<C>(w, p, z);
     } else {
 #pragma unroll
@@ -246,9 +248,10 @@ __device__ __forceinline__ bool take_tile(LatentRows<C>& w, const char* buf, Lat
     return false;
 }
 
-// Any tile: some keys may be masked, references move if they have to.  (Rows that see none of its keys give zero weights.)
+// Any tile: some keys may be masked, references move if they have to.  (Rows that see none of its keys give zero weights.)  True: all of the
+// workgroup's references are powers of two.
 template <class C>
-__device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, int key0, bool live, float scale_log2, int lane, int wave) {
+__device__ __forceinline__ bool take_any_tile(LatentRows<C>& w, const char* buf, LatentShared& sh, int key0, bool live, float scale_log2, int lane, int wave) {
     const int li = lane & 31, h = lane >> 5, part = wave & 1;
     char* p = reinterpret_cast<char*>(sh.p);
     f32x16 z;
@@ -263,25 +266,30 @@ __device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf,
             z[e] = key0 + 32 * part + 8 * (e >> 2) + 4 * h + (e & 3) <= w.seen ? z[e] : -INFINITY;
         }
         odd_scores = __any(odd != 0.0f);
-        top = largest(z) * scale_log2;
+        top = largest(z);
     }
     if (h == 0) sh.top[wave][li] = top;
     if (lane == 0) sh.odd[wave] = odd_scores;
     lds_barrier();
     const bool careful = uniform(sh.odd[wave & 2] | sh.odd[wave | 1]);
     if (live) {
-        const float both = fmaxf(sh.top[wave & 2][li], sh.top[wave | 1][li]), old = w.m;
-        if (both > old) w.m = both + kAhead;
-        if (__any(both > old && old > -INFINITY)) {
-            const float alpha = w.m == -INFINITY || old == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(old - w.m);
+        const float both = fmaxf(sh.top[wave & 2][li], sh.top[wave | 1][li]);
+        const Reference old = w.of;
+        const bool ahead = exponent(both, old, scale_log2) > 0.0f, moved = ahead && old.log2 > -INFINITY;
+        if (ahead) w.of = reference_for(both, scale_log2);
+        if (__any(moved)) {
+            const float alpha = moved ? __builtin_amdgcn_exp2f(distance(old, w.of, scale_log2)) : 1.0f;
             w.l *= alpha;
 #pragma unroll
             for (int b = 0; b < LatentRows<C>::kBlocks; ++b) change_sums(w.acc[b], [&](float x, int) { return x * alpha; });
         }
-        w.l += weights_of(z, w.m, scale_log2);
+        w.l += weights_of(z, w.of, scale_log2);
         write_weights<C>(w, p, z);
     }
+    const int far = live && __any(w.of.raw != 0.0f);
+    if (lane == 0) sh.far[wave] = far;
     lds_barrier();
+    const bool near = !uniform(sh.far[0] | sh.far[1] | sh.far[2] | sh.far[3]);
     if (live) {
         if (careful) second_product_carefully<C>(w, buf, p);
         else second_product<C>(w, buf, p);
@@ -298,6 +306,7 @@ __device__ __forceinline__ void take_any_tile(LatentRows<C>& w, const char* buf,
             else second_product<C>(w, buf, p);
         }
     }
+    return near;
 }
 
 template <class C>
@@ -307,7 +316,7 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
     const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + (wave >> 1) * 32;
     const bool live = first < n_packed;  // a wave without rows helps to load
     R w;
-    w.m = -INFINITY;
+    w.of = Reference{0.0f, -INFINITY};
     w.l = 0.0f;
     w.seen = -1;
     w.place_operands(lane, wave >> 1, part);
@@ -366,22 +375,24 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
             load_all(odd ? buf0 : buf1);
         }
         loaded = false;
-        take_any_tile<C>(w, odd ? buf1 : buf0, sh, p.q.k_begin + t * C::kKeys, live, a.scale_log2, lane, wave);
+        const bool near = take_any_tile<C>(w, odd ? buf1 : buf0, sh, p.q.k_begin + t * C::kKeys, live, a.scale_log2, lane, wave);
         ++t;
         // all the others: here the sums are the matrix instructions' alone, and stay in the accumulation registers
-        if (!odd)
+        if (!odd && near) {
+            w.of.raw = 0.0f;  // (known, and in no register of the loop)
             while (whole()) {
                 if (!step(buf1, buf0)) { loaded = true; break; }
                 if (!whole()) break;
                 if (!step(buf0, buf1)) { loaded = true; break; }
             }
+        }
     }
     // The sums leave by way of LDS, row by row: from the accumulators a store would touch 32 rows.  (16-byte chunks permuted by row, so
     // that eight rows' writes of one column reach all banks.)
     w.l += other_half(w.l);
     arrive();  // (the load too many has its place until it has come)
     if (h == 0) sh.top[wave][li] = w.l;
-    if (h == 0 && part == 0) sh.m[wave >> 1][li] = w.m * kLn2;
+    if (h == 0 && part == 0) sh.of[wave >> 1][li] = w.of;
     constexpr int kRowBytes = C::kDv * 4;
     static_assert(32 * kRowBytes <= C::kBuf, "32 rows' sums fit into a buffer");
     auto place = [&](int row, int chunk) { return (row < 32 ? buf0 : buf1) + (row & 31) * kRowBytes + ((chunk ^ (row & 7)) << 4); };
@@ -396,7 +407,8 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
     const size_t row0 = (size_t)p.q.row0 * a.H + p.rt * C::kM, slot0 = (size_t)p.slot * a.m_cap;  // (a request's rows follow each other)
 #pragma unroll 1
     for (int r = wave; r < rows; r += C::kWaves) {
-        const float l = sh.top[r >> 5 << 1][r & 31] + sh.top[(r >> 5 << 1) | 1][r & 31], m = sh.m[r >> 5][r & 31];
+        const float l = sh.top[r >> 5 << 1][r & 31] + sh.top[(r >> 5 << 1) | 1][r & 31];
+        const Reference of = sh.of[r >> 5][r & 31];
         f32x4 x[C::kDv / 256];
 #pragma unroll
         for (int k = 0; k < C::kDv / 256; ++k) x[k] = *reinterpret_cast<const f32x4*>(place(r, k * 64 + lane));
@@ -404,11 +416,11 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
             const float inv = inverse(l);
 #pragma unroll
             for (int k = 0; k < C::kDv / 256; ++k) store4((typename C::Out*)a.out + (row0 + r) * C::kDv + 4 * (k * 64 + lane), x[k] * inv);
-            if (lane == 0 && a.lse) a.lse[row0 + r] = log_sum(m, l);
+            if (lane == 0 && a.lse) a.lse[row0 + r] = log_sum(of, l, a.scale);
         } else {
 #pragma unroll
             for (int k = 0; k < C::kDv / 256; ++k) store4(a.part_o + (slot0 + r) * C::kDv + 4 * (k * 64 + lane), x[k]);
-            if (lane < 2) a.part_ml[2 * (slot0 + r) + lane] = lane ? l : m;
+            if (lane == 0) store4(a.part_ml + 4 * (slot0 + r), f32x4{of.raw, of.log2, l, 0.0f});
         }
     }
 }

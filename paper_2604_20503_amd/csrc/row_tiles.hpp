@@ -66,10 +66,10 @@ struct Args {
     int nb, shares_cap, min_share, m_cap;
     int even_cap;     // latent: most pieces of a batch that is cut evenly
     float* part_o;    // [2 * shares_cap][m_cap][D_v]
-    float* part_ml;   // [2 * shares_cap][m_cap][2] score that the weights refer to, sum
+    float* part_ml;   // [2 * shares_cap][m_cap][4] what the weights refer to (a Reference), their sum
     int32_t* desc;    // [2 * shares_cap][kDescInts]
     float* row_o;     // shared: [2][N_cap * H][D_v] sums of items that are whole: prefix, own
-    float* row_ml;    // shared: [2][N_cap * H][2]
+    float* row_ml;    // shared: [2][N_cap * H][4]
     int32_t* refs;    // shared: [2][N_cap * H][2] pieces of the item (0: in row_o; -1: done); its first share, the row's place in its tile, kRefPrefix
 };
 
@@ -305,8 +305,26 @@ __device__ __forceinline__ void store4(uint16_t* p, f32x4 x) {
     *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
 }
 
-// Logarithm of exp(m) * l, -inf without any weight.
-__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2; }
+// What a row's weights refer to: product z weighs 2^((z - raw) * scale_log2 - log2).  One of the two numbers would do, were they exact.  In
+// powers of two (raw = 0) the exponent is one fma a score, but a reference beyond 2^27 is rounded by more than it is kept ahead: weights would
+// overflow, or vanish for a whole row.  There the reference is a product, from which differences are as exact as the products themselves, also
+// where their multiples by the scale are beyond fp32.
+struct Reference {
+    float raw, log2;
+};
+constexpr float kNear = 134217728.0f;  // 2^27, where a reference's rounding is half a step of 8, and so is its largest score's
+__device__ __forceinline__ float exponent(float z, Reference of, float scale_log2) { return fmaf(z - of.raw, scale_log2, -of.log2); }
+__device__ __forceinline__ float distance(Reference x, Reference y, float scale_log2) { return fmaf(x.raw - y.raw, scale_log2, x.log2 - y.log2); }  // powers of two
+// For a row whose largest product is `top`.
+__device__ __forceinline__ Reference reference_for(float top, float scale_log2) {
+    const float score = top * scale_log2;
+    return fabsf(score) <= kNear ? Reference{0.0f, score + kAhead} : Reference{top, kAhead};
+}
+
+// Logarithm of the sum of exp of the scores whose weights add up to l, -inf without any weight.
+__device__ __forceinline__ float log_sum(Reference of, float l, float scale) {
+    return l == 0.0f ? -INFINITY : fmaf(of.raw, scale, of.log2 * kLn2) + __builtin_amdgcn_logf(l) * kLn2;
+}
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
 // Where the result of a row's share of the keys goes.
@@ -314,7 +332,7 @@ template <class C>
 struct Target {
     typename C::Out* out;  // the result (kDv values and, if wanted, lse), or
     float* lse;
-    float* sums;           // the sums of weighted values, not divided, with the score that the weights refer to and their sum
+    float* sums;           // the sums of weighted values, not divided, with what the weights refer to and their sum
     float* ml;
 };
 // For row r_tile of the piece; `first_lane` says (in a batch behind prefixes) where the row's parts are to be found.
@@ -339,27 +357,24 @@ __device__ __forceinline__ Target<C> target_of(const Args& a, const Piece& p, in
     }
     if (p.whole) {
         const size_t n = (size_t)a.N_cap * a.H, k = prefix ? row : n + row;
-        return Target<C>{nullptr, nullptr, a.row_o + k * C::kDv, a.row_ml + k * 2};
+        return Target<C>{nullptr, nullptr, a.row_o + k * C::kDv, a.row_ml + k * 4};
     }
     const size_t k = (size_t)p.slot * a.m_cap + r_tile;
-    return Target<C>{nullptr, nullptr, a.part_o + k * C::kDv, a.part_ml + k * 2};
+    return Target<C>{nullptr, nullptr, a.part_o + k * C::kDv, a.part_ml + k * 4};
 }
 
-// Result of a row's share of the keys: sums o[4] at columns d .. d + 3 (called for all of the lane's columns), the score m that the
-// weights refer to (-inf: no key), their sum l.
+// Result of a row's share of the keys: sums o[4] at columns d .. d + 3 (called for all of the lane's columns), what the weights refer to
+// (-inf: no key), their sum l.
 template <class C, class ForEach4>
-__device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_tile, bool first_lane, float m, float l, ForEach4 each) {
+__device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_tile, bool first_lane, Reference of, float l, ForEach4 each) {
     const Target<C> to = target_of<C>(a, p, r_tile, first_lane);
     if (to.out) {
         const float inv = inverse(l);
         each([&](int d, f32x4 x) { store4(to.out + d, x * inv); });
-        if (first_lane && to.lse) *to.lse = log_sum(m, l);
+        if (first_lane && to.lse) *to.lse = log_sum(of, l, a.scale);
     } else {
         each([&](int d, f32x4 x) { store4(to.sums + d, x); });
-        if (first_lane) {
-            to.ml[0] = m;
-            to.ml[1] = l;
-        }
+        if (first_lane) store4(to.ml, f32x4{of.raw, of.log2, l, 0.0f});
     }
 }
 
@@ -496,7 +511,7 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
     if (first + li < n_packed)
-        hand_over<C>(a, p, wave * 16 + li, lg == 0, m * a.scale, l, [&](auto put) {
+        hand_over<C>(a, p, wave * 16 + li, lg == 0, Reference{m, 0.0f}, l, [&](auto put) {
 #pragma unroll
             for (int b = 0; b < C::kDv / 16; ++b) put(16 * b + 4 * lg, acc[b]);
         });
@@ -712,7 +727,8 @@ struct Rows {
     static constexpr int kOwnK = std::min(kHeadSteps, 8), kOwnV = std::min(kBlocks, 4);
     bf16x8 q[kHeadSteps + kTailSteps];
     f32x16 acc[kBlocks];
-    float m, l;          // exponent reference (times log2(e)), sum of this lane's weights
+    Reference of;        // of the row's weights
+    float l;             // sum of this lane's weights
     int seen;            // last key of the lane's row
     int k_at[kOwnK], tail_at[std::max(kTailSteps, 1)], v_at[kOwnV];
 
@@ -740,11 +756,11 @@ __device__ __forceinline__ float largest(const f32x16& z) {
     for (int e = 2; e < 16; ++e) top = fmaxf(top, z[e]);
     return fmaxf(top, other_half(top));
 }
-// Weights of the scores; their sum.
-__device__ __forceinline__ float weights_of(f32x16& z, float m, float scale_log2) {
-    const float use = m == -INFINITY ? 0.0f : m;
+// Weights of the scores; their sum.  (Where nothing has been seen, the reference is -inf, and so are the scores.)
+__device__ __forceinline__ float weights_of(f32x16& z, Reference of, float scale_log2) {
+    const Reference use{of.raw, of.log2 == -INFINITY ? 0.0f : of.log2};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], scale_log2, -use));
+    for (int e = 0; e < 16; ++e) z[e] = __builtin_amdgcn_exp2f(exponent(z[e], use, scale_log2));
     return sum_of(z);
 }
 // Eight weights as an operand.
@@ -794,14 +810,15 @@ __device__ __forceinline__ float largest_of_lane(const f32x16& z) {
     return top;
 }
 
-// A tile of 64 keys that every row of the wave sees whole.  True: a score is ahead of its row's reference, and nothing has been added.
+// A tile of 64 keys that every row of the wave sees whole, by references in powers of two.  True: a score is ahead of its row's reference, and
+// nothing has been added.
 // The weights of a half are computed beside the products of the other: a product takes 32 cycles, in which eight instructions can be issued.
 template <class C, class Beside>
 __device__ __forceinline__ bool take_tile(Rows<C>& w, const char* buf, float scale_log2, Beside beside) {
     typedef Rows<C> R;
     typedef Weights<C::kPair> W;
     constexpr int kSteps = R::kHeadSteps + R::kTailSteps, kProducts = 2 * R::kBlocks;
-    const float use = w.m == -INFINITY ? 0.0f : w.m;
+    const float use = w.of.log2 == -INFINITY ? 0.0f : w.of.log2;
     W x0, x1;
     const f32x16 z0 = scores_of<C>(w, buf, 0, [&](int s) __attribute__((always_inline)) { beside(s); });
     float top = -INFINITY;
@@ -810,7 +827,7 @@ __device__ __forceinline__ bool take_tile(Rows<C>& w, const char* buf, float sca
         if (s == 0) top = largest_of_lane(z0);
         x0.take_part(s, kSteps, z0, use, scale_log2);
     });
-    if (__any(fmaxf(top, largest_of_lane(z1)) * scale_log2 > w.m)) return true;
+    if (__any(fmaxf(top, largest_of_lane(z1)) * scale_log2 > w.of.log2)) return true;
     __builtin_amdgcn_s_setprio(1);  // the wave beside this one on the SIMD, at its scores or weights, gives way: 4 % of a long prompt's time
     auto add = [&](int block, const W& x, auto between) __attribute__((always_inline)) {
         in_turn<kProducts, 6, s16x8>([&](int k) __attribute__((always_inline)) { return values_of<C>(w, buf, block, k / R::kBlocks, k % R::kBlocks); },
@@ -839,18 +856,19 @@ __device__ __forceinline__ void take_any_keys(Rows<C>& w, const char* buf, int b
         const int key = key0 + 8 * (e >> 2) + 4 * h + (e & 3);
         z[e] = key >= k_first && key <= w.seen ? z[e] : -INFINITY;
     }
-    const float top = largest(z) * scale_log2;
+    const float top = largest(z);
     // The reference keeps a distance above the largest score and is moved only when a score overtakes it: weights stay below one,
     // lose nothing (they are floating-point numbers) and the accumulators are rescaled a few times per row, not per tile.
-    if (__any(top > w.m)) {
-        const float m = top > w.m ? top + kAhead : w.m;
-        const float alpha = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(w.m - m);
-        w.m = m;
+    const bool ahead = exponent(top, w.of, scale_log2) > 0.0f;
+    if (__any(ahead)) {
+        const Reference old = w.of;
+        if (ahead) w.of = reference_for(top, scale_log2);
+        const float alpha = !ahead || old.log2 == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(distance(old, w.of, scale_log2));
         w.l *= alpha;
 #pragma unroll
         for (int b = 0; b < R::kBlocks; ++b) w.acc[b] *= alpha;
     }
-    w.l += weights_of(z, w.m, scale_log2);
+    w.l += weights_of(z, w.of, scale_log2);
     bf16x8 hi[2], lo[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) hi[s] = operand_of(z, s);
@@ -884,7 +902,7 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
     const bool active = first < n_packed;  // a wave without rows helps to load
     typedef Rows<C> R;
     R w;
-    w.m = -INFINITY;
+    w.of = Reference{0.0f, -INFINITY};
     w.l = 0.0f;
     w.seen = -1;
     w.place_operands(lane);
@@ -946,18 +964,22 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
             ++t;
             // all the others: here the sums are the products' alone (where something else may touch them, the compiler makes a second
             // set and copies them in every tile)
-            if (!odd)
+            // (Said to be one value for the wave: otherwise the loop saves masks around itself, 13 moves a tile, 2 % of a long prompt.)
+            const bool near = uniform((int)__any(w.of.raw != 0.0f)) == 0;
+            if (!odd && near) {
+                w.of.raw = 0.0f;  // (known, and in no register of the loop)
                 while (whole()) {
                     if (!step(buf1, buf0)) { loaded = true; break; }
                     if (!whole()) break;
                     if (!step(buf0, buf1)) { loaded = true; break; }
                 }
+            }
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);  // the load too many has its place until it has come
     }
     w.l += other_half(w.l);
     if (active && first + li < n_packed)
-        hand_over<C>(a, p, wave * 32 + li, h == 0, w.m * kLn2, w.l, [&](auto put) {
+        hand_over<C>(a, p, wave * 32 + li, h == 0, w.of, w.l, [&](auto put) {
 #pragma unroll
             for (int b = 0; b < R::kBlocks; ++b)
 #pragma unroll
@@ -1085,31 +1107,48 @@ struct Kernel<Tiled<OP, KH, KT, DV, OUT, PAGES16>> {
     static constexpr auto run = tiled_kernel<Tiled<OP, KH, KT, DV, OUT, PAGES16>>;
 };
 
-// A row's result out of the sums of its `pieces`: a wave per row.  source(k) says where piece k has its sums and its (score, sum of weights).
+// The reference of the piece, of a wave's 64, that is furthest ahead, and of `more`.
+__device__ __forceinline__ Reference furthest(Reference x, Reference more, float scale_log2) {
+    if (distance(more, x, scale_log2) > 0.0f) x = more;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const Reference y{__shfl_xor(x.raw, o, kWave), __shfl_xor(x.log2, o, kWave)};
+        if (distance(y, x, scale_log2) > 0.0f) x = y;
+    }
+    return Reference{__shfl(x.raw, 0, kWave), __shfl(x.log2, 0, kWave)};  // (lanes may hold different ones of the same height)
+}
+
+// A row's result out of the sums of its `pieces`: a wave per row.  source(k) says where piece k has its sums and its (reference, sum of weights).
 // The statistics of 64 pieces are fetched at once, a piece a lane, and then the sums one behind the other without waiting.
 struct Source {
     const float* sums;
     const float* ml;
 };
 template <class C, class SourceOf>
-__device__ __forceinline__ void join(int pieces, SourceOf source, typename C::Out* out, float* lse, int lane) {
+__device__ __forceinline__ void join(const Args& a, int pieces, SourceOf source, typename C::Out* out, float* lse, int lane) {
     constexpr int kColumns = C::kDv / 64, kVector = kColumns < 4 ? kColumns : 4, kVectors = kColumns / kVector;
-    float o[kColumns], m = -INFINITY, l = 0.0f;
+    constexpr Reference kNone{-INFINITY, 0.0f};
+    float o[kColumns], l = 0.0f;
+    Reference of = kNone;
 #pragma unroll
     for (int c = 0; c < kColumns; ++c) o[c] = 0.0f;
     for (int first = 0; first < pieces; first += kWave) {
         const int n = min(pieces - first, kWave);
         const Source mine = source(first + min(lane, n - 1));
-        float pm = mine.ml[0], pl = mine.ml[1];
-        if (lane >= n || pl == 0.0f) pm = -INFINITY, pl = 0.0f;  // (a piece without a visible key)
-        const float m_new = fmaxf(m, wave_max(pm)), use = m_new == -INFINITY ? 0.0f : m_new;
-        const float before = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((m - use) * kLog2e);
-        const float w = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((pm - use) * kLog2e);
+        const f32x4 stats = *reinterpret_cast<const f32x4*>(mine.ml);
+        const float pl = lane < n ? stats[2] : 0.0f;
+        const Reference pm = pl == 0.0f ? kNone : Reference{stats[0], stats[1]};  // (none: a piece without a visible key)
+        // Any number near the furthest reference will do; where powers of two are too coarse for one, it is that reference itself.
+        const float top = fmaxf(wave_max(fmaf(pm.raw, a.scale_log2, pm.log2)), fmaf(of.raw, a.scale_log2, of.log2));
+        Reference use{0.0f, top};
+        if (!(fabsf(top) <= kNear)) use = furthest(pm, of, a.scale_log2);
+        const float before = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(of, use, a.scale_log2));
+        const float w = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(pm, use, a.scale_log2));
         float sum = w * pl;
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, kWave);
         l = l * before + sum;
-        m = m_new;
+        of = l == 0.0f ? kNone : use;
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) o[c] *= before;
         const uint32_t lo = (uint32_t)(uintptr_t)mine.sums, hi = (uint32_t)((uintptr_t)mine.sums >> 32);
@@ -1151,7 +1190,7 @@ __device__ __forceinline__ void join(int pieces, SourceOf source, typename C::Ou
         }
         __builtin_memcpy(out + v * 64 * kVector + lane * kVector, y, sizeof y);
     }
-    if (lse && lane == 0) *lse = log_sum(m, l);
+    if (lse && lane == 0) *lse = log_sum(of, l, a.scale);
 }
 
 // Joins the item of which a share has the first piece and others have more.  blockIdx.x: share, blockIdx.y: rows of the tile, kWaves at a time.
@@ -1164,9 +1203,9 @@ __global__ __launch_bounds__(kThreads) void join_shares_kernel(Args a) {
     for (int r = blockIdx.y * kWaves + uniform(threadIdx.x >> 6); r < desc[4]; r += gridDim.y * kWaves) {
         const Place to = place_of(a, desc[1], desc[2], desc[3] * C::kM + r);
         const size_t row = (size_t)to.row * a.H + to.head;
-        join<C>(pieces, [&](int k) {
+        join<C>(a, pieces, [&](int k) {
             const size_t at = (size_t)(k == 0 ? first : second + (k - 1) * step) * a.m_cap + r;
-            return Source{a.part_o + at * C::kDv, a.part_ml + at * 2};
+            return Source{a.part_o + at * C::kDv, a.part_ml + at * 4};
         }, (typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
     }
 }
@@ -1188,12 +1227,12 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
     const int share0[2] = {(int)(common[1] & ((1 << kRefPlace) - 1)), (int)(own[1] & ((1 << kRefPlace) - 1))};
     const int place[2] = {min((int)(common[1] >> kRefPlace & 1023), a.m_cap - 1), min((int)(own[1] >> kRefPlace & 1023), a.m_cap - 1)};
     const int n0 = pieces[0] < 0 ? 0 : max(pieces[0], 1), n1 = max(pieces[1], 1);  // (no pieces: the whole in row_o)
-    join<C>(n0 + n1, [&](int k) {
+    join<C>(a, n0 + n1, [&](int k) {
         const int part = k < n0 ? 0 : 1, j = part ? k - n0 : k;
-        if (pieces[part] <= 0) return Source{a.row_o + (part * n + row) * C::kDv, a.row_ml + (part * n + row) * 2};
+        if (pieces[part] <= 0) return Source{a.row_o + (part * n + row) * C::kDv, a.row_ml + (part * n + row) * 4};
         const int share = clamp_to(share0[part] + j, 0, a.shares_cap - 1);
         const size_t at = (size_t)(2 * share + (j == 0 ? 1 : 0)) * a.m_cap + place[part];
-        return Source{a.part_o + at * C::kDv, a.part_ml + at * 2};
+        return Source{a.part_o + at * C::kDv, a.part_ml + at * 4};
     }, (typename C::Out*)a.out + row * C::kDv, a.lse ? a.lse + row : nullptr, lane);
 }
 
@@ -1210,11 +1249,11 @@ inline Layout layout_of(int m_cap, int dv, long long rows, bool shared) {
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t p = at; at += align_up(bytes, 256); return p; };
     l.part_o = take((size_t)2 * kSharesCap * m_cap * dv * sizeof(float));
-    l.part_ml = take((size_t)2 * kSharesCap * m_cap * 2 * sizeof(float));
+    l.part_ml = take((size_t)2 * kSharesCap * m_cap * 4 * sizeof(float));
     l.desc = take((size_t)2 * kSharesCap * kDescInts * sizeof(int32_t));
     if (shared) {
         l.row_o = take((size_t)2 * rows * dv * sizeof(float));
-        l.row_ml = take((size_t)2 * rows * 2 * sizeof(float));
+        l.row_ml = take((size_t)2 * rows * 4 * sizeof(float));
         l.refs = take((size_t)2 * rows * 2 * sizeof(int32_t));
     }
     l.total = at;
