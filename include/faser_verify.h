@@ -518,7 +518,7 @@ int fsr_latent_workspace_bytes(const fsr_latent_params* p /*host*/, size_t* out_
  *   workspace >= fsr_latent_workspace_bytes(p) bytes, 256-byte aligned
  * Scores, softmax statistics and sums are fp32.  With bf16 out the weights enter the second product in bf16 (an error of the size
  * of the output's own rounding); with fp32 out of bf16 inputs they are carried as a hi+lo pair.  Values that a row does not see
- * do not reach it, infinities and NaN included.
+ * do not reach it, infinities and NaN included.  An infinity that it sees makes its column infinite, or NaN where the weight is below 2^-80.
  */
 int fsr_latent_attention(const void* q, const void* cache, const int32_t* block_tables, const int32_t* ctx_lens, const int32_t* cu_q,
                          void* out, float* lse, const fsr_latent_params* p /*host*/, void* workspace, size_t ws_bytes, void* stream);

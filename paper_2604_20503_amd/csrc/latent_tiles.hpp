@@ -150,6 +150,8 @@ __device__ __forceinline__ f32x16 scores_of(const LatentRows<C>& w, const char* 
     }, w.q, beside);
 }
 
+constexpr float kLeast = 1.17549435e-38f;  // 2^-126, in bf16 as well
+
 template <class C>
 __device__ __forceinline__ void write_weights(const LatentRows<C>& w, char* p, const f32x16& z) {
 #pragma unroll
@@ -284,6 +286,9 @@ __device__ __forceinline__ bool take_any_tile(LatentRows<C>& w, const char* buf,
             for (int b = 0; b < LatentRows<C>::kBlocks; ++b) change_sums(w.acc[b], [&](float x, int) { return x * alpha; });
         }
         w.l += weights_of(z, w.of, scale_log2);
+        if (careful)  // a value that is not finite reaches every row that sees it, however small the weight
+#pragma unroll
+            for (int e = 0; e < 16; ++e) z[e] = key0 + 32 * part + 8 * (e >> 2) + 4 * h + (e & 3) <= w.seen && z[e] < kLeast ? kLeast : z[e];
         write_weights<C>(w, p, z);
     }
     const int far = live && __any(w.of.raw != 0.0f);

@@ -484,20 +484,21 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
                 v[b] = kEarly ? value[kEarly ? e : 0][b] : value_of(now, e, b);
                 odd |= (__builtin_bit_cast(uint32_t, v[b]) & 0x7f800000u) == 0x7f800000u;
             }
+            const float sees = kb + 4 * lg + e >= p.q.k_first && kb + 4 * lg + e <= seen && kb + 4 * lg + e < k_last ? 1.0f : 0.0f;
             if (!masked || !__any(odd)) {
 #pragma unroll
                 for (int b = 0; b < C::kDv / 16; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b], x[e], acc[b], 0, 0, 0);
             } else {
                 // a value that is not finite must not meet the zero weight of a row that does not see it: each kind is
-                // multiplied as 1 and takes its place only in rows that give it weight
+                // multiplied as 1 and takes its place in rows that see it, however small the weight
 #pragma unroll
                 for (int b = 0; b < C::kDv / 16; ++b) {
                     const bool fine = (__builtin_bit_cast(uint32_t, v[b]) & 0x7f800000u) != 0x7f800000u;
                     acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fine ? v[b] : 0.0f, x[e], acc[b], 0, 0, 0);
                     const f32x4 none = {0, 0, 0, 0};
-                    const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] == INFINITY ? 1.0f : 0.0f, x[e], none, 0, 0, 0);
-                    const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] == -INFINITY ? 1.0f : 0.0f, x[e], none, 0, 0, 0);
-                    const f32x4 nan = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] != v[b] ? 1.0f : 0.0f, x[e], none, 0, 0, 0);
+                    const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] == INFINITY ? 1.0f : 0.0f, sees, none, 0, 0, 0);
+                    const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] == -INFINITY ? 1.0f : 0.0f, sees, none, 0, 0, 0);
+                    const f32x4 nan = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b] != v[b] ? 1.0f : 0.0f, sees, none, 0, 0, 0);
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         float add = up[u] != 0.0f ? INFINITY : 0.0f;
@@ -883,11 +884,24 @@ __device__ __forceinline__ void take_any_keys(Rows<C>& w, const char* buf, int b
         const s16x8 v0 = values_of<C>(w, buf, block, 0, b), v1 = values_of<C>(w, buf, block, 1, b);
         if (__any(any_odd(v0) | any_odd(v1))) {
             // a value that is not finite must not meet the zero weight of a row that does not see it: each kind is
-            // multiplied as 1 and takes its place only in rows that give it weight
+            // multiplied as 1 and takes its place in rows that see it, however small the weight
             w.acc[b] = product(elements(v1, kFinite), hi[1], product(elements(v0, kFinite), hi[0], w.acc[b]));
             if constexpr (C::kPair) w.acc[b] = product(elements(v1, kFinite), lo[1], product(elements(v0, kFinite), lo[0], w.acc[b]));
 #pragma unroll 1
-            for (int kind = kUp; kind <= kNan; ++kind) put_odd(w.acc[b], product(elements(v1, kind), hi[1], product(elements(v0, kind), hi[0], zeros())), kind);
+            for (int kind = kUp; kind <= kNan; ++kind) {
+                int first_key = key0 + 4 * h;
+                asm volatile("" : "+v"(first_key));  // (computed for each kind and block: otherwise it is kept beside everything else)
+                auto sees = [&](int s) {
+                    u32x4 one;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int key = first_key + 16 * s + 8 * (k >> 1) + 2 * (k & 1);
+                        one[k] = (key >= k_first && key <= w.seen ? 0x3f80u : 0u) | (key + 1 >= k_first && key + 1 <= w.seen ? 0x3f800000u : 0u);
+                    }
+                    return __builtin_bit_cast(bf16x8, one);
+                };
+                put_odd(w.acc[b], product(elements(v1, kind), sees(1), product(elements(v0, kind), sees(0), zeros())), kind);
+            }
         } else {
             w.acc[b] = product(__builtin_bit_cast(bf16x8, v1), hi[1], product(__builtin_bit_cast(bf16x8, v0), hi[0], w.acc[b]));
             if constexpr (C::kPair) w.acc[b] = product(__builtin_bit_cast(bf16x8, v1), lo[1], product(__builtin_bit_cast(bf16x8, v0), lo[0], w.acc[b]));
@@ -895,8 +909,10 @@ __device__ __forceinline__ void take_any_keys(Rows<C>& w, const char* buf, int b
     }
 }
 
+// False: with weights in pairs, an infinite value that has met the rest of a weight, of either sign or zero, is NaN (to look at the values in the
+// loop over whole tiles would cost a third of it).  Sums that are not finite are not handed over; the piece is to be taken again without that loop.
 template <class C>
-__device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* buf0, char* buf1) {
+__device__ __forceinline__ bool run_tiled(const Args& a, const Piece& p, char* buf0, char* buf1, bool fast) {
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), li = lane & 31, h = lane >> 5;
     const int n_packed = p.q.rows * a.G, first = p.rt * C::kM + wave * 32;
     const bool active = first < n_packed;  // a wave without rows helps to load
@@ -966,7 +982,7 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
             // set and copies them in every tile)
             // (Said to be one value for the wave: otherwise the loop saves masks around itself, 13 moves a tile, 2 % of a long prompt.)
             const bool near = uniform((int)__any(w.of.raw != 0.0f)) == 0;
-            if (!odd && near) {
+            if (!odd && near && fast) {
                 w.of.raw = 0.0f;  // (known, and in no register of the loop)
                 while (whole()) {
                     if (!step(buf1, buf0)) { loaded = true; break; }
@@ -977,6 +993,21 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);  // the load too many has its place until it has come
     }
+    if constexpr (C::kPair) {
+        if (fast && p.t1 - p.t0 > 1) {
+            float odd = 0.0f;
+#pragma unroll
+            for (int b = 0; b < R::kBlocks; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) odd = fmaf(w.acc[b][e], 0.0f, odd);
+            __syncthreads();  // (all loads have come, nobody reads the buffers any more)
+            int* any = reinterpret_cast<int*>(buf0);
+            const int mine = __any(odd != 0.0f);
+            if (lane == 0) any[wave] = mine;
+            __syncthreads();
+            if (uniform(any[0] | any[1] | any[2] | any[3])) return false;
+        }
+    }
     w.l += other_half(w.l);
     if (active && first + li < n_packed)
         hand_over<C>(a, p, wave * 32 + li, h == 0, w.of, w.l, [&](auto put) {
@@ -985,6 +1016,7 @@ __device__ __forceinline__ void run_tiled(const Args& a, const Piece& p, char* b
 #pragma unroll
                 for (int g = 0; g < 4; ++g) put(32 * b + 8 * g + 4 * h, f32x4{w.acc[b][4 * g], w.acc[b][4 * g + 1], w.acc[b][4 * g + 2], w.acc[b][4 * g + 3]});
         });
+    return true;
 }
 
 // The pieces of a share of the line, one after the other.
@@ -1093,7 +1125,10 @@ __global__ __launch_bounds__(C::kBlockThreads, 2) void tiled_kernel(Args a) {  /
     Walk<C> walk;
     walk.begin(a, share, line);
     Piece p;
-    while (walk.next(a, share, p)) run_tiled<C>(a, p, buf0, buf1);
+    while (walk.next(a, share, p)) {
+        bool fast = true;
+        while (!run_tiled<C>(a, p, buf0, buf1, fast)) fast = false;
+    }
 }
 
 template <class C>
