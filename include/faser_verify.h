@@ -552,7 +552,8 @@ int fsr_shared_workspace_bytes(const fsr_attn_params* p /*host*/, size_t* out_by
  *   cu_groups   [n_groups+1] int32, ascending; requests outside cu_groups[0] .. cu_groups[n_groups]-1 get no output
  *   prefix_lens [n_groups] int32, 0 allowed.  A request whose ctx_lens is below its group's prefix counts as one of exactly the
  *               prefix: all its rows see the prefix whole, and row j its own positions prefix .. prefix + j.
- *   q, caches, block_tables, ctx_lens, cu_q, out, lse and *p as for fsr_verify_attention (any page size, any H_q / H_kv).
+ *   q, caches, block_tables, ctx_lens, cu_q, out, lse and *p as for fsr_verify_attention (any page size, any H_q / H_kv), except that
+ *               max_workgroups counts compute units here: bf16 calls put two workgroups on each
  *   workspace   >= fsr_shared_workspace_bytes(p) bytes, 256-byte aligned
  */
 int fsr_verify_attention_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,

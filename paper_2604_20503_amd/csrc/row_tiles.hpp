@@ -1328,9 +1328,9 @@ inline int compute_units() {
 
 template <class C>
 int launch(Args a, int max_workgroups, void* stream, const char* who) {
-    int nb = compute_units() * C::kPerUnit;
-    if (max_workgroups > 0) nb = std::min(nb, max_workgroups * C::kPerUnit);
-    a.nb = std::min(nb, kSharesCap);
+    int units = compute_units();
+    if (max_workgroups > 0) units = std::min(units, max_workgroups);  // (any number is allowed: taken times the workgroups of a unit only now)
+    a.nb = std::min(units * C::kPerUnit, kSharesCap);
     a.min_share = C::kMinShare;
     a.even_cap = a.nb;
     // Items that may outnumber the workgroups are cut into pieces for several rounds.  (Else that many descriptors need not be looked at.)
