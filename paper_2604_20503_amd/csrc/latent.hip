@@ -25,13 +25,14 @@ struct MoveArgs {
     const int32_t* ctx;  // append: position of a request's first row; gather: null, position 0
     const int32_t* cu;
     int B, rows_cap, P, max_pages, n_pages;
+    int row0;            // first row of the launch
     int head16, tail16;  // 16-byte pieces of a latent and of a rope part
 };
 
 template <bool APPEND>
 __global__ __launch_bounds__(kThreads) void move_rows_kernel(MoveArgs a) {
     __shared__ long long slots[kMoveRows];  // -1: no such row, or nowhere to put it
-    const int row0 = blockIdx.x * kMoveRows;
+    const int row0 = a.row0 + blockIdx.x * kMoveRows;
     if (threadIdx.x < kMoveRows) {
         const int row = row0 + threadIdx.x;
         long long slot = -1;
@@ -91,9 +92,13 @@ int move_rows(bool append, void* cache, void* latent, void* rope, const int32_t*
     a.bt = bt; a.ctx = ctx; a.cu = cu;
     a.B = p->B; a.rows_cap = rows_cap; a.P = p->P; a.max_pages = p->max_pages; a.n_pages = p->n_pages;
     a.head16 = p->D_latent * elem / 16; a.tail16 = p->D_rope * elem / 16;
-    const dim3 grid(((unsigned)rows_cap + kMoveRows - 1) / kMoveRows);
-    if (append) hipLaunchKernelGGL(move_rows_kernel<true>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL(move_rows_kernel<false>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+    constexpr long long kMost = (long long)kMaxBlocks * kMoveRows;
+    for (long long first = 0; first < rows_cap; first += kMost) {
+        a.row0 = (int)first;
+        const dim3 grid((unsigned)((std::min(rows_cap - first, kMost) + kMoveRows - 1) / kMoveRows));
+        if (append) hipLaunchKernelGGL(move_rows_kernel<true>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL(move_rows_kernel<false>, grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+    }
     return check_launch(who);
 }
 

@@ -38,6 +38,7 @@ constexpr int kDescInts = 8;       // merge descriptor of a share
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kSharesCap = 512;
+constexpr int kMaxBlocks = 1 << 23;  // of a launch: its threads are counted in 32 bits
 constexpr int kEvenRounds = 3;       // latent: most pieces of a workgroup in a batch that is cut evenly
 constexpr int kRefPlace = 10, kRefPrefix = 1 << 24;  // fields of a reference to a part of a row: its place in the tile; there is a prefix before it
 constexpr float kAhead = 40.0f;    // distance of a row's exponent reference from its largest score, in powers of two
@@ -1245,12 +1246,12 @@ __global__ __launch_bounds__(kThreads) void join_shares_kernel(Args a) {
     }
 }
 
-// Joins what a row's prefix and its own keys left.  A wave per (call row, query head).
+// Joins what a row's prefix and its own keys left.  A wave per (call row, query head), from `first` on.
 template <class C>
-__global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a) {
+__global__ __launch_bounds__(kThreads) void join_rows_kernel(Args a, size_t first) {
     const int lane = threadIdx.x & 63;
     const size_t n = (size_t)a.N_cap * a.H;
-    const size_t row = (size_t)blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
+    const size_t row = first + (size_t)blockIdx.x * kWaves + uniform(threadIdx.x >> 6);
     if (row >= n) return;
     const int i0 = clamp_to(a.cu_groups[0], 0, a.B), i1 = clamp_to(a.cu_groups[a.n_groups], 0, a.B);
     const int call_row = (int)(row / a.H), head = (int)(row - (size_t)call_row * a.H);
@@ -1340,8 +1341,12 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
     int rc = check_launch(who);
     if (rc != FSR_OK) return rc;
     if (C::kOp == kShared) {
+        constexpr size_t kMost = (size_t)kMaxBlocks * kWaves;
         const size_t rows = (size_t)a.N_cap * a.H;
-        hipLaunchKernelGGL((join_rows_kernel<C>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
+        for (size_t first = 0; first < rows; first += kMost) {
+            const size_t now = std::min(rows - first, kMost);
+            hipLaunchKernelGGL((join_rows_kernel<C>), dim3((unsigned)((now + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a, first);
+        }
     } else {
         // 16 workgroups a share: one row a wave of a latent tile, two of a tile of heads; with 32 there the launching of workgroups took longer: 20 us, not 17.6
         hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.even_cap, std::min(16, (a.m_cap + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);
