@@ -1340,7 +1340,7 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
     hipLaunchKernelGGL((Kernel<C>::run), dim3(a.nb), dim3(C::kBlockThreads), 0, s, a);
     int rc = check_launch(who);
     if (rc != FSR_OK) return rc;
-    if (C::kOp == kShared) {
+    if constexpr (C::kOp == kShared) {  // (each operator's join is compiled for it alone)
         constexpr size_t kMost = (size_t)kMaxBlocks * kWaves;
         const size_t rows = (size_t)a.N_cap * a.H;
         for (size_t first = 0; first < rows; first += kMost) {
