@@ -114,7 +114,7 @@ typedef struct fsr_latent_params {
     int32_t B;         /* requests in the batch (>= 0) */
     int32_t N_cap;     /* rows allocated: of q/out or of the new rows (cu_q[B] <= N_cap); of the gathered rows (cu_k[B] <= N_cap) */
     int32_t H;         /* query heads; they all read the same cache row (attention only) */
-    int32_t D_latent;  /* elements of a token's latent vector: any that fill 16-byte pieces; attention: 256 or 512 */
+    int32_t D_latent;  /* elements of a token's latent vector: any up to 8192 that fill 16-byte pieces; attention: 256 or 512 */
     int32_t D_rope;    /* elements of its position part, likewise; attention: 32 or 64 */
     int32_t P;         /* tokens per page, any */
     int32_t max_pages; /* row stride of block_tables */
@@ -122,8 +122,8 @@ typedef struct fsr_latent_params {
     int32_t dtype;     /* FSR_F32 or FSR_BF16: element type of the cache, the rows and q */
     int32_t out_dtype; /* attention: FSR_F32 always allowed; FSR_BF16 with bf16 inputs */
     float scale;       /* attention: softmax scale, > 0 */
-    int32_t max_q_len; /* attention: upper bound on the rows of any one request, or 0 if unknown.  A hint, as in
-                          fsr_attn_params: requests with more rows are still computed correctly. */
+    int32_t max_q_len; /* attention: upper bound on the rows of any one request, or 0 if unknown.  Results and times do not
+                          depend on it: the rows are counted on the device. */
     int32_t max_workgroups; /* 0, or the compute units that the call's stream owns (as in fsr_attn_params) */
     int32_t reserved;  /* must be 0 */
 } fsr_latent_params;
@@ -140,7 +140,7 @@ typedef struct fsr_expanded_params {
     int32_t dtype;     /* FSR_F32 or FSR_BF16: element type of q, kv, k_rope */
     int32_t out_dtype; /* FSR_F32 always allowed; FSR_BF16 with bf16 inputs */
     float scale;       /* softmax scale, > 0 */
-    int32_t max_q_len; /* upper bound on the rows of any one request, or 0 if unknown (a hint, as above) */
+    int32_t max_q_len; /* upper bound on the rows of any one request, or 0 if unknown (nothing depends on it, as above) */
     int32_t max_workgroups; /* 0, or the compute units that the call's stream owns */
     int32_t reserved;  /* must be 0 */
 } fsr_expanded_params;
@@ -540,7 +540,7 @@ int fsr_expanded_workspace_bytes(const fsr_expanded_params* p /*host*/, size_t* 
 int fsr_latent_attention_expanded(const void* q, const void* kv, const void* k_rope, const int32_t* cu_q, const int32_t* cu_k, void* out,
                                   float* lse, const fsr_expanded_params* p /*host*/, void* workspace, size_t ws_bytes, void* stream);
 
-/* Workspace bytes needed by fsr_verify_attention_shared for shapes up to *p (host query). */
+/* Workspace bytes needed by fsr_verify_attention_shared (host query).  The same size covers every smaller B and N_cap with the same heads. */
 int fsr_shared_workspace_bytes(const fsr_attn_params* p /*host*/, size_t* out_bytes /*host*/);
 
 /*
@@ -548,12 +548,15 @@ int fsr_shared_workspace_bytes(const fsr_attn_params* p /*host*/, size_t* out_by
  * first prefix_lens[g] positions hold the same tokens, and are read once for all of the group's rows, through the block table
  * of its first request (any length: where the prefix ends inside a page, the other requests' copies of that page hold the same
  * values).  Positions from prefix_lens[g] on are read through a request's own table.  Results are those of
- * fsr_verify_attention, up to the order of sums and the rounding of the weights (see fsr_latent_attention).
+ * fsr_verify_attention, up to the order of sums and the rounding of the weights: once to bf16 where out is bf16, as a hi+lo pair
+ * where it is fp32 (see fsr_latent_attention).  It pays where groups of many requests share long prefixes: measured, from about 1000
+ * tokens in common on for groups of 8 and more in a batch of 64, from 8000 on for a batch of 8; it loses, up to twofold, behind shorter
+ * ones and in groups of one request, where fsr_verify_attention is to be called.
  *   cu_groups   [n_groups+1] int32, ascending; requests outside cu_groups[0] .. cu_groups[n_groups]-1 get no output
  *   prefix_lens [n_groups] int32, 0 allowed.  A request whose ctx_lens is below its group's prefix counts as one of exactly the
  *               prefix: all its rows see the prefix whole, and row j its own positions prefix .. prefix + j.
  *   q, caches, block_tables, ctx_lens, cu_q, out, lse and *p as for fsr_verify_attention (any page size, any H_q / H_kv), except that
- *               max_workgroups counts compute units here: bf16 calls put two workgroups on each
+ *               max_workgroups counts compute units here (bf16 calls put two workgroups on each), and nothing depends on max_q_len
  *   workspace   >= fsr_shared_workspace_bytes(p) bytes, 256-byte aligned
  */
 int fsr_verify_attention_shared(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,

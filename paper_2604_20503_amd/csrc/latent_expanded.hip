@@ -3,7 +3,8 @@
 //     z[j, t] = scale * (q_nope[j] . k_nope[t, h] + q_rope[j] . k_rope[t]).
 // Per row and key it costs D_nope + D_rope + D_v multiply-adds a head where the form in the latent's space costs
 // 2 D_latent + D_rope, which is worth the up-projection once a request has many rows (a chunk of a prompt).
-// Measured: 2048 rows behind 6000 tokens, 32 heads: 326 us, 906 TFLOP/s; 4 prompts of 200-700 rows, 16 heads: 66 us, 387 TFLOP/s.
+// Measured: 2048 rows behind 6000 tokens, 32 heads: 314-341 us by card, 938-864 TFLOP/s; 4 prompts of 200-700 rows, 16 heads: 67-69 us, 381-372
+// TFLOP/s.  fp32: 2 prompts of 200-700 rows behind up to 1000 keys, 16 heads: 156 us, 47 TFLOP/s of 150.
 #include "row_tiles.hpp"
 
 namespace fsr {

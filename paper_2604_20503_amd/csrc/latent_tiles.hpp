@@ -6,8 +6,10 @@
 // LDS has to deliver per tile, keys once per two waves and values once per two waves, is 370 KB against 2176 cycles of the matrix
 // cores (2900 cycles at 128 bytes each); with 16 rows a wave it would be 626 KB.
 //
-// Measured: 4350 cycles a tile whose keys come from the cache (scores 1660, weights 690, second product 1500, three barriers).  64
-// requests of 512-4096 keys, 1-4 rows, 128 heads: 223-240 us, 496-462 TFLOP/s by card; 32 of 1024-8192 keys, 16 heads: 82 us, 2.0 TB/s.
+// Measured: 4350 cycles a tile whose keys come from the cache, scores 1660, weights 690, second product 1500 and three barriers one after the
+// other: with one wave a SIMD nothing runs beside them, and that, not LDS, is the bound.  64 requests of 512-4096 keys, 1-4 rows, 128 heads:
+// 210-219 us by card, 529-507 TFLOP/s; 32 of 1024-8192 keys, 16 heads: 75-82 us, 2.2-2.0 TB/s.  The kernels of 512 elements use all 512
+// registers, and what is set up once a piece (addresses, schedule) and the general tiles spill 110-200 more; the loop over whole tiles does not.
 //
 // The exponent reference of a row has to be common to both waves.  It is kept kAhead powers of two above the largest score seen and
 // changed only in a tile where a score overtakes it, the first one for the most part, with two more barriers.
@@ -22,8 +24,8 @@ template <int KH, int KT, class OUT, bool PAGES16>
 struct Latent {
     static constexpr int kOp = kLatent, kHead = KH, kTail = KT, kDk = KH + KT, kDv = KH;
     static constexpr bool kPair = sizeof(OUT) == 4, kPages16 = PAGES16;
-    // Where row tiles outnumber the workgroups: even pieces in rounds (below), 272 -> 240 us for 64 requests of 128 heads, 418 -> 335 us with
-    // lengths of 100-8000.  Rows of 256 + 32 pass the cache at half the bytes: there the cut line stays, 92 us and not 99.
+    // Where row tiles outnumber the workgroups: even pieces in rounds (below), 202 us and not 234 for 64 requests of 512-4096 keys and 128 heads,
+    // 224 and not 342 for 100 of 30-3000.  Rows of 256 + 32 pass the cache at half the bytes: there the cut line stays, 92 us and not 99.
     static constexpr bool kEven = KH >= 512;
     static constexpr int kM = 64, kKeys = 64, kBlockThreads = 256, kWaves = 4, kPerUnit = 1, kItemCost = 2, kMinShare = kItemCost + 1;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kBuf = kTailAt + kKeys * KT * 2;
@@ -435,7 +437,10 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
 // keys, row tile by row tile, are neighbours (and share a die's cache).  The length is the shortest of 64 candidates, one per lane, from
 // an equal share of all key tiles upwards, for which the pieces do not outnumber the workgroups.  Where there are more row tiles, every
 // workgroup takes up to kEvenRounds pieces: taking one up costs 38000 cycles (7 tiles), but row tiles of a request that run at different
-// keys read these anew from behind the die's cache, 8000 cycles a tile and not 5300.  False: the line is cut instead.
+// keys read these anew from behind the die's cache, 8000 cycles a tile and not 5300.  False: the line is cut instead, where the length that
+// is needed is much beyond an equal share: few long requests among as many short ones as there are workgroups.  us by the line / by even
+// pieces, 16 heads: within the bound, 32 requests of 1024-8192 keys 82 / 59, one of 8000 and 31 of 100-500 60 / 55, 250 of 300 77 / 51; just
+// beyond it, 230 of 500 and 20 of 900 83 / 68, 220 of 300 and 30 of 2000 86 / 98; far beyond it, 240 of 64 and 10 of 8000 95 / 259.
 constexpr int kEvenRequests = 256;
 struct EvenScratch {
     int tiles[kEvenRequests], row_tiles[kEvenRequests];

@@ -534,8 +534,9 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
 //
 // What bounds it: each of the four waves reads all keys and values of a tile, 128 KB with heads of 128 (160 KB with a second part of 64)
 // and 32 KB (40) to write, 1280 (1600) cycles of a compute unit's LDS against 1024 (1280) of its matrix cores and 900 of exponentials
-// and conversions.  Measured: 1775 cycles a tile where two workgroups share a unit; 2048 rows of 32 heads behind 6000 tokens of
-// context: 326 us, 906 TFLOP/s (clocks differ: 313 on another card).  (64 rows a wave would halve what LDS delivers, but leave one wave to a SIMD.)
+// and conversions.  Measured: 2048 rows of 32 heads behind 6000 tokens of context: 314-341 us by card, 938-864 TFLOP/s; a workgroup's 111
+// tiles and two pieces take 496 000 cycles at 1.74 GHz (short calls run at 2.1-2.3), 4050 a tile, 2025 a tile of the unit, which two
+// workgroups share.  (64 rows a wave would halve what LDS delivers, but leave one wave to a SIMD.)
 //
 // PAGES16: 16 keys from a multiple of 16 on are 16 rows that follow each other (no pages, or pages of a multiple of 16 tokens).
 template <int OP, int KH, int KT, int DV, class OUT, bool PAGES16>

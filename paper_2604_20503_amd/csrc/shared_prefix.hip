@@ -3,8 +3,10 @@
 // and 128 packed rows, and their products are matrix-core sized, where request by request every one reads them again.  A
 // request's own tokens behind the prefix are a second sequence of the same launch; the two results of a row are joined by
 // their softmax statistics.
-// Measured: 64 requests of 2-9 rows behind 8192 common tokens and 64-1024 of their own, 32/8 heads of 128: 104 us; 192 requests in 4
-// groups, 64/8 heads: 506 us, 770 TFLOP/s.  Own contexts of few rows cost most for what they are: three of four waves only load.
+// Measured: 64 requests of 2-9 rows behind 8192 common tokens and 64-1024 of their own, 32/8 heads of 128: 101-107 us by card; 192 requests in
+// 4 groups, 64/8 heads: 490-526 us, 795-741 TFLOP/s.  Own contexts of few rows cost most for what they are: three of four waves only load.
+// us beside fsr_verify_attention with a plan, 300 tokens of their own, 32/8 heads, behind 256 / 1024 / 8192 common ones: 8 requests 33 and 19 / 32
+// and 23 / 39 and 42; 64 requests 48 and 38 / 57 and 59 / 103 and 324; 64 requests in groups of one 57 and 40 / 96 and 70 / 426 and 366.
 #include "row_tiles.hpp"
 
 namespace fsr {
