@@ -145,6 +145,65 @@ typedef struct fsr_expanded_params {
     int32_t reserved;  /* must be 0 */
 } fsr_expanded_params;
 
+/* Most words of 64 bits that a row of a tree mask has, and most alternatives that fsr_token_logprobs gives. */
+#define FSR_TREE_WORDS_MAX 16
+#define FSR_TOP_MAX 64
+
+/* Static shape of one append with rotation. */
+typedef struct fsr_rope_params {
+    int32_t B;         /* requests in the batch (>= 0) */
+    int32_t N_cap;     /* rows allocated in q/k_new/v_new/q_out; cu_q[B] <= N_cap */
+    int32_t H_q;       /* query heads */
+    int32_t H_kv;      /* KV heads */
+    int32_t D;         /* head dim, a multiple of 8 (8-bit caches: of 16) up to 8192 */
+    int32_t R;         /* elements of a head that are rotated, from the first on: a multiple of 16, <= D */
+    int32_t P;         /* tokens per page, any */
+    int32_t max_pages; /* row stride of block_tables */
+    int32_t n_pages;   /* pages in the caches */
+    int32_t T;         /* rows of cos_sin (positions are clamped into [0, T)) */
+    int32_t tree_words; /* words of 64 bits of a row of tree_mask, up to FSR_TREE_WORDS_MAX; ignored without a mask */
+    int32_t pairs;     /* 0: element i is rotated with element i + R/2; 1: element 2i with 2i + 1 */
+    int32_t dtype;     /* FSR_F32 or FSR_BF16: element type of q, k_new, v_new, q_out (and of caches that are not 8-bit) */
+    int32_t kv_layout; /* as in fsr_attn_params */
+    int64_t q_stride;  /* elements from a row of q to the next (H_q * D where rows are dense; a slice of fused projections has more) */
+    int64_t k_stride;  /* of k_new (dense: H_kv * D) */
+    int64_t v_stride;  /* of v_new; rows must lie a multiple of 16 bytes apart */
+    int64_t reserved;  /* must be 0 */
+} fsr_rope_params;
+
+/* Static shape of one acceptance of trees. */
+typedef struct fsr_tree_params {
+    int32_t B;          /* requests */
+    int32_t N_cap;      /* rows allocated; cu_q[B] <= N_cap */
+    int32_t tree_words; /* words of 64 bits of a row of tree_mask: 1 .. FSR_TREE_WORDS_MAX */
+    int32_t S_max;      /* most drafts that are accepted of a request; emitted and path have S_max + 1 columns */
+    int32_t reserved;   /* must be 0 */
+} fsr_tree_params;
+
+/* Static shape of one commit of accepted paths. */
+typedef struct fsr_commit_params {
+    int32_t B;         /* requests */
+    int32_t H_kv;      /* KV heads */
+    int32_t row_bytes; /* bytes of a head's key or value in the cache (D times the element's size), a multiple of 16 */
+    int32_t P;         /* tokens per page, any */
+    int32_t max_pages; /* row stride of block_tables */
+    int32_t n_pages;   /* pages in the caches */
+    int32_t S_max;     /* path has S_max + 1 columns */
+    int32_t kv_layout; /* as in fsr_attn_params */
+} fsr_commit_params;
+
+/* Static shape of one call of log probabilities. */
+typedef struct fsr_logprob_params {
+    int32_t N_cap;      /* rows allocated */
+    int32_t V;          /* logits of a row (> 0) */
+    int32_t M;          /* given tokens of a row (0 allowed) */
+    int32_t K;          /* alternatives of a row, 0 .. FSR_TOP_MAX, <= V */
+    int32_t dtype;      /* FSR_F32 or FSR_BF16: element type of the logits */
+    int32_t reserved;   /* must be 0 */
+    int64_t stride;     /* elements from a row of logits to the next, >= V */
+    double temperature; /* p = softmax(z / temperature), 1e-6 .. 1e6 */
+} fsr_logprob_params;
+
 /* Static description of the last failure on the calling thread ("" if none).  Host. */
 const char* fsr_last_error(void);
 
@@ -563,6 +622,102 @@ int fsr_verify_attention_shared(const void* q, const void* k_cache, const void* 
                                 const int32_t* ctx_lens, const int32_t* cu_q, const int32_t* cu_groups, const int32_t* prefix_lens,
                                 int32_t n_groups, void* out, float* lse, const fsr_attn_params* p /*host*/, void* workspace,
                                 size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Trees of drafted tokens.
+ *
+ * A request may bring a tree of drafts instead of a chain (Sec. 6.4.1: heads that draft several continuations).  Its rows are the last
+ * committed token (row 0) and the drafts, parents in front of their children.  tree_mask [N_cap, tree_words] holds, in row j of the
+ * request, a bit for each row of the request that row j sees: bit a % 64 of word a / 64 for row a -- its ancestors and itself.  A row's
+ * depth is the number of its bits less one, its parent the highest of its bits below itself.  Row j's key and value lie at position
+ * ctx_lens[i] + j of the cache like a chain's; what it is rotated to is the position ctx_lens[i] + depth.
+ *     fsr_kv_append_rope         rows are rotated and enter the cache          (once per layer)
+ *     fsr_verify_attention_tree  they attend to the context and their ancestors (once per layer)
+ *     fsr_tree_accept            the path that the target agrees with
+ *     fsr_kv_commit              its keys and values move to the positions behind the context (once per layer)
+ *
+ * fsr_kv_append_rope: fsr_kv_append with the rotation on the way.  Row j of request i, at rotary position t, has the pairs (a, b) of
+ * elements of every query and key head, pair m of R/2, replaced by
+ *     (a cos[t][m] - b sin[t][m], b cos[t][m] + a sin[t][m]);
+ * elements from R on, and values, stay as they are.  t is positions[row] where given, else ctx_lens[i] + depth by tree_mask where
+ * given, else ctx_lens[i] + j.  The arithmetic is fp32; results are rounded once.  Any other use of positions (several axes, scaled
+ * frequencies) goes by the table.
+ *   q [N_cap, H_q, D], k_new, v_new [N_cap, H_kv, D] dtype, rows apart by the strides; rows >= cu_q[B] are not used
+ *   cos_sin    [T, R] float32: the R/2 cosines of a position, then its sines
+ *   positions  [N_cap] int32, nullable; tree_mask nullable; not both
+ *   q_out      [N_cap, H_q, D] dtype, dense; may be q itself where q is dense; rows >= cu_q[B] are not written
+ *   caches, block_tables, ctx_lens, cu_q as for fsr_kv_append; positions without a page and page ids outside the pool are skipped
+ * fsr_kv_append_rope_kv8: into 8-bit caches as fsr_kv_append_kv8 stores them (bf16 rows); a rotated key is rounded once, from fp32.
+ * Pointers of rows, caches and cos_sin 16-byte aligned, no workspace.
+ */
+int fsr_kv_append_rope(const void* q, const void* k_new, const void* v_new, const float* cos_sin, const int32_t* positions,
+                       const uint64_t* tree_mask, void* q_out, void* k_cache, void* v_cache, const int32_t* block_tables,
+                       const int32_t* ctx_lens, const int32_t* cu_q, const fsr_rope_params* p /*host*/, void* stream);
+int fsr_kv_append_rope_kv8(const void* q, const void* k_new, const void* v_new, const float* cos_sin, const int32_t* positions,
+                           const uint64_t* tree_mask, void* q_out, void* k_cache, void* v_cache, const float* k_scale,
+                           const float* v_scale, const int32_t* block_tables, const int32_t* ctx_lens, const int32_t* cu_q,
+                           const fsr_rope_params* p /*host*/, void* stream);
+
+/* Workspace bytes needed by fsr_verify_attention_tree (host query).  The same size covers every smaller B and N_cap with the same heads. */
+int fsr_tree_workspace_bytes(const fsr_attn_params* p /*host*/, size_t* out_bytes /*host*/);
+
+/*
+ * fsr_verify_attention for trees: row j of request i attends to the positions 0 .. ctx_lens[i] - 1 and to ctx_lens[i] + a for every bit
+ * a of its row of tree_mask.  Any mask is allowed, not only those of trees; a row that sees nothing (no context, no bit) gets zeros and
+ * lse = -inf.  Rows that the mask has no bit for (a >= 64 tree_words) are seen by none.  Results are those of
+ * fsr_verify_attention_shared in accuracy: weights enter the second product rounded once to bf16 where out is bf16, as a hi+lo pair
+ * where it is fp32.  Values that a row does not see do not reach it, infinities and NaN included.
+ *   tree_mask  [N_cap, tree_words] 64-bit words, 1 <= tree_words <= FSR_TREE_WORDS_MAX
+ *   q, caches, block_tables, ctx_lens, cu_q, out, lse and *p as for fsr_verify_attention_shared (any page size, any H_q / H_kv)
+ *   workspace  >= fsr_tree_workspace_bytes(p) bytes, 256-byte aligned
+ */
+int fsr_verify_attention_tree(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                              const int32_t* ctx_lens, const int32_t* cu_q, const uint64_t* tree_mask, int32_t tree_words, void* out,
+                              float* lse, const fsr_attn_params* p /*host*/, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Accept trees (Sec. 2.1 for a tree: accept while a draft is what the target chose).  target_tokens holds the target's token at every
+ * row: its arg max (temperature 0), or a token drawn from its distribution there, which makes the emitted tokens the target's own.
+ * From row 0 on, the first child (lowest row) whose draft token is the target's token at its parent is accepted, at most S_max of them.
+ *   target_tokens, draft_tokens [N_cap] int32 (a request's row 0 has no draft; its entry is not read), tree_mask, cu_q [B+1]
+ *   accepted_len [B] int32: drafts accepted; n_emitted [B]: accepted_len + 1 (a request without rows: -1 and 0)
+ *   emitted      [B, S_max+1] int32: the target's tokens along the path, padded -1
+ *   path         [B, S_max+1] int32: the rows of the path within the request, row 0 first, padded -1
+ *   keep_mask    nullable [N_cap] uint8: 1 for the rows of the path (feed it to fsr_prune_compact with suffix_close = 0); rows
+ *                >= cu_q[B] are not written
+ */
+int fsr_tree_accept(const int32_t* target_tokens, const int32_t* draft_tokens, const uint64_t* tree_mask, const int32_t* cu_q,
+                    int32_t* accepted_len, int32_t* n_emitted, int32_t* emitted, int32_t* path, uint8_t* keep_mask,
+                    const fsr_tree_params* p /*host*/, void* stream);
+
+/*
+ * Commit accepted paths (Sec. 2.1: the accepted tokens become context): for k = 1 .. accepted_len[i], in this order, the key and the
+ * value at position ctx_lens[i] + path[i][k] are copied, bit for bit, to position ctx_lens[i] + k.  The caller then adds n_emitted to
+ * ctx_lens (the last emitted token is the next step's row 0).
+ *   caches     in either layout, of any element type; row_bytes bytes a head, 16-byte aligned
+ *   accepted_len [B] int32 (negative: nothing moves), path [B, S_max+1] int32 as fsr_tree_accept gives them.  Entries must be >= their
+ *              place (those of a tree's path are); lower ones, positions without a page and page ids outside the pool are skipped.
+ */
+int fsr_kv_commit(void* k_cache, void* v_cache, const int32_t* block_tables, const int32_t* ctx_lens, const int32_t* accepted_len,
+                  const int32_t* path, const fsr_commit_params* p /*host*/, void* stream);
+
+/* Workspace bytes needed by fsr_token_logprobs (host query).  The same size covers every smaller N_cap with the same V, M, K and dtype. */
+int fsr_logprob_workspace_bytes(const fsr_logprob_params* p /*host*/, size_t* out_bytes /*host*/);
+
+/*
+ * What a server reports of the target's rows (Sec. 2.1: the rows that fsr_spec_accept judges): with p = softmax(z / temperature),
+ *   logprobs     [N_cap, M] float32: log p of the given tokens (-inf for an id outside [0, V))
+ *   entropy      [N_cap] float32, nullable: -sum p log p, in natural units
+ *   top_ids      [N_cap, K] int32, top_logprobs [N_cap, K] float32: the K largest logits in descending order, the lowest id first
+ *                among equals
+ * of logits [N_cap, V] dtype, rows `stride` elements apart.  A NaN logit counts as -inf, which has probability 0.  A row without a
+ * finite logit, or with one that is +inf, has NaN for its log probabilities and entropy; its top_ids are as ever.
+ *   tokens [N_cap, M] int32;  n_rows nullable [1] int32, device: rows from n_rows[0] on are neither read nor written (&cu_q[B])
+ *   workspace >= fsr_logprob_workspace_bytes(p) bytes, 256-byte aligned
+ */
+int fsr_token_logprobs(const void* logits, const int32_t* n_rows, const int32_t* tokens, float* logprobs, float* entropy,
+                       int32_t* top_ids, float* top_logprobs, const fsr_logprob_params* p /*host*/, void* workspace, size_t ws_bytes,
+                       void* stream);
 
 /* ---------------------------------------------------------------------------------------
  * Measurement aid (not a step of the verification path): one launch that reads `bytes` bytes at

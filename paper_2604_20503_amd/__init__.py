@@ -18,6 +18,8 @@ from .binding import (  # noqa: F401
     hbm_read_probe,
     kv_append,
     kv_append_kv8,
+    kv_append_rope,
+    kv_commit,
     last_error,
     latent_append,
     latent_attention,
@@ -26,6 +28,7 @@ from .binding import (  # noqa: F401
     latent_workspace_bytes,
     library_path,
     load_library,
+    logprob_workspace_bytes,
     prune_compact,
     prune_restore,
     prune_scatter,
@@ -33,11 +36,15 @@ from .binding import (  # noqa: F401
     spec_accept,
     survivor_compact,
     survivor_mask,
+    token_logprobs,
     topk_rank_check,
+    tree_accept,
+    tree_workspace_bytes,
     verify_attention,
     verify_attention_kv8,
     verify_attention_shared,
     verify_attention_static,
+    verify_attention_tree,
     version,
 )
 from .frontier import verify_chunked  # noqa: F401
@@ -48,4 +55,5 @@ __all__ = [
     "spec_accept", "survivor_compact", "survivor_mask", "topk_rank_check", "verify_attention", "verify_attention_kv8", "verify_attention_static", "verify_chunked", "version",
     "expanded_workspace_bytes", "latent_append", "latent_attention", "latent_attention_expanded", "latent_gather", "latent_workspace_bytes",
     "shared_workspace_bytes", "verify_attention_shared",
+    "kv_append_rope", "kv_commit", "logprob_workspace_bytes", "token_logprobs", "tree_accept", "tree_workspace_bytes", "verify_attention_tree",
 ]

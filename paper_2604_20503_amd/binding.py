@@ -30,6 +30,8 @@ SYMBOLS = [
     "fsr_prune_scatter", "fsr_survivor_mask", "fsr_survivor_compact", "fsr_topk_rank_check", "fsr_frontier_init", "fsr_frontier_plan", "fsr_frontier_commit",
     "fsr_latent_append", "fsr_latent_gather", "fsr_latent_workspace_bytes", "fsr_latent_attention", "fsr_expanded_workspace_bytes",
     "fsr_latent_attention_expanded", "fsr_shared_workspace_bytes", "fsr_verify_attention_shared",
+    "fsr_kv_append_rope", "fsr_kv_append_rope_kv8", "fsr_tree_workspace_bytes", "fsr_verify_attention_tree", "fsr_tree_accept", "fsr_kv_commit",
+    "fsr_logprob_workspace_bytes", "fsr_token_logprobs",
     "fsr_hbm_read_probe",
 ]
 
@@ -59,6 +61,14 @@ _ARGUMENTS = {
     "fsr_latent_attention_expanded": "t:q t:kv t:k_rope i:cu_q i:cu_k t:out f:lse S:params t:workspace n:ws_bytes n:stream",
     "fsr_verify_attention_shared":
         f"{_ATTENTION} {_LENGTHS} i:cu_q i:cu_groups i:prefix_lens n:n_groups t:out f:lse S:params t:workspace n:ws_bytes n:stream",
+    "fsr_kv_append_rope": f"s:q s:k_new s:v_new f:cos_sin i:positions l:tree_mask t:q_out t:k_cache t:v_cache {_LENGTHS} i:cu_q S:params n:stream",
+    "fsr_kv_append_rope_kv8": "s:q s:k_new s:v_new f:cos_sin i:positions l:tree_mask t:q_out t:k_cache t:v_cache f:k_scale f:v_scale "
+                              f"{_LENGTHS} i:cu_q S:params n:stream",
+    "fsr_verify_attention_tree":
+        f"{_ATTENTION} {_LENGTHS} i:cu_q l:tree_mask n:tree_words t:out f:lse S:params t:workspace n:ws_bytes n:stream",
+    "fsr_tree_accept": "i:target_tokens i:draft_tokens l:tree_mask i:cu_q i:accepted_len i:n_emitted i:emitted i:path b:keep_mask S:params n:stream",
+    "fsr_kv_commit": f"t:k_cache t:v_cache {_LENGTHS} i:accepted_len i:path S:params n:stream",
+    "fsr_token_logprobs": "s:logits i:n_rows i:tokens f:logprobs f:entropy i:top_ids f:top_logprobs S:params t:workspace n:ws_bytes n:stream",
     "fsr_prune_scatter": "t:compact i:src_row i:n_rows t:out n:row_bytes n:N_cap n:stream",
 }
 
@@ -99,6 +109,25 @@ class LatentParams(ctypes.Structure):
 class ExpandedParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "N_cap", "T_cap", "H", "D_nope", "D_rope", "D_v", "dtype", "out_dtype")] + \
                [("scale", ctypes.c_float), ("max_q_len", ctypes.c_int32), ("max_workgroups", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("B", "N_cap", "H_q", "H_kv", "D", "R", "P", "max_pages", "n_pages", "T", "tree_words", "pairs", "dtype", "kv_layout")] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "reserved")]
+
+
+class TreeParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "N_cap", "tree_words", "S_max", "reserved")]
+
+
+class CommitParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H_kv", "row_bytes", "P", "max_pages", "n_pages", "S_max", "kv_layout")]
+
+
+class LogprobParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N_cap", "V", "M", "K", "dtype", "reserved")] + \
+               [("stride", ctypes.c_int64), ("temperature", ctypes.c_double)]
 
 
 def library_path() -> str:
@@ -552,6 +581,177 @@ def shared_workspace_bytes(*, N_cap, H_q, H_kv, D, dtype, out_dtype) -> int:
     p = AttnParams(B=1, N_cap=N_cap, H_q=H_q, H_kv=H_kv, D=D, P=1, max_pages=1, n_pages=1, dtype=_code(dtype), out_dtype=_code(out_dtype),
                    scale=1.0, max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR)
     return _workspace_of("fsr_shared_workspace_bytes", p)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# trees of drafted tokens, and what is reported of the target's rows
+# ---------------------------------------------------------------------------------------------------------------
+TREE_WORDS_MAX, TOP_MAX = 16, 64
+
+
+def _tree_words(tree_mask, N_cap) -> int:
+    if tree_mask.dim() != 2 or tree_mask.shape[0] != N_cap or not 1 <= tree_mask.shape[1] <= TREE_WORDS_MAX:
+        raise ValueError(f"tree_mask must be [{N_cap}, 1 .. {TREE_WORDS_MAX}], got {tuple(tree_mask.shape)}")
+    return tree_mask.shape[1]
+
+
+def _row_stride(t, inner, name) -> int:
+    """Elements from a row to the next of a tensor whose rows are dense (a slice of wider rows, as fused projections give it)."""
+    want = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and stride != want:
+            raise ValueError(f"the rows of {name} must be contiguous")
+        want *= size
+    return inner if t.shape[0] <= 1 else t.stride(0)
+
+
+def _one_of(tensor, shape, dtype, device, name):
+    """The caller's buffer checked, or a new one."""
+    if tensor is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(tensor.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(tensor.shape)}")
+    return tensor
+
+
+def kv_append_rope(q, k_new, v_new, cos_sin, k_cache, v_cache, block_tables, ctx_lens, cu_q, *, positions=None, tree_mask=None, q_out=None, pairs=False,
+                   k_scale=None, v_scale=None, kv_layout=KV_HEAD_MAJOR):
+    """fsr_kv_append_rope: turn the call's rows, q [N_cap, H_q, D] and k_new / v_new [N_cap, H_kv, D] (rows may be slices of wider ones), to
+    their positions by the table cos_sin [T, R] and store keys and values into the paged caches (in place).  Rotary positions: positions
+    [N_cap], or by depth in the trees of tree_mask [N_cap, words] int64, or one behind the other.  k_scale / v_scale [H_kv]: the caches are
+    uint8 tensors of E4M3 bytes -> fsr_kv_append_rope_kv8.  Returns the queries, q_out (may be q)."""
+    B = ctx_lens.shape[0]
+    _check_offsets(B, block_tables, cu_q=cu_q)
+    if q.dim() != 3 or k_new.dim() != 3 or k_cache.dim() != 4 or cos_sin.dim() != 2:
+        raise ValueError("q [N_cap, H_q, D], k_new and v_new [N_cap, H_kv, D], cos_sin [T, R] and caches of four dimensions are wanted")
+    N_cap, H_q, D = q.shape
+    n_pages, a, b, D_c = k_cache.shape
+    P, H_kv = (a, b) if kv_layout == KV_TOKEN_MAJOR else (b, a)
+    if k_new.shape != v_new.shape or tuple(k_new.shape) != (N_cap, H_kv, D) or v_cache.shape != k_cache.shape or D_c != D:
+        raise ValueError("k_new and v_new must be [N_cap, H_kv, D] matching q and the caches")
+    kv8 = k_scale is not None or v_scale is not None
+    if not (q.dtype == k_new.dtype == v_new.dtype) or k_cache.dtype != v_cache.dtype or k_cache.dtype != (torch.uint8 if kv8 else q.dtype):
+        raise ValueError("q, k_new, v_new and the caches must share a dtype (with scales: bf16 rows and uint8 caches)")
+    if kv8 and (k_scale is None or v_scale is None or tuple(k_scale.shape) != (H_kv,) or tuple(v_scale.shape) != (H_kv,)):
+        raise ValueError("k_scale and v_scale need one entry per KV head")
+    if positions is not None and tuple(positions.shape) != (N_cap,):
+        raise ValueError(f"positions must have {N_cap} entries, got {tuple(positions.shape)}")
+    words = _tree_words(tree_mask, N_cap) if tree_mask is not None else 0
+    q_out = _one_of(q_out, q.shape, q.dtype, q.device, "q_out")
+    if q_out.dtype != q.dtype:
+        raise ValueError("q_out must have the dtype of q")
+    _on_current_device(q=q, k_new=k_new, v_new=v_new, cos_sin=cos_sin, positions=positions, tree_mask=tree_mask, q_out=q_out, k_cache=k_cache,
+                       v_cache=v_cache, k_scale=k_scale, v_scale=v_scale, block_tables=block_tables, ctx_lens=ctx_lens, cu_q=cu_q)
+    p = RopeParams(B=B, N_cap=N_cap, H_q=H_q, H_kv=H_kv, D=D, R=cos_sin.shape[1], P=P, max_pages=block_tables.shape[1], n_pages=n_pages,
+                   T=cos_sin.shape[0], tree_words=words, pairs=1 if pairs else 0, dtype=_code(q.dtype), kv_layout=int(kv_layout),
+                   q_stride=_row_stride(q, H_q * D, "q"), k_stride=_row_stride(k_new, H_kv * D, "k_new"),
+                   v_stride=_row_stride(v_new, H_kv * D, "v_new"), reserved=0)
+    if kv8:
+        _call("fsr_kv_append_rope_kv8", q, k_new, v_new, cos_sin, positions, tree_mask, q_out, k_cache, v_cache, k_scale, v_scale, block_tables,
+              ctx_lens, cu_q, p)
+    else:
+        _call("fsr_kv_append_rope", q, k_new, v_new, cos_sin, positions, tree_mask, q_out, k_cache, v_cache, block_tables, ctx_lens, cu_q, p)
+    return q_out
+
+
+def verify_attention_tree(q, k_cache, v_cache, block_tables, ctx_lens, cu_q, tree_mask, *, scale, out=None, lse=None, out_dtype=None, workspace=None,
+                          max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR):
+    """fsr_verify_attention_tree: verify_attention whose rows see the context and the rows of their request that tree_mask [N_cap, words]
+    int64 has a bit for.  Returns (out, lse)."""
+    B = ctx_lens.shape[0]
+    _check_offsets(B, block_tables, cu_q=cu_q)
+    if q.dim() != 3 or k_cache.dim() != 4 or v_cache.shape != k_cache.shape or not (q.dtype == k_cache.dtype == v_cache.dtype):
+        raise ValueError("q, k_cache and v_cache must share dtype; caches must share shape")
+    words = _tree_words(tree_mask, q.shape[0])
+    out, out_dtype = _outputs(tuple(q.shape), out, lse, out_dtype, q.dtype, q.device)
+    p = _attn_params(q, k_cache, block_tables, B, out_dtype, scale, max_q_len, max_workgroups, kv_layout)
+    _on_current_device(q=q, k_cache=k_cache, v_cache=v_cache, block_tables=block_tables, ctx_lens=ctx_lens, cu_q=cu_q, tree_mask=tree_mask, out=out,
+                       lse=lse, workspace=workspace)
+    token = _guard_workspace(workspace)
+    workspace, ws_bytes = _scratch("fsr_tree_workspace_bytes", p, workspace, q.device)
+    _call("fsr_verify_attention_tree", q, k_cache, v_cache, block_tables, ctx_lens, cu_q, tree_mask, words, out, lse, p, workspace, ws_bytes)
+    _note_workspace_use(token)
+    return out, lse
+
+
+def tree_accept(target_tokens, draft_tokens, tree_mask, cu_q, *, S_max, accepted_len=None, n_emitted=None, emitted=None, path=None, keep_mask=None):
+    """fsr_tree_accept.  Returns (accepted_len [B], n_emitted [B], emitted [B, S_max+1], path [B, S_max+1]); keep_mask [N_cap] uint8, if
+    given, receives the rows of the paths."""
+    B, N_cap, dev = cu_q.shape[0] - 1, target_tokens.shape[0], cu_q.device
+    _check_offsets(B, cu_q=cu_q)
+    words = _tree_words(tree_mask, N_cap)
+    if tuple(target_tokens.shape) != (N_cap,) or tuple(draft_tokens.shape) != (N_cap,) or (keep_mask is not None and tuple(keep_mask.shape) != (N_cap,)):
+        raise ValueError("target_tokens, draft_tokens and keep_mask must have one entry per row")
+    if S_max < 0:
+        raise ValueError("S_max must not be negative")
+    accepted_len = _one_of(accepted_len, (B,), torch.int32, dev, "accepted_len")
+    n_emitted = _one_of(n_emitted, (B,), torch.int32, dev, "n_emitted")
+    emitted = _one_of(emitted, (B, S_max + 1), torch.int32, dev, "emitted")
+    path = _one_of(path, (B, S_max + 1), torch.int32, dev, "path")
+    _on_current_device(target_tokens=target_tokens, draft_tokens=draft_tokens, tree_mask=tree_mask, cu_q=cu_q, accepted_len=accepted_len,
+                       n_emitted=n_emitted, emitted=emitted, path=path, keep_mask=keep_mask)
+    p = TreeParams(B=B, N_cap=N_cap, tree_words=words, S_max=int(S_max), reserved=0)
+    _call("fsr_tree_accept", target_tokens, draft_tokens, tree_mask, cu_q, accepted_len, n_emitted, emitted, path, keep_mask, p)
+    return accepted_len, n_emitted, emitted, path
+
+
+def kv_commit(k_cache, v_cache, block_tables, ctx_lens, accepted_len, path, *, kv_layout=KV_HEAD_MAJOR):
+    """fsr_kv_commit: move the keys and values of accepted paths (tree_accept) to the positions behind the context, in place, in caches of
+    any dtype."""
+    B = ctx_lens.shape[0]
+    _check_offsets(B, block_tables)
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+        raise ValueError("the caches must share shape and dtype")
+    if tuple(accepted_len.shape) != (B,) or path.dim() != 2 or path.shape[0] != B or path.shape[1] < 1:
+        raise ValueError(f"accepted_len must be [{B}] and path [{B}, S_max + 1]")
+    _on_current_device(k_cache=k_cache, v_cache=v_cache, block_tables=block_tables, ctx_lens=ctx_lens, accepted_len=accepted_len, path=path)
+    n_pages, a, b, D = k_cache.shape
+    P, H_kv = (a, b) if kv_layout == KV_TOKEN_MAJOR else (b, a)
+    p = CommitParams(B=B, H_kv=H_kv, row_bytes=D * k_cache.element_size(), P=P, max_pages=block_tables.shape[1], n_pages=n_pages,
+                     S_max=path.shape[1] - 1, kv_layout=int(kv_layout))
+    _call("fsr_kv_commit", k_cache, v_cache, block_tables, ctx_lens, accepted_len, path, p)
+
+
+def token_logprobs(logits, tokens=None, *, top_k=0, temperature=1.0, n_rows=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None,
+                   workspace=None):
+    """fsr_token_logprobs.  logits [N_cap, V] (rows may be slices of wider ones), tokens [N_cap] or [N_cap, M] int32, n_rows [1] int32 on the
+    device.  Returns (logprobs like tokens, entropy [N_cap], top_ids [N_cap, top_k], top_logprobs [N_cap, top_k]), None for what is not
+    asked for."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [N_cap, V]")
+    N_cap, V = logits.shape
+    if tokens is not None and (tokens.dim() not in (1, 2) or tokens.shape[0] != N_cap):
+        raise ValueError(f"tokens must be [{N_cap}] or [{N_cap}, M], got {tuple(tokens.shape)}")
+    if n_rows is not None and n_rows.numel() != 1:
+        raise ValueError("n_rows must be one number")
+    M = 0 if tokens is None else 1 if tokens.dim() == 1 else tokens.shape[1]
+    dev = logits.device
+    logprobs = None if tokens is None else _one_of(logprobs, tokens.shape, torch.float32, dev, "logprobs")
+    entropy = _one_of(entropy, (N_cap,), torch.float32, dev, "entropy")
+    top_ids = _one_of(top_ids, (N_cap, top_k), torch.int32, dev, "top_ids") if top_k else None
+    top_logprobs = _one_of(top_logprobs, (N_cap, top_k), torch.float32, dev, "top_logprobs") if top_k else None
+    p = LogprobParams(N_cap=N_cap, V=V, M=M, K=int(top_k), dtype=_code(logits.dtype), reserved=0, stride=_row_stride(logits, V, "logits"),
+                      temperature=float(temperature))
+    _on_current_device(logits=logits, n_rows=n_rows, tokens=tokens, logprobs=logprobs, entropy=entropy, top_ids=top_ids, top_logprobs=top_logprobs,
+                       workspace=workspace)
+    token = _guard_workspace(workspace)
+    workspace, ws_bytes = _scratch("fsr_logprob_workspace_bytes", p, workspace, dev)
+    _call("fsr_token_logprobs", logits, n_rows, tokens, logprobs, entropy, top_ids, top_logprobs, p, workspace, ws_bytes)
+    _note_workspace_use(token)
+    return logprobs, entropy, top_ids, top_logprobs
+
+
+def tree_workspace_bytes(*, N_cap, H_q, H_kv, D, dtype, out_dtype) -> int:
+    """Workspace of verify_attention_tree for calls of up to N_cap rows."""
+    p = AttnParams(B=1, N_cap=N_cap, H_q=H_q, H_kv=H_kv, D=D, P=1, max_pages=1, n_pages=1, dtype=_code(dtype), out_dtype=_code(out_dtype),
+                   scale=1.0, max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR)
+    return _workspace_of("fsr_tree_workspace_bytes", p)
+
+
+def logprob_workspace_bytes(*, N_cap, V, M, K, dtype) -> int:
+    """Workspace of token_logprobs for calls of up to N_cap rows."""
+    p = LogprobParams(N_cap=N_cap, V=V, M=M, K=K, dtype=_code(dtype), reserved=0, stride=V, temperature=1.0)
+    return _workspace_of("fsr_logprob_workspace_bytes", p)
 
 
 def _workspace_of(size_of, p) -> int:

@@ -105,4 +105,30 @@ __device__ __forceinline__ int count_arrival(unsigned long long* word, unsigned 
     }
 }
 
+// Two fp32 values -> two E4M3 bytes in the low or high half of `old`.
+__device__ __forceinline__ uint32_t pack_e4m3(float x, float y, uint32_t old, bool high) {
+    // the conversion instruction rounds to nearest even; saturation and NaN are made explicit here
+    const float cx = fminf(fmaxf(x, -448.0f), 448.0f), cy = fminf(fmaxf(y, -448.0f), 448.0f);
+    uint32_t w = high ? (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(cx, cy, (int)old, true)
+                      : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(cx, cy, (int)old, false);
+    const int sh = high ? 16 : 0;
+    if (x != x) w = (w & ~(0xffu << sh)) | (0x7fu << sh);
+    if (y != y) w = (w & ~(0xffu << (sh + 8))) | (0x7fu << (sh + 8));
+    return w;
+}
+
+// Largest i in [0, B) with cu[i] <= x (requests without rows are skipped), found by a whole wave: 64 offsets at a time, one round trip
+// to memory up to 64 requests.  For cu[0] <= x < cu[B]; whatever the offsets hold, the answer lies in [0, B).
+__device__ __forceinline__ int owner_by_wave(const int32_t* __restrict__ cu, int B, int x) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+        const int before = __popcll(__ballot(at < hi && cu[min(at, hi - 1)] <= x));
+        lo += max(before - 1, 0) * step;
+        hi = min(lo + step, hi);
+    }
+    return lo;
+}
+
 }  // namespace fsr

@@ -8,6 +8,7 @@
 #include <cstdint>
 
 #include "common.hpp"
+#include "device_utils.hpp"
 
 namespace fsr {
 namespace {
@@ -75,18 +76,6 @@ struct Append8Args {
 };
 
 __device__ __forceinline__ float bf16_bits_to_float(uint32_t h) { return __builtin_bit_cast(float, h << 16); }
-
-// Two fp32 values -> two E4M3 bytes in the low or high half of `old`.
-__device__ __forceinline__ uint32_t pack_e4m3(float x, float y, uint32_t old, bool high) {
-    // the conversion instruction rounds to nearest even; saturation and NaN are made explicit here
-    const float cx = fminf(fmaxf(x, -448.0f), 448.0f), cy = fminf(fmaxf(y, -448.0f), 448.0f);
-    uint32_t w = high ? (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(cx, cy, (int)old, true)
-                      : (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(cx, cy, (int)old, false);
-    const int sh = high ? 16 : 0;
-    if (x != x) w = (w & ~(0xffu << sh)) | (0x7fu << sh);
-    if (y != y) w = (w & ~(0xffu << (sh + 8))) | (0x7fu << (sh + 8));
-    return w;
-}
 
 __device__ __forceinline__ u32x4 quantise16(const uint16_t* src, float scale) {
     // (elements to scalars before use: see rank_check.hip on bit casts of vector-element expressions)

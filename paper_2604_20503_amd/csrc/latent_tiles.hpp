@@ -423,7 +423,7 @@ __device__ __forceinline__ void run_latent(const Args& a, const Piece& p, char* 
             const float inv = inverse(l);
 #pragma unroll
             for (int k = 0; k < C::kDv / 256; ++k) store4((typename C::Out*)a.out + (row0 + r) * C::kDv + 4 * (k * 64 + lane), x[k] * inv);
-            if (lane == 0 && a.lse) a.lse[row0 + r] = log_sum(of, l, a.scale);
+            if (lane == 0 && a.lse) a.lse[row0 + r] = log_sum<kLatent>(of, l, a.scale);
         } else {
 #pragma unroll
             for (int k = 0; k < C::kDv / 256; ++k) store4(a.part_o + (slot0 + r) * C::kDv + 4 * (k * 64 + lane), x[k]);

@@ -4,8 +4,8 @@
 // tensor in Python and passed through ctypes cost as much again (host time of one layer's append and attention, 17 tensors: 18.6 us so, 14.8 here; of an
 // early exit's rank check, compaction and restore 30.2 and 17.0).
 //
-// Argument kinds: 't' any tensor, 'f' 'i' 'b' 'l' tensor of float32 / int32 / uint8 / int64 (all: or None, a null pointer),
-// 'S' an object with a buffer (a ctypes structure), 'n' an integer.
+// Argument kinds: 't' any tensor, 's' one whose strides the binding has looked at, 'f' 'i' 'b' 'l' tensor of float32 / int32 / uint8 /
+// int64 (all: or None, a null pointer), 'S' an object with a buffer (a ctypes structure), 'n' an integer.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -60,7 +60,7 @@ bool address_of(PyObject* o, char kind, const std::string& name, uint64_t& out) 
             PyErr_Format(PyExc_ValueError, "%s must live on the GPU", name.c_str());
             return false;
         }
-        if (!t.is_contiguous()) {
+        if (kind != 's' && !t.is_contiguous()) {
             PyErr_Format(PyExc_ValueError, "%s must be contiguous", name.c_str());
             return false;
         }
@@ -139,8 +139,8 @@ PyObject* make(PyObject*, PyObject* args) {
     const std::string k(kinds);
     size_t buffers = 0;
     for (char x : k) buffers += x == 'S';
-    if ((Py_ssize_t)k.size() != PyTuple_GET_SIZE(names) || k.size() > kMaxArgs || buffers > 2 || k.find_first_not_of("tfiblSn") != std::string::npos) {
-        PyErr_SetString(PyExc_ValueError, "one name for each of at most 20 kinds out of t f i b l S n, at most two of them S");
+    if ((Py_ssize_t)k.size() != PyTuple_GET_SIZE(names) || k.size() > kMaxArgs || buffers > 2 || k.find_first_not_of("tsfiblSn") != std::string::npos) {
+        PyErr_SetString(PyExc_ValueError, "one name for each of at most 20 kinds out of t s f i b l S n, at most two of them S");
         return nullptr;
     }
     std::vector<std::string> list;

@@ -1,5 +1,5 @@
-// Attention of many query rows on one stream of keys: what attention over a latent cache, its expanded form and attention
-// behind a shared prefix have in common.
+// Attention of many query rows on one stream of keys: what attention over a latent cache, its expanded form, attention
+// behind a shared prefix and attention of trees have in common.
 //
 // A *sequence* is a set of query rows that read the same keys (a request's rows, or all rows of the requests that share a
 // prefix); per stream head, G query heads of a call row read the same key.  The rows of a sequence are packed (packed row r =
@@ -43,7 +43,7 @@ constexpr int kEvenRounds = 3;       // latent: most pieces of a workgroup in a 
 constexpr int kRefPlace = 10, kRefPrefix = 1 << 24;  // fields of a reference to a part of a row: its place in the tile; there is a prefix before it
 constexpr float kAhead = 40.0f;    // distance of a row's exponent reference from its largest score, in powers of two
 
-enum : int { kLatent = 0, kExpanded = 1, kShared = 2 };
+enum : int { kLatent = 0, kExpanded = 1, kShared = 2, kTree = 3 };
 
 struct Args {
     const void* q;       // [N_cap, H, D_k]
@@ -56,6 +56,8 @@ struct Args {
     const int32_t* cu_k;      // expanded: offsets of the keys
     const int32_t* cu_groups; // shared
     const int32_t* prefix;    // shared
+    const uint32_t* tree;     // tree: [N_cap][tree_words] the rows of its request that a row sees, a bit each
+    int tree_words;
     void* out;
     float* lse;
     int B, N_cap, H, H_stream, G, n_groups, T_cap;
@@ -78,7 +80,7 @@ struct Seq {
     int row0, rows;      // call rows
     int k_begin, k_end;  // keys (tiles begin at k_begin)
     int k_first;         // the first one that is seen
-    int base;            // packed row r sees keys up to base + r / G
+    int base;            // packed row r sees keys up to base + r / G (tree: the keys in front of base, and of the others what its bits say)
     int table;           // row of the block table
     uint32_t first;      // expanded: slot of the first key
 };
@@ -323,7 +325,12 @@ __device__ __forceinline__ Reference reference_for(float top, float scale_log2) 
 }
 
 // Logarithm of the sum of exp of the scores whose weights add up to l, -inf without any weight.
+// (Trees: the powers of two of reference and sum are added first.  A reference is 2^40 ahead, the sum as much smaller, and logarithms of
+// that size are off by 2.6e-6 each.)
+template <int OP>
 __device__ __forceinline__ float log_sum(Reference of, float l, float scale) {
+    if constexpr (OP == kTree)
+        return l == 0.0f ? -INFINITY : fmaf(of.raw, scale, ((of.log2 + (float)__builtin_amdgcn_frexp_expf(l)) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l))) * kLn2);
     return l == 0.0f ? -INFINITY : fmaf(of.raw, scale, of.log2 * kLn2) + __builtin_amdgcn_logf(l) * kLn2;
 }
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
@@ -372,7 +379,7 @@ __device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_t
     if (to.out) {
         const float inv = inverse(l);
         each([&](int d, f32x4 x) { store4(to.out + d, x * inv); });
-        if (first_lane && to.lse) *to.lse = log_sum(of, l, a.scale);
+        if (first_lane && to.lse) *to.lse = log_sum<C::kOp>(of, l, a.scale);
     } else {
         each([&](int d, f32x4 x) { store4(to.sums + d, x); });
         if (first_lane) store4(to.ml, f32x4{of.raw, of.log2, l, 0.0f});
@@ -396,9 +403,27 @@ struct Simple {
     typedef float Out;
 };
 
-// Last key that packed row r sees.
+// Last key that packed row r sees (of a tree: that it may see).
+template <int OP = kLatent>
 __device__ __forceinline__ int last_key(const Args& a, const Seq& q, int r) {
+    if constexpr (OP == kTree) return q.k_end - 1;
     return min(q.k_end - 1, q.base + (int)((uint32_t)r / (uint32_t)a.G));
+}
+// The last one up to which it sees them all.
+template <int OP>
+__device__ __forceinline__ int last_common_key(const Args& a, const Seq& q, int r) {
+    if constexpr (OP == kTree) return q.base - 1;
+    return last_key<OP>(a, q, r);
+}
+
+// Which of the 32 keys from `key` on a row of a tree sees, a bit each: the keys in front of `base` and what the row's bits say (bits that
+// the mask does not hold are zero).
+__device__ __forceinline__ uint32_t tree_window(const uint32_t* row, int words, int base, int key) {
+    const int off = key - base;
+    if (off <= -32) return 0xffffffffu;
+    const int w = off >> 5, sh = off & 31;  // (off < 0: word -1 is all ones)
+    const uint32_t lo = w < 0 ? 0xffffffffu : w < words ? row[w] : 0u, hi = w + 1 < words ? row[w + 1] : 0u;
+    return (uint32_t)((((uint64_t)hi << 32) | lo) >> sh);
 }
 
 template <class C>
@@ -412,7 +437,8 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
     f32x4 q[C::kDk / 16];
 #pragma unroll
     for (int s = 0; s < C::kDk / 16; ++s) q[s] = *reinterpret_cast<const f32x4*>(qp + 16 * s + 4 * lg);
-    const int seen = last_key(a, p.q, r);
+    const int seen = last_key<C::kOp>(a, p.q, r);
+    const uint32_t* tree = C::kOp == kTree ? a.tree + (size_t)at.row * a.tree_words : nullptr;
     f32x4 acc[C::kDv / 16];
 #pragma unroll
     for (int b = 0; b < C::kDv / 16; ++b) acc[b] = f32x4{0, 0, 0, 0};
@@ -457,10 +483,14 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) key[s] = key_of(slot, s);
         float top = -INFINITY;
+        const uint32_t window = C::kOp == kTree ? tree_window(tree, a.tree_words, p.q.base, kb) : 0xffffffffu;
+        auto sees_key = [&](int e) {
+            const int key = kb + 4 * lg + e;
+            return key >= p.q.k_first && key <= seen && key < k_last && (C::kOp != kTree || (window >> (4 * lg + e) & 1));
+        };
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int key = kb + 4 * lg + e;
-            z[e] = key >= p.q.k_first && key <= seen && key < k_last ? z[e] : -INFINITY;
+            z[e] = sees_key(e) ? z[e] : -INFINITY;
             top = fmaxf(top, z[e]);
         }
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
@@ -475,7 +505,7 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
         m = m_new;
 #pragma unroll
         for (int b = 0; b < C::kDv / 16; ++b) acc[b] *= alpha;
-        const bool masked = __any(kb + 15 > seen || kb + 15 >= k_last || kb < p.q.k_first);
+        const bool masked = __any(kb + 15 > seen || kb + 15 >= k_last || kb < p.q.k_first || (C::kOp == kTree && (window & 0xffffu) != 0xffffu));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float v[kBlocks];
@@ -485,7 +515,7 @@ __device__ __forceinline__ void run_simple(const Args& a, const Piece& p) {
                 v[b] = kEarly ? value[kEarly ? e : 0][b] : value_of(now, e, b);
                 odd |= (__builtin_bit_cast(uint32_t, v[b]) & 0x7f800000u) == 0x7f800000u;
             }
-            const float sees = kb + 4 * lg + e >= p.q.k_first && kb + 4 * lg + e <= seen && kb + 4 * lg + e < k_last ? 1.0f : 0.0f;
+            const float sees = sees_key(e) ? 1.0f : 0.0f;
             if (!masked || !__any(odd)) {
 #pragma unroll
                 for (int b = 0; b < C::kDv / 16; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b], x[e], acc[b], 0, 0, 0);
@@ -733,6 +763,8 @@ struct Rows {
     Reference of;        // of the row's weights
     float l;             // sum of this lane's weights
     int seen;            // last key of the lane's row
+    const uint32_t* tree; // tree: the row's bits
+    int tree_words, tree_base;
     int k_at[kOwnK], tail_at[std::max(kTailSteps, 1)], v_at[kOwnV];
 
     __device__ __forceinline__ void place_operands(int lane) {
@@ -854,10 +886,11 @@ __device__ __forceinline__ void take_any_keys(Rows<C>& w, const char* buf, int b
     typedef Rows<C> R;
     const int h = lane >> 5;
     f32x16 z = scores_of<C>(w, buf, block, [](int) {});
+    const uint32_t window = C::kOp == kTree ? tree_window(w.tree, w.tree_words, w.tree_base, key0) : 0;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        const int key = key0 + 8 * (e >> 2) + 4 * h + (e & 3);
-        z[e] = key >= k_first && key <= w.seen ? z[e] : -INFINITY;
+        const int at = 8 * (e >> 2) + 4 * h + (e & 3), key = key0 + at;
+        z[e] = key >= k_first && key <= w.seen && (C::kOp != kTree || (window >> at & 1)) ? z[e] : -INFINITY;
     }
     const float top = largest(z);
     // The reference keeps a distance above the largest score and is moved only when a score overtakes it: weights stay below one,
@@ -898,7 +931,8 @@ __device__ __forceinline__ void take_any_keys(Rows<C>& w, const char* buf, int b
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int key = first_key + 16 * s + 8 * (k >> 1) + 2 * (k & 1);
-                        one[k] = (key >= k_first && key <= w.seen ? 0x3f80u : 0u) | (key + 1 >= k_first && key + 1 <= w.seen ? 0x3f800000u : 0u);
+                        const uint32_t bits = C::kOp == kTree ? window >> (key - key0) : 3u;
+                        one[k] = (key >= k_first && key <= w.seen && (bits & 1) ? 0x3f80u : 0u) | (key + 1 >= k_first && key + 1 <= w.seen && (bits & 2) ? 0x3f800000u : 0u);
                     }
                     return __builtin_bit_cast(bf16x8, one);
                 };
@@ -933,9 +967,14 @@ __device__ __forceinline__ bool run_tiled(const Args& a, const Piece& p, char* b
         const uint16_t* qp = (const uint16_t*)a.q + ((size_t)at.row * a.H + at.head) * C::kDk;
 #pragma unroll
         for (int s = 0; s < C::kDk / 16; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * h);
-        w.seen = last_key(a, p.q, r);
-        seen_first = last_key(a, p.q, first);
-        seen_last = last_key(a, p.q, min(first + 31, n_packed - 1));
+        w.seen = last_key<C::kOp>(a, p.q, r);
+        if constexpr (C::kOp == kTree) {
+            w.tree = a.tree + (size_t)at.row * a.tree_words;
+            w.tree_words = a.tree_words;
+            w.tree_base = p.q.base;
+        }
+        seen_first = last_common_key<C::kOp>(a, p.q, first);
+        seen_last = last_key<C::kOp>(a, p.q, min(first + 31, n_packed - 1));
     }
     TileLoads<C> loads;
     loads.place_lane(a, lane);
@@ -1227,7 +1266,7 @@ __device__ __forceinline__ void join(const Args& a, int pieces, SourceOf source,
         }
         __builtin_memcpy(out + v * 64 * kVector + lane * kVector, y, sizeof y);
     }
-    if (lse && lane == 0) *lse = log_sum(of, l, a.scale);
+    if (lse && lane == 0) *lse = log_sum<C::kOp>(of, l, a.scale);
 }
 
 // Joins the item of which a share has the first piece and others have more.  blockIdx.x: share, blockIdx.y: rows of the tile, kWaves at a time.
