@@ -2,6 +2,12 @@
 //     x_v = (z_v - m) / T with m the row's largest logit,  S = sum_v exp x_v
 //     log p_v = x_v - log S,   H = log S - sum_v exp(x_v) x_v / S
 // Differences are taken before they are scaled, so that logits of any size keep their digits; H is a sum of terms of one sign.
+//
+// One pass over the logits: a row is cut into chunks, a workgroup takes a chunk tile by tile, a thread a *group* of 32 bytes of each
+// tile.  Beside its running (m, S, sum) it leaves the largest logit of every group in LDS, and nothing else is done for the
+// alternatives while the logits go by.  The K largest of a chunk lie in the K groups whose largest logits come first: with
+// keys (logit, lowest id) any K groups that come before a group hold K logits that come before all of that group's.  Those groups are
+// found in LDS and read once more, 32 K bytes.  The workgroup of a row that is done last joins the chunks.
 #include <algorithm>
 #include <cstdint>
 
@@ -27,7 +33,19 @@ struct LogprobArgs {
     int N_cap, V, M, K;
     float scale;   // log2(e) / T
     double inv_t;
+    int chunks, tiles;  // of a row, of a chunk
+    unsigned long long* arrivals;  // [N_cap]
+    uint64_t* stats;    // [N_cap * chunks][3]: m, S, sum of S's terms times x, as doubles
+    uint64_t* keys;     // [N_cap * chunks][K]
+    unsigned long long call_id;
 };
+
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+
+// What another workgroup of the launch reads: stored through to memory, loaded past the caches.
+__device__ __forceinline__ void publish(uint64_t* p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint64_t fetch(const uint64_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 __device__ __forceinline__ float value_of(const float* p) { return *p; }
 __device__ __forceinline__ float value_of(const uint16_t* p) { return __builtin_bit_cast(float, (uint32_t)*p << 16); }
@@ -44,46 +62,265 @@ __device__ __forceinline__ float value_of_key(uint64_t key) {
 }
 __device__ __forceinline__ int id_of_key(uint64_t key) { return (int)~(uint32_t)key; }
 
-// A workgroup a row; K more passes over the row for the alternatives.
+constexpr int kTilesMax = 32;    // of a chunk
+constexpr int kChunksMax = 64;   // of a row
+constexpr int kWorkgroups = 1024; // that a call is cut into, if its rows are fewer
+constexpr int kGroupsMax = 512;  // groups that may hold alternatives, listed
+constexpr float kLeast = -200.0f; // least power of two that is told from no weight at all
+static_assert((long long)kTilesMax * kChunksMax * kThreads * 8 == 1 << 22, "longest row of fp32");
+
+// Eight or sixteen logits: 32 bytes.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void logprob_row_kernel(LogprobArgs a) {
-    __shared__ double sums[2][kThreads / kWave];
-    __shared__ uint64_t keys[kThreads / kWave];
-    const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+struct Group;
+template <>
+struct Group<float> {
+    static constexpr int kN = 8;
+    f32x4 a, b;
+    __device__ __forceinline__ void load(const float* p) { __builtin_memcpy(&a, p, 16); __builtin_memcpy(&b, p + 4, 16); }
+    __device__ __forceinline__ float get(int k) const { return k < 4 ? a[k] : b[k - 4]; }
+};
+template <>
+struct Group<uint16_t> {
+    static constexpr int kN = 16;
+    u32x4 a, b;
+    __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(&a, p, 16); __builtin_memcpy(&b, p + 8, 16); }
+    __device__ __forceinline__ float get(int k) const {
+        const uint32_t w = k < 8 ? a[k >> 1] : b[(k - 8) >> 1];
+        return __builtin_bit_cast(float, k & 1 ? w & 0xffff0000u : w << 16);
+    }
+};
+
+// Sums of weights 2^x and of weights times x, x = (z - m) * scale.
+struct Sums {
+    float m, s, e;
+    // Refers them to a larger logit.
+    __device__ __forceinline__ void refer(float to, float scale) {
+        const float d = fmaxf((m - to) * scale, kLeast), w = __builtin_amdgcn_exp2f(d);
+        e = fmaf(d, s, e) * w;
+        s *= w;
+        m = to;
+    }
+    template <int N, class Get>
+    __device__ __forceinline__ void add(Get get, float top, float scale) {
+        if (__any(top > m)) {
+            if (top > m) refer(top, scale);
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float x = fmaxf((get(k) - m) * scale, kLeast);  // (NaN, -inf: no weight)
+            const float w = __builtin_amdgcn_exp2f(x);
+            s += w;
+            e = fmaf(w, x, e);
+        }
+    }
+};
+
+__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int o) {
+    return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, kWave) << 32 | (uint32_t)__shfl_xor((int)v, o, kWave);
+}
+
+struct Shared {
+    double s[kThreads / kWave], e[kThreads / kWave];
+    float m[kThreads / kWave];
+    uint64_t key[kThreads / kWave];
+    int count[kThreads / kWave], n, last;
+    int chosen[FSR_TOP_MAX];
+    uint64_t top[FSR_TOP_MAX];
+    uint64_t list[kGroupsMax];
+};
+
+// The K largest of n keys (all different, or 0: none), in descending order; 0 behind the last one.  Called by the whole workgroup, whose
+// keys are in LDS behind a barrier; top is there behind the next one.
+__device__ __forceinline__ void rank(const uint64_t* keys, int n, int K, uint64_t* top) {
+    for (int k = threadIdx.x; k < K; k += kThreads) top[k] = 0;
+    __syncthreads();
+    for (int c = threadIdx.x; c < n; c += kThreads) {
+        const uint64_t mine = keys[c];
+        int before = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) before += keys[j] > mine;
+        if (mine != 0 && before < K) top[before] = mine;
+    }
+}
+
+// Groups in descending order of their largest logits, the first of them first among equals.
+__device__ __forceinline__ uint64_t group_key(float top, int tile) { return key_of(top, tile * kThreads + threadIdx.x); }
+
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
+    typedef Group<T> G;
+    constexpr int N = G::kN, kTile = kThreads * N, kWaves = kThreads / kWave, kAtOnce = 4;
+    extern __shared__ __align__(16) char room[];  // largest logits of the groups, then keys
+    __shared__ Shared sh;
+    float* tops = reinterpret_cast<float*>(room);
+    uint64_t* keys = reinterpret_cast<uint64_t*>(room);
+    const int row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (a.n_rows && row >= a.n_rows[0]) return;
     const T* z = (const T*)a.logits + row * a.stride;
-    auto best_below = [&](uint64_t bound) {
-        uint64_t best = 0;
-        for (int v = threadIdx.x; v < a.V; v += kThreads) {
-            const uint64_t k = key_of(value_of(z + v), v);
-            if (k < bound && k > best) best = k;
+    const int first = chunk * a.tiles * kTile, tiles = min(a.tiles, (a.V - first + kTile - 1) / kTile);
+    Sums sums{-3.402823466e38f, 0.0f, 0.0f};
+    float best = -INFINITY;
+    int best_tile = 0;
+    bool any = false;
+    auto take = [&](int t, int n, auto get) __attribute__((always_inline)) {  // n logits of the group: 0, or the row ends in it
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < N; ++k) top = fmaxf(top, __builtin_canonicalizef(get(k)));  // (a signalling NaN would take the largest one's place)
+        sums.add<N>(get, top, a.scale);
+        if (TOP) {
+            tops[t * kThreads + threadIdx.x] = top;
+            if (n > 0 && (!any || top > best)) { best = top; best_tile = t; any = true; }
         }
-        for (int o = 32; o > 0; o >>= 1) {
-            const uint64_t other = (uint64_t)(uint32_t)__shfl_xor((int)(best >> 32), o, kWave) << 32 | (uint32_t)__shfl_xor((int)best, o, kWave);
-            best = other > best ? other : best;
-        }
-        __syncthreads();
-        if (lane == 0) keys[wave] = best;
-        __syncthreads();
-        for (int w = 0; w < kThreads / kWave; ++w) best = keys[w] > best ? keys[w] : best;
-        return best;
     };
-    const uint64_t first = best_below(~0ull);
-    const float m = value_of_key(first);
-    float s = 0.0f, e = 0.0f;
-    for (int v = threadIdx.x; v < a.V; v += kThreads) {
-        const float x = fmaxf((value_of(z + v) - m) * a.scale, -200.0f);  // (NaN, -inf: no weight)
-        const float w = __builtin_amdgcn_exp2f(x);
-        s += w;
-        e = fmaf(w, x, e);
+    const int mine = first + threadIdx.x * N;
+    int t = 0;
+    const int whole = min(tiles, (a.V - first) / kTile);
+    for (; t + kAtOnce <= whole; t += kAtOnce) {
+        G g[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) g[k].load(z + mine + (t + k) * kTile);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) take(t + k, N, [&](int i) __attribute__((always_inline)) { return g[k].get(i); });
     }
-    const double ws = wave_sum((double)s), we = wave_sum((double)e);
-    if (lane == 0) { sums[0][wave] = ws; sums[1][wave] = we; }
+    for (; t < whole; ++t) {
+        G g;
+        g.load(z + mine + t * kTile);
+        take(t, N, [&](int i) __attribute__((always_inline)) { return g.get(i); });
+    }
+    if (t < tiles) {  // the row ends in this tile
+        const int at = mine + t * kTile, n = min(max(a.V - at, 0), N);
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = i < n ? value_of(z + at + i) : -INFINITY;
+        take(t, n, [&](int i) __attribute__((always_inline)) { return v[i]; });
+    }
+
+    // sums of the chunk
+    const float wave_m = wave_max(sums.m);
+    if (lane == 0) sh.m[wave] = wave_m;
+    if (threadIdx.x == 0) sh.n = 0;
+    uint64_t least = ~0ull;  // of the threads' sets of 8 (4): the largest key of a set, the least of those of all sets
+    if (TOP) {
+        uint64_t k = any ? key_of(best, best_tile * kThreads + threadIdx.x) : 0;
+        const int set = a.K <= kThreads / 8 ? 8 : 4;
+        for (int o = 1; o < set; o <<= 1) { const uint64_t other = shfl_xor64(k, o); k = other > k ? other : k; }
+        for (int o = set; o < kWave; o <<= 1) { const uint64_t other = shfl_xor64(k, o); k = other < k ? other : k; }
+        if (lane == 0) sh.key[wave] = k;
+    }
+    __syncthreads();
+    float m = sh.m[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sh.m[w]);
+    sums.refer(m, a.scale);
+    const double ws = wave_sum((double)sums.s), we = wave_sum((double)sums.e);
+    if (lane == 0) { sh.s[wave] = ws; sh.e[wave] = we; }
+    if (TOP) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) least = sh.key[w] < least ? sh.key[w] : least;
+        // (at least K groups come before it or are it, if there are so many)
+        auto has = [&](int t) { return first + t * kTile + (int)threadIdx.x * N < a.V; };
+        for (int t = 0; t < tiles; ++t) {
+            const uint64_t k = has(t) ? group_key(tops[t * kThreads + threadIdx.x], t) : 0;
+            if (k != 0 && k >= least) {
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < kGroupsMax) sh.list[at] = k;
+            }
+        }
+        __syncthreads();
+        int n = sh.n;
+        if (n > kGroupsMax) {
+            // Many groups of few threads: the K-th key, bit by bit.
+            uint64_t kth = 0;
+            for (int bit = 63; bit >= 0; --bit) {
+                const uint64_t probe = kth | 1ull << bit;
+                int c = 0;
+                for (int t = 0; t < tiles; ++t) c += has(t) && group_key(tops[t * kThreads + threadIdx.x], t) >= probe;
+                c = wave_sum_i(c);
+                if (lane == 0) sh.count[wave] = c;
+                __syncthreads();
+                c = 0;
+                for (int w = 0; w < kWaves; ++w) c += sh.count[w];
+                if (c >= a.K) kth = probe;
+                __syncthreads();
+            }
+            if (threadIdx.x == 0) sh.n = 0;
+            __syncthreads();
+            for (int t = 0; t < tiles; ++t) {
+                const uint64_t k = has(t) ? group_key(tops[t * kThreads + threadIdx.x], t) : 0;
+                if (k != 0 && k >= kth) sh.list[min(atomicAdd(&sh.n, 1), kGroupsMax - 1)] = k;
+            }
+            __syncthreads();
+            n = sh.n;
+        }
+        rank(sh.list, n, a.K, sh.top);
+        __syncthreads();
+        // the logits of those groups that are not below the last group's largest one (of fewer than K groups: all)
+        const int groups = min(n, a.K);
+        const uint64_t bound = groups == a.K ? sh.top[groups - 1] >> 32 << 32 : 0;
+        if (threadIdx.x == 0) sh.n = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < groups * N; i += kThreads) {
+            const int id = first + id_of_key(sh.top[i / N]) * N + i % N;
+            const uint64_t k = id < a.V ? key_of(value_of(z + id), id) : 0;
+            if (k >= bound && k != 0) keys[atomicAdd(&sh.n, 1)] = k;
+        }
+        __syncthreads();
+        n = sh.n;
+        rank(keys, n, a.K, sh.top);
+    }
     __syncthreads();
     double S = 0.0, E = 0.0;
-    for (int w = 0; w < kThreads / kWave; ++w) { S += sums[0][w]; E += sums[1][w]; }
-    const bool none = !(fabsf(m) < INFINITY);  // no finite logit, or one that is infinite
-    const double log_s = none ? __builtin_nan("") : log(S);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) { S += sh.s[w]; E += sh.e[w]; }
+
+    if (a.chunks > 1) {
+        const size_t entry = (size_t)row * a.chunks + chunk;
+        if (threadIdx.x == 0) {
+            publish(a.stats + 3 * entry, __builtin_bit_cast(uint64_t, (double)m));
+            publish(a.stats + 3 * entry + 1, __builtin_bit_cast(uint64_t, S));
+            publish(a.stats + 3 * entry + 2, __builtin_bit_cast(uint64_t, E));
+        }
+        if (TOP)
+            for (int k = threadIdx.x; k < a.K; k += kThreads) publish(a.keys + entry * a.K + k, sh.top[k]);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the chunk is in memory once every wave's stores are acknowledged
+        __syncthreads();
+        if (threadIdx.x == 0) sh.last = count_arrival(a.arrivals + row, a.call_id) == a.chunks;
+        __syncthreads();
+        if (!sh.last) return;
+        // The chunks' sums, one a lane (every wave for itself), in an order that does not depend on who was last.
+        const bool in = lane < a.chunks;
+        const size_t theirs = (size_t)row * a.chunks + min(lane, a.chunks - 1);
+        const double cm = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs)), cs = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 1)),
+                     ce = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 2));
+        m = wave_max(in ? (float)cm : -3.402823466e38f);
+        const float d = fmaxf(((float)cm - m) * a.scale, kLeast);
+        const double w = in ? (double)__builtin_amdgcn_exp2f(d) : 0.0;
+        S = wave_sum(w * cs);
+        E = wave_sum(w * (ce + (double)d * cs));
+        if (TOP) {
+            uint64_t bound = 1;  // the largest of the chunks' last ones: K keys are not below it
+            for (int c = threadIdx.x; c < a.chunks; c += kThreads) {
+                const uint64_t k = fetch(a.keys + ((size_t)row * a.chunks + c) * a.K + a.K - 1);
+                bound = k > bound ? k : bound;
+            }
+            for (int o = 1; o < kWave; o <<= 1) { const uint64_t other = shfl_xor64(bound, o); bound = other > bound ? other : bound; }
+            if (lane == 0) sh.key[wave] = bound;
+            if (threadIdx.x == 0) sh.n = 0;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) bound = sh.key[w] > bound ? sh.key[w] : bound;
+            for (int i = threadIdx.x; i < a.chunks * a.K; i += kThreads) {
+                const uint64_t k = fetch(a.keys + (size_t)row * a.chunks * a.K + i);
+                if (k >= bound) keys[atomicAdd(&sh.n, 1)] = k;
+            }
+            __syncthreads();
+            const int n = sh.n;
+            rank(keys, n, a.K, sh.top);
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) __hip_atomic_store(a.arrivals + row, a.call_id << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for a graph's next replay
+    }
+    const double log_s = S > 0.0 ? log(S) : __builtin_nan("");  // (no finite logit, or an infinite one: no sum)
     auto logprob = [&](float zv) { return (float)(((double)zv - (double)m) * a.inv_t - log_s); };
     if (threadIdx.x == 0 && a.entropy) a.entropy[row] = (float)(log_s - E / S * kLn2);
     for (int t = threadIdx.x; t < a.M; t += kThreads) {
@@ -92,14 +329,46 @@ __global__ __launch_bounds__(kThreads) void logprob_row_kernel(LogprobArgs a) {
         if (zv != zv) zv = -INFINITY;
         a.logprobs[(size_t)row * a.M + t] = logprob(zv);
     }
-    uint64_t key = first;
-    for (int k = 0; k < a.K; ++k) {
-        if (k) key = best_below(key);
-        if (threadIdx.x == 0) {
-            a.top_ids[(size_t)row * a.K + k] = id_of_key(key);
-            a.top_logprobs[(size_t)row * a.K + k] = logprob(value_of_key(key));
+    if (TOP)
+        for (int k = threadIdx.x; k < a.K; k += kThreads) {
+            a.top_ids[(size_t)row * a.K + k] = id_of_key(sh.top[k]);
+            a.top_logprobs[(size_t)row * a.K + k] = logprob(value_of_key(sh.top[k]));
         }
+}
+
+// How a call is cut, and its workspace: arrivals [rows], (m, S, sum) [entries][3], keys [entries][K].
+struct Cut {
+    int chunks, tiles;  // of a row, of a chunk
+    size_t arrivals, stats, keys, total;
+};
+Cut cut(const fsr_logprob_params* p) {
+    const int tile = kThreads * (p->dtype == FSR_F32 ? 8 : 16), all = (p->V + tile - 1) / tile, least = (all + kTilesMax - 1) / kTilesMax;
+    const long long n = std::max(p->N_cap, 1);
+    const int most = std::min(all, kChunksMax);
+    const int wanted = std::max(least, (int)std::min((long long)most, (kWorkgroups + n - 1) / n));
+    Cut c;
+    c.tiles = (all + wanted - 1) / wanted;
+    c.chunks = (all + c.tiles - 1) / c.tiles;
+    // (rows times chunks of no smaller call are more)
+    const size_t entries = (size_t)std::max(n * least, std::min(n * most, kWorkgroups + n));
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t x = at; at += align_up(bytes, 256); return x; };
+    c.arrivals = take(n * 8);
+    c.stats = take(entries * 24);
+    c.keys = take(entries * p->K * 8);
+    c.total = at;
+    return c;
+}
+
+template <typename T>
+void launch(const LogprobArgs& a, void* stream) {
+    const dim3 grid((unsigned)((long long)a.N_cap * a.chunks));
+    if (a.K == 0) {
+        hipLaunchKernelGGL((logprob_kernel<T, false>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+        return;
     }
+    const size_t room = std::max({(size_t)a.tiles * kThreads * 4, (size_t)a.K * Group<T>::kN * 8, a.chunks > 1 ? (size_t)a.chunks * a.K * 8 : 0});
+    hipLaunchKernelGGL((logprob_kernel<T, true>), grid, dim3(kThreads), room, (hipStream_t)stream, a);
 }
 
 int check(const fsr_logprob_params* p, const char* who) {
@@ -112,6 +381,8 @@ int check(const fsr_logprob_params* p, const char* who) {
     if (p->stride < p->V) return fail(FSR_ESHAPE, "%s: rows overlap (stride=%lld V=%d)", who, (long long)p->stride, p->V);
     if (!(p->temperature >= 1e-6) || !(p->temperature <= 1e6)) return fail(FSR_EINVAL, "%s: temperature=%g must be 1e-6 .. 1e6", who, p->temperature);
     if (p->N_cap > (1 << 22)) return fail(FSR_EUNSUP, "%s: N_cap=%d exceeds 2^22 rows", who, p->N_cap);
+    if (p->V > (1 << 22)) return fail(FSR_EUNSUP, "%s: V=%d exceeds 2^22 logits", who, p->V);
+    if ((long long)p->N_cap * cut(p).chunks > (1 << 23)) return fail(FSR_EUNSUP, "%s: N_cap=%d rows of V=%d logits are too many for one launch", who, p->N_cap, p->V);
     return FSR_OK;
 }
 
@@ -124,7 +395,7 @@ extern "C" int fsr_logprob_workspace_bytes(const fsr_logprob_params* p, size_t* 
     int rc = check(p, "fsr_logprob_workspace_bytes");
     if (rc != FSR_OK) return rc;
     if (!out_bytes) return fail(FSR_EINVAL, "fsr_logprob_workspace_bytes: out_bytes is null");
-    *out_bytes = 256;
+    *out_bytes = cut(p).total;
     return FSR_OK;
 }
 
@@ -137,16 +408,22 @@ extern "C" int fsr_token_logprobs(const void* logits, const int32_t* n_rows, con
     if (!logits || (p->M > 0 && (!tokens || !logprobs)) || (p->K > 0 && (!top_ids || !top_logprobs)))
         return fail(FSR_EINVAL, "%s: null pointer among logits/tokens/logprobs/top_ids/top_logprobs", who);
     if ((uintptr_t)logits & (p->dtype == FSR_F32 ? 3 : 1)) return fail(FSR_EINVAL, "%s: logits must be aligned to their elements", who);
-    size_t need;
-    fsr_logprob_workspace_bytes(p, &need);
-    if (!workspace || ws_bytes < need) return fail(FSR_EWS, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
+    const Cut c = cut(p);
+    if (!workspace || ws_bytes < c.total) return fail(FSR_EWS, "%s: workspace %zu bytes, need %zu", who, ws_bytes, c.total);
     if ((uintptr_t)workspace & 255) return fail(FSR_EWS, "%s: workspace must be 256-byte aligned", who);
     LogprobArgs a{};
     a.logits = logits; a.n_rows = n_rows; a.tokens = tokens; a.logprobs = logprobs; a.entropy = entropy; a.top_ids = top_ids; a.top_logprobs = top_logprobs;
     a.stride = p->stride; a.N_cap = p->N_cap; a.V = p->V; a.M = p->M; a.K = p->K;
     a.scale = (float)(kLog2e / p->temperature);
     a.inv_t = 1.0 / p->temperature;
-    if (p->dtype == FSR_F32) hipLaunchKernelGGL((logprob_row_kernel<float>), dim3(p->N_cap), dim3(kThreads), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL((logprob_row_kernel<uint16_t>), dim3(p->N_cap), dim3(kThreads), 0, (hipStream_t)stream, a);
+    a.chunks = c.chunks;
+    a.tiles = c.tiles;
+    char* w = (char*)workspace;
+    a.arrivals = (unsigned long long*)(w + c.arrivals);
+    a.stats = (uint64_t*)(w + c.stats);
+    a.keys = (uint64_t*)(w + c.keys);
+    a.call_id = c.chunks > 1 ? next_call_id() : 0;
+    if (p->dtype == FSR_F32) launch<float>(a, stream);
+    else launch<uint16_t>(a, stream);
     return check_launch(who);
 }
