@@ -1060,6 +1060,13 @@ __device__ __forceinline__ bool run_tiled(const Args& a, const Piece& p, char* b
     return true;
 }
 
+// How a workgroup takes a piece (trees: tree_tiles.hpp).
+template <class C>
+struct Pieces {
+    static constexpr int kShared = 0;  // bytes of LDS besides the buffers
+    static __device__ __forceinline__ bool take(const Args& a, const Piece& p, char* buf0, char* buf1, int*, bool fast) { return run_tiled<C>(a, p, buf0, buf1, fast); }
+};
+
 // The pieces of a share of the line, one after the other.
 template <class C>
 struct Walk {
@@ -1168,7 +1175,12 @@ __global__ __launch_bounds__(C::kBlockThreads, 2) void tiled_kernel(Args a) {  /
     Piece p;
     while (walk.next(a, share, p)) {
         bool fast = true;
-        while (!run_tiled<C>(a, p, buf0, buf1, fast)) fast = false;
+        if constexpr (Pieces<C>::kShared > 0) {
+            __shared__ int more[Pieces<C>::kShared / sizeof(int)];
+            while (!Pieces<C>::take(a, p, buf0, buf1, more, fast)) fast = false;
+        } else {
+            while (!Pieces<C>::take(a, p, buf0, buf1, nullptr, fast)) fast = false;
+        }
     }
 }
 

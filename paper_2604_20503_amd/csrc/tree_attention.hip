@@ -1,7 +1,7 @@
 // Verification attention of trees: a request's rows are a tree of drafted tokens, and a row attends to the context and to its
 // ancestors.  The rows of a request and the query heads of a KV head are packed into tiles (row_tiles.hpp); keys of the context are seen
 // by all of them, so that only the last tiles of an item, where the call's own rows lie, look at the rows' bits.
-#include "row_tiles.hpp"
+#include "tree_tiles.hpp"
 
 namespace fsr {
 namespace {
