@@ -7,7 +7,9 @@ there is no fallback: if the library is missing, the first call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -71,6 +73,10 @@ _ARGUMENTS = {
     "fsr_token_logprobs": "s:logits i:n_rows i:tokens f:logprobs f:entropy i:top_ids f:top_logprobs S:params t:workspace n:ws_bytes n:stream",
     "fsr_prune_scatter": "t:compact i:src_row i:n_rows t:out n:row_bytes n:N_cap n:stream",
 }
+
+
+# Calls whose tensors' device is looked at where they are handed over (13 tensors one by one in Python: 1.9 us).
+_HERE_ONLY = {"fsr_kv_append_rope", "fsr_kv_append_rope_kv8", "fsr_verify_attention_tree", "fsr_tree_accept", "fsr_kv_commit", "fsr_token_logprobs"}
 
 
 class FsrError(RuntimeError):
@@ -154,7 +160,7 @@ def load_library():
         calls = {}
         for name, arguments in _ARGUMENTS.items():
             kinds, names = zip(*(a.split(":") for a in arguments.split()))
-            calls[name] = _marshal.make(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value, "".join(kinds), names)
+            calls[name] = _marshal.make(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value, "".join(kinds), names, name in _HERE_ONLY)
         _calls = calls
         _lib = lib
     return _lib
@@ -588,6 +594,10 @@ def shared_workspace_bytes(*, N_cap, H_q, H_kv, D, dtype, out_dtype) -> int:
 # ---------------------------------------------------------------------------------------------------------------
 TREE_WORDS_MAX, TOP_MAX = 16, 64
 
+# The structures of a call as bytes: a fourth of the time that a ctypes structure with named fields takes.
+_ATTN_BYTES, _ROPE_BYTES, _LOGPROB_BYTES = struct.Struct("10if3i"), struct.Struct("14i4q"), struct.Struct("6iqd")
+_TREE_BYTES, _COMMIT_BYTES = struct.Struct("5i"), struct.Struct("8i")
+
 
 def _tree_words(tree_mask, N_cap) -> int:
     if tree_mask.dim() != 2 or tree_mask.shape[0] != N_cap or not 1 <= tree_mask.shape[1] <= TREE_WORDS_MAX:
@@ -597,6 +607,8 @@ def _tree_words(tree_mask, N_cap) -> int:
 
 def _row_stride(t, inner, name) -> int:
     """Elements from a row to the next of a tensor whose rows are dense (a slice of wider rows, as fused projections give it)."""
+    if t.is_contiguous():
+        return inner
     want = 1
     for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
         if size != 1 and stride != want:
@@ -609,9 +621,14 @@ def _one_of(tensor, shape, dtype, device, name):
     """The caller's buffer checked, or a new one."""
     if tensor is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(tensor.shape) != tuple(shape):
+    if tensor.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(tensor.shape)}")
     return tensor
+
+
+def _on_gpu(t, name):  # (that all others are, and on the current device, is seen where they are handed over)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
 
 
 def kv_append_rope(q, k_new, v_new, cos_sin, k_cache, v_cache, block_tables, ctx_lens, cu_q, *, positions=None, tree_mask=None, q_out=None, pairs=False,
@@ -620,32 +637,33 @@ def kv_append_rope(q, k_new, v_new, cos_sin, k_cache, v_cache, block_tables, ctx
     their positions by the table cos_sin [T, R] and store keys and values into the paged caches (in place).  Rotary positions: positions
     [N_cap], or by depth in the trees of tree_mask [N_cap, words] int64, or one behind the other.  k_scale / v_scale [H_kv]: the caches are
     uint8 tensors of E4M3 bytes -> fsr_kv_append_rope_kv8.  Returns the queries, q_out (may be q)."""
-    B = ctx_lens.shape[0]
+    B, rows, cache = ctx_lens.shape[0], q.shape, k_cache.shape
     _check_offsets(B, block_tables, cu_q=cu_q)
-    if q.dim() != 3 or k_new.dim() != 3 or k_cache.dim() != 4 or cos_sin.dim() != 2:
+    if len(rows) != 3 or len(cache) != 4 or cos_sin.dim() != 2:
         raise ValueError("q [N_cap, H_q, D], k_new and v_new [N_cap, H_kv, D], cos_sin [T, R] and caches of four dimensions are wanted")
-    N_cap, H_q, D = q.shape
-    n_pages, a, b, D_c = k_cache.shape
-    P, H_kv = (a, b) if kv_layout == KV_TOKEN_MAJOR else (b, a)
-    if k_new.shape != v_new.shape or tuple(k_new.shape) != (N_cap, H_kv, D) or v_cache.shape != k_cache.shape or D_c != D:
+    N_cap, H_q, D = rows
+    n_pages, P, H_kv, D_c = cache
+    if kv_layout != KV_TOKEN_MAJOR:
+        P, H_kv = H_kv, P
+    if k_new.shape != (N_cap, H_kv, D) or v_new.shape != (N_cap, H_kv, D) or v_cache.shape != cache or D_c != D:
         raise ValueError("k_new and v_new must be [N_cap, H_kv, D] matching q and the caches")
-    kv8 = k_scale is not None or v_scale is not None
-    if not (q.dtype == k_new.dtype == v_new.dtype) or k_cache.dtype != v_cache.dtype or k_cache.dtype != (torch.uint8 if kv8 else q.dtype):
+    kv8, dtype = k_scale is not None or v_scale is not None, q.dtype
+    stored = torch.uint8 if kv8 else dtype
+    if k_new.dtype != dtype or v_new.dtype != dtype or k_cache.dtype != stored or v_cache.dtype != stored:
         raise ValueError("q, k_new, v_new and the caches must share a dtype (with scales: bf16 rows and uint8 caches)")
-    if kv8 and (k_scale is None or v_scale is None or tuple(k_scale.shape) != (H_kv,) or tuple(v_scale.shape) != (H_kv,)):
+    if kv8 and (k_scale is None or v_scale is None or k_scale.shape != (H_kv,) or v_scale.shape != (H_kv,)):
         raise ValueError("k_scale and v_scale need one entry per KV head")
-    if positions is not None and tuple(positions.shape) != (N_cap,):
+    if positions is not None and positions.shape != (N_cap,):
         raise ValueError(f"positions must have {N_cap} entries, got {tuple(positions.shape)}")
     words = _tree_words(tree_mask, N_cap) if tree_mask is not None else 0
-    q_out = _one_of(q_out, q.shape, q.dtype, q.device, "q_out")
-    if q_out.dtype != q.dtype:
-        raise ValueError("q_out must have the dtype of q")
-    _on_current_device(q=q, k_new=k_new, v_new=v_new, cos_sin=cos_sin, positions=positions, tree_mask=tree_mask, q_out=q_out, k_cache=k_cache,
-                       v_cache=v_cache, k_scale=k_scale, v_scale=v_scale, block_tables=block_tables, ctx_lens=ctx_lens, cu_q=cu_q)
-    p = RopeParams(B=B, N_cap=N_cap, H_q=H_q, H_kv=H_kv, D=D, R=cos_sin.shape[1], P=P, max_pages=block_tables.shape[1], n_pages=n_pages,
-                   T=cos_sin.shape[0], tree_words=words, pairs=1 if pairs else 0, dtype=_code(q.dtype), kv_layout=int(kv_layout),
-                   q_stride=_row_stride(q, H_q * D, "q"), k_stride=_row_stride(k_new, H_kv * D, "k_new"),
-                   v_stride=_row_stride(v_new, H_kv * D, "v_new"), reserved=0)
+    if q_out is None:
+        q_out = torch.empty(rows, dtype=dtype, device=q.device)
+    elif q_out.shape != rows or q_out.dtype != dtype:
+        raise ValueError(f"q_out must be {tuple(rows)} of {dtype}, got {tuple(q_out.shape)} of {q_out.dtype}")
+    _on_gpu(q, "q")
+    T, R = cos_sin.shape
+    p = _ROPE_BYTES.pack(B, N_cap, H_q, H_kv, D, R, P, block_tables.shape[1], n_pages, T, words, 1 if pairs else 0, _code(dtype), int(kv_layout),
+                         _row_stride(q, H_q * D, "q"), _row_stride(k_new, H_kv * D, "k_new"), _row_stride(v_new, H_kv * D, "v_new"), 0)
     if kv8:
         _call("fsr_kv_append_rope_kv8", q, k_new, v_new, cos_sin, positions, tree_mask, q_out, k_cache, v_cache, k_scale, v_scale, block_tables,
               ctx_lens, cu_q, p)
@@ -654,21 +672,39 @@ def kv_append_rope(q, k_new, v_new, cos_sin, k_cache, v_cache, block_tables, ctx
     return q_out
 
 
+@functools.lru_cache(maxsize=256)
+def _tree_workspace(N_cap, H_q, H_kv, D, dtype, out_dtype) -> int:
+    return _workspace_of("fsr_tree_workspace_bytes", AttnParams(B=1, N_cap=N_cap, H_q=H_q, H_kv=H_kv, D=D, P=1, max_pages=1, n_pages=1, dtype=dtype,
+                                                                out_dtype=out_dtype, scale=1.0))
+
+
 def verify_attention_tree(q, k_cache, v_cache, block_tables, ctx_lens, cu_q, tree_mask, *, scale, out=None, lse=None, out_dtype=None, workspace=None,
                           max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR):
     """fsr_verify_attention_tree: verify_attention whose rows see the context and the rows of their request that tree_mask [N_cap, words]
     int64 has a bit for.  Returns (out, lse)."""
-    B = ctx_lens.shape[0]
+    B, rows, cache, dtype = ctx_lens.shape[0], q.shape, k_cache.shape, q.dtype
     _check_offsets(B, block_tables, cu_q=cu_q)
-    if q.dim() != 3 or k_cache.dim() != 4 or v_cache.shape != k_cache.shape or not (q.dtype == k_cache.dtype == v_cache.dtype):
+    if len(rows) != 3 or len(cache) != 4 or v_cache.shape != cache or k_cache.dtype != dtype or v_cache.dtype != dtype:
         raise ValueError("q, k_cache and v_cache must share dtype; caches must share shape")
-    words = _tree_words(tree_mask, q.shape[0])
-    out, out_dtype = _outputs(tuple(q.shape), out, lse, out_dtype, q.dtype, q.device)
-    p = _attn_params(q, k_cache, block_tables, B, out_dtype, scale, max_q_len, max_workgroups, kv_layout)
-    _on_current_device(q=q, k_cache=k_cache, v_cache=v_cache, block_tables=block_tables, ctx_lens=ctx_lens, cu_q=cu_q, tree_mask=tree_mask, out=out,
-                       lse=lse, workspace=workspace)
-    token = _guard_workspace(workspace)
-    workspace, ws_bytes = _scratch("fsr_tree_workspace_bytes", p, workspace, q.device)
+    N_cap, H_q, D = rows
+    n_pages, P, H_kv, D_c = cache
+    if kv_layout != KV_TOKEN_MAJOR:
+        P, H_kv = H_kv, P
+    if D_c != D:
+        raise ValueError("head dim of q and k_cache differ")
+    words = _tree_words(tree_mask, N_cap)
+    _on_gpu(q, "q")
+    out, out_dtype = _outputs(rows, out, lse, out_dtype, dtype, q.device)
+    code, out_code = _code(dtype), _code(out_dtype)
+    p = _ATTN_BYTES.pack(B, N_cap, H_q, H_kv, D, P, block_tables.shape[1], n_pages, code, out_code, float(scale), int(max_q_len), int(max_workgroups),
+                         int(kv_layout))
+    token = None
+    if workspace is None:
+        ws_bytes = _tree_workspace(N_cap, H_q, H_kv, D, code, out_code)
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+    else:
+        token = _guard_workspace(workspace)
+        ws_bytes = workspace.numel() * workspace.element_size()
     _call("fsr_verify_attention_tree", q, k_cache, v_cache, block_tables, ctx_lens, cu_q, tree_mask, words, out, lse, p, workspace, ws_bytes)
     _note_workspace_use(token)
     return out, lse
@@ -677,39 +713,49 @@ def verify_attention_tree(q, k_cache, v_cache, block_tables, ctx_lens, cu_q, tre
 def tree_accept(target_tokens, draft_tokens, tree_mask, cu_q, *, S_max, accepted_len=None, n_emitted=None, emitted=None, path=None, keep_mask=None):
     """fsr_tree_accept.  Returns (accepted_len [B], n_emitted [B], emitted [B, S_max+1], path [B, S_max+1]); keep_mask [N_cap] uint8, if
     given, receives the rows of the paths."""
-    B, N_cap, dev = cu_q.shape[0] - 1, target_tokens.shape[0], cu_q.device
-    _check_offsets(B, cu_q=cu_q)
+    if cu_q.dim() != 1 or cu_q.shape[0] < 1 or target_tokens.dim() != 1:
+        raise ValueError("cu_q must be [B + 1] and target_tokens [N_cap]")
+    B, N_cap, S = cu_q.shape[0] - 1, target_tokens.shape[0], int(S_max) + 1
     words = _tree_words(tree_mask, N_cap)
-    if tuple(target_tokens.shape) != (N_cap,) or tuple(draft_tokens.shape) != (N_cap,) or (keep_mask is not None and tuple(keep_mask.shape) != (N_cap,)):
+    if draft_tokens.shape != (N_cap,) or (keep_mask is not None and keep_mask.shape != (N_cap,)):
         raise ValueError("target_tokens, draft_tokens and keep_mask must have one entry per row")
-    if S_max < 0:
+    if S < 1:
         raise ValueError("S_max must not be negative")
-    accepted_len = _one_of(accepted_len, (B,), torch.int32, dev, "accepted_len")
-    n_emitted = _one_of(n_emitted, (B,), torch.int32, dev, "n_emitted")
-    emitted = _one_of(emitted, (B, S_max + 1), torch.int32, dev, "emitted")
-    path = _one_of(path, (B, S_max + 1), torch.int32, dev, "path")
-    _on_current_device(target_tokens=target_tokens, draft_tokens=draft_tokens, tree_mask=tree_mask, cu_q=cu_q, accepted_len=accepted_len,
-                       n_emitted=n_emitted, emitted=emitted, path=path, keep_mask=keep_mask)
-    p = TreeParams(B=B, N_cap=N_cap, tree_words=words, S_max=int(S_max), reserved=0)
-    _call("fsr_tree_accept", target_tokens, draft_tokens, tree_mask, cu_q, accepted_len, n_emitted, emitted, path, keep_mask, p)
+    _on_gpu(cu_q, "cu_q")
+    if accepted_len is None and n_emitted is None and emitted is None and path is None:  # (one allocation)
+        accepted_len, n_emitted, emitted, path = torch.empty(2 * B * (S + 1), dtype=torch.int32, device=cu_q.device).split((B, B, B * S, B * S))
+        emitted, path = emitted.view(B, S), path.view(B, S)
+    else:
+        accepted_len = _one_of(accepted_len, (B,), torch.int32, cu_q.device, "accepted_len")
+        n_emitted = _one_of(n_emitted, (B,), torch.int32, cu_q.device, "n_emitted")
+        emitted = _one_of(emitted, (B, S), torch.int32, cu_q.device, "emitted")
+        path = _one_of(path, (B, S), torch.int32, cu_q.device, "path")
+    _call("fsr_tree_accept", target_tokens, draft_tokens, tree_mask, cu_q, accepted_len, n_emitted, emitted, path, keep_mask,
+          _TREE_BYTES.pack(B, N_cap, words, S - 1, 0))
     return accepted_len, n_emitted, emitted, path
 
 
 def kv_commit(k_cache, v_cache, block_tables, ctx_lens, accepted_len, path, *, kv_layout=KV_HEAD_MAJOR):
     """fsr_kv_commit: move the keys and values of accepted paths (tree_accept) to the positions behind the context, in place, in caches of
     any dtype."""
-    B = ctx_lens.shape[0]
-    _check_offsets(B, block_tables)
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+    B, cache = ctx_lens.shape[0], k_cache.shape
+    if block_tables.dim() != 2 or block_tables.shape[0] != B:
+        raise ValueError(f"block_tables must be [{B}, max_pages], got {tuple(block_tables.shape)}")
+    if len(cache) != 4 or v_cache.shape != cache or v_cache.dtype != k_cache.dtype:
         raise ValueError("the caches must share shape and dtype")
-    if tuple(accepted_len.shape) != (B,) or path.dim() != 2 or path.shape[0] != B or path.shape[1] < 1:
+    if accepted_len.shape != (B,) or path.dim() != 2 or path.shape[0] != B or path.shape[1] < 1:
         raise ValueError(f"accepted_len must be [{B}] and path [{B}, S_max + 1]")
-    _on_current_device(k_cache=k_cache, v_cache=v_cache, block_tables=block_tables, ctx_lens=ctx_lens, accepted_len=accepted_len, path=path)
-    n_pages, a, b, D = k_cache.shape
-    P, H_kv = (a, b) if kv_layout == KV_TOKEN_MAJOR else (b, a)
-    p = CommitParams(B=B, H_kv=H_kv, row_bytes=D * k_cache.element_size(), P=P, max_pages=block_tables.shape[1], n_pages=n_pages,
-                     S_max=path.shape[1] - 1, kv_layout=int(kv_layout))
-    _call("fsr_kv_commit", k_cache, v_cache, block_tables, ctx_lens, accepted_len, path, p)
+    _on_gpu(k_cache, "k_cache")
+    n_pages, P, H_kv, D = cache
+    if kv_layout != KV_TOKEN_MAJOR:
+        P, H_kv = H_kv, P
+    _call("fsr_kv_commit", k_cache, v_cache, block_tables, ctx_lens, accepted_len, path,
+          _COMMIT_BYTES.pack(B, H_kv, D * k_cache.element_size(), P, block_tables.shape[1], n_pages, path.shape[1] - 1, int(kv_layout)))
+
+
+@functools.lru_cache(maxsize=256)
+def _logprob_workspace(N_cap, V, M, K, dtype) -> int:
+    return _workspace_of("fsr_logprob_workspace_bytes", LogprobParams(N_cap=N_cap, V=V, M=M, K=K, dtype=dtype, reserved=0, stride=V, temperature=1.0))
 
 
 def token_logprobs(logits, tokens=None, *, top_k=0, temperature=1.0, n_rows=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None,
@@ -720,22 +766,32 @@ def token_logprobs(logits, tokens=None, *, top_k=0, temperature=1.0, n_rows=None
     if logits.dim() != 2:
         raise ValueError("logits must be [N_cap, V]")
     N_cap, V = logits.shape
-    if tokens is not None and (tokens.dim() not in (1, 2) or tokens.shape[0] != N_cap):
-        raise ValueError(f"tokens must be [{N_cap}] or [{N_cap}, M], got {tuple(tokens.shape)}")
+    given = None if tokens is None else tokens.shape
+    if given is not None and (len(given) not in (1, 2) or given[0] != N_cap):
+        raise ValueError(f"tokens must be [{N_cap}] or [{N_cap}, M], got {tuple(given)}")
     if n_rows is not None and n_rows.numel() != 1:
         raise ValueError("n_rows must be one number")
-    M = 0 if tokens is None else 1 if tokens.dim() == 1 else tokens.shape[1]
-    dev = logits.device
-    logprobs = None if tokens is None else _one_of(logprobs, tokens.shape, torch.float32, dev, "logprobs")
-    entropy = _one_of(entropy, (N_cap,), torch.float32, dev, "entropy")
-    top_ids = _one_of(top_ids, (N_cap, top_k), torch.int32, dev, "top_ids") if top_k else None
-    top_logprobs = _one_of(top_logprobs, (N_cap, top_k), torch.float32, dev, "top_logprobs") if top_k else None
-    p = LogprobParams(N_cap=N_cap, V=V, M=M, K=int(top_k), dtype=_code(logits.dtype), reserved=0, stride=_row_stride(logits, V, "logits"),
-                      temperature=float(temperature))
-    _on_current_device(logits=logits, n_rows=n_rows, tokens=tokens, logprobs=logprobs, entropy=entropy, top_ids=top_ids, top_logprobs=top_logprobs,
-                       workspace=workspace)
-    token = _guard_workspace(workspace)
-    workspace, ws_bytes = _scratch("fsr_logprob_workspace_bytes", p, workspace, dev)
+    M, K, dev, code = 0 if given is None else 1 if len(given) == 1 else given[1], int(top_k), logits.device, _code(logits.dtype)
+    if K < 0:
+        raise ValueError("top_k must not be negative")
+    _on_gpu(logits, "logits")
+    if logprobs is None and entropy is None and top_ids is None and top_logprobs is None:  # (one allocation)
+        logprobs, entropy, top_ids, top_logprobs = torch.empty(N_cap * (M + 1 + 2 * K), dtype=torch.float32, device=dev).split((N_cap * M, N_cap, N_cap * K, N_cap * K))
+        logprobs = None if given is None else logprobs.view(given)
+        top_ids, top_logprobs = (top_ids.view(torch.int32).view(N_cap, K), top_logprobs.view(N_cap, K)) if K else (None, None)
+    else:
+        logprobs = None if given is None else _one_of(logprobs, given, torch.float32, dev, "logprobs")
+        entropy = _one_of(entropy, (N_cap,), torch.float32, dev, "entropy")
+        top_ids = _one_of(top_ids, (N_cap, K), torch.int32, dev, "top_ids") if K else None
+        top_logprobs = _one_of(top_logprobs, (N_cap, K), torch.float32, dev, "top_logprobs") if K else None
+    p = _LOGPROB_BYTES.pack(N_cap, V, M, K, code, 0, _row_stride(logits, V, "logits"), float(temperature))
+    token = None
+    if workspace is None:
+        ws_bytes = _logprob_workspace(N_cap, V, M, K, code)
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    else:
+        token = _guard_workspace(workspace)
+        ws_bytes = workspace.numel() * workspace.element_size()
     _call("fsr_token_logprobs", logits, n_rows, tokens, logprobs, entropy, top_ids, top_logprobs, p, workspace, ws_bytes)
     _note_workspace_use(token)
     return logprobs, entropy, top_ids, top_logprobs
@@ -743,15 +799,12 @@ def token_logprobs(logits, tokens=None, *, top_k=0, temperature=1.0, n_rows=None
 
 def tree_workspace_bytes(*, N_cap, H_q, H_kv, D, dtype, out_dtype) -> int:
     """Workspace of verify_attention_tree for calls of up to N_cap rows."""
-    p = AttnParams(B=1, N_cap=N_cap, H_q=H_q, H_kv=H_kv, D=D, P=1, max_pages=1, n_pages=1, dtype=_code(dtype), out_dtype=_code(out_dtype),
-                   scale=1.0, max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR)
-    return _workspace_of("fsr_tree_workspace_bytes", p)
+    return _tree_workspace(N_cap, H_q, H_kv, D, _code(dtype), _code(out_dtype))
 
 
 def logprob_workspace_bytes(*, N_cap, V, M, K, dtype) -> int:
     """Workspace of token_logprobs for calls of up to N_cap rows."""
-    p = LogprobParams(N_cap=N_cap, V=V, M=M, K=K, dtype=_code(dtype), reserved=0, stride=V, temperature=1.0)
-    return _workspace_of("fsr_logprob_workspace_bytes", p)
+    return _logprob_workspace(N_cap, V, M, K, _code(dtype))
 
 
 def _workspace_of(size_of, p) -> int:

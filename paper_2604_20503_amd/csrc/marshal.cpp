@@ -28,6 +28,7 @@ struct Call {
     void* address;
     std::string* kinds;
     std::vector<std::string>* names;
+    bool here;  // tensors of another device than the current one are refused
 };
 
 // All arguments are pointers or integers, which the System V x86-64 convention passes alike, one register or stack word each.
@@ -44,8 +45,8 @@ Invoke invoke_of(int n, std::integer_sequence<int, N...>) {
     return table[n];
 }
 
-// Address of tensor `o` (None: 0).  False with a Python error set.
-bool address_of(PyObject* o, char kind, const std::string& name, uint64_t& out) {
+// Address of tensor `o` (None: 0); device: where it has to live (-1: anywhere).  False with a Python error set.
+bool address_of(PyObject* o, char kind, const std::string& name, int device, uint64_t& out) {
     if (o == Py_None) {
         out = 0;
         return true;
@@ -58,6 +59,10 @@ bool address_of(PyObject* o, char kind, const std::string& name, uint64_t& out) 
         const at::Tensor& t = THPVariable_Unpack(o);
         if (!t.is_cuda()) {
             PyErr_Format(PyExc_ValueError, "%s must live on the GPU", name.c_str());
+            return false;
+        }
+        if (device >= 0 && t.get_device() != device) {
+            PyErr_Format(PyExc_ValueError, "%s lives on cuda:%d, the current device is cuda:%d", name.c_str(), (int)t.get_device(), device);
             return false;
         }
         if (kind != 's' && !t.is_contiguous()) {
@@ -92,6 +97,8 @@ PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyObject* k
     Py_buffer held[2];
     int n_held = 0;
     bool ok = true;
+    int device = -1;
+    if (c->here && hipGetDevice(&device) != hipSuccess) device = -1;
     for (Py_ssize_t k = 0; ok && k < n; ++k) {
         const char kind = (*c->kinds)[k];
         if (kind == 'n') {
@@ -101,7 +108,7 @@ PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyObject* k
             ok = PyObject_GetBuffer(args[k], &held[n_held], PyBUF_SIMPLE) == 0;
             if (ok) a[k] = (uint64_t)held[n_held++].buf;
         } else {
-            ok = address_of(args[k], kind, (*c->names)[k], a[k]);
+            ok = address_of(args[k], kind, (*c->names)[k], device, a[k]);
         }
     }
     int rc = 0;
@@ -130,12 +137,13 @@ PyType_Slot slots[] = {{Py_tp_dealloc, (void*)dealloc}, {Py_tp_call, (void*)PyVe
 PyType_Spec spec = {"_marshal.Call", sizeof(Call), 0, Py_TPFLAGS_DEFAULT | Py_TPFLAGS_HAVE_VECTORCALL | Py_TPFLAGS_DISALLOW_INSTANTIATION, slots};
 PyObject* call_type = nullptr;
 
-// make(address, kinds, names) -> call object
+// make(address, kinds, names, here=False) -> call object
 PyObject* make(PyObject*, PyObject* args) {
     unsigned long long address;
     const char* kinds;
     PyObject* names;
-    if (!PyArg_ParseTuple(args, "KsO!", &address, &kinds, &PyTuple_Type, &names)) return nullptr;
+    int here = 0;
+    if (!PyArg_ParseTuple(args, "KsO!|p", &address, &kinds, &PyTuple_Type, &names, &here)) return nullptr;
     const std::string k(kinds);
     size_t buffers = 0;
     for (char x : k) buffers += x == 'S';
@@ -156,6 +164,7 @@ PyObject* make(PyObject*, PyObject* args) {
     c->address = (void*)(uintptr_t)address;
     c->kinds = new std::string(k);
     c->names = new std::vector<std::string>(std::move(list));
+    c->here = here != 0;
     return reinterpret_cast<PyObject*>(c);
 }
 
@@ -174,7 +183,7 @@ PyObject* without_system_fence(PyObject*, PyObject* event) {
 }
 
 PyMethodDef methods[] = {{"without_system_fence", without_system_fence, METH_O, "make an unrecorded torch.cuda.Event a light one"},
-                         {"make", make, METH_VARARGS, "make(address, kinds, names): a callable for the C entry point"}, {nullptr, nullptr, 0, nullptr}};
+                         {"make", make, METH_VARARGS, "make(address, kinds, names, here=False): a callable for the C entry point"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -157,6 +157,11 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     const int row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (a.n_rows && row >= a.n_rows[0]) return;
     const T* z = (const T*)a.logits + row * a.stride;
+    float given = -INFINITY;  // the logit of this thread's given token: it is there when the row is done
+    if ((int)threadIdx.x < a.M) {
+        const int id = a.tokens[(size_t)row * a.M + threadIdx.x];
+        if (id >= 0 && id < a.V) given = value_of(z + id);
+    }
     const int first = chunk * a.tiles * kTile, tiles = min(a.tiles, (a.V - first + kTile - 1) / kTile);
     Sums sums{-3.402823466e38f, 0.0f, 0.0f};
     float best = -INFINITY;
@@ -212,8 +217,8 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sh.m[w]);
     sums.refer(m, a.scale);
-    const double ws = wave_sum((double)sums.s), we = wave_sum((double)sums.e);
-    if (lane == 0) { sh.s[wave] = ws; sh.e[wave] = we; }
+    const double ws = wave_sum_to_last((double)sums.s), we = wave_sum_to_last((double)sums.e);
+    if (lane == kWave - 1) { sh.s[wave] = ws; sh.e[wave] = we; }
     if (TOP) {
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) least = sh.key[w] < least ? sh.key[w] : least;
@@ -292,40 +297,56 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
         const size_t theirs = (size_t)row * a.chunks + min(lane, a.chunks - 1);
         const double cm = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs)), cs = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 1)),
                      ce = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 2));
+        // ... and their keys beside them, the first 1024 of up to 4096 in registers
+        constexpr int kMine = 4;
+        const uint64_t* theirs_keys = a.keys + (size_t)row * a.chunks * a.K;
+        const int total = a.chunks * a.K;
+        uint64_t k[kMine];
+        if (TOP)
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int at = threadIdx.x + i * kThreads;
+                k[i] = at < total ? fetch(theirs_keys + at) : 0;
+            }
         m = wave_max(in ? (float)cm : -3.402823466e38f);
         const float d = fmaxf(((float)cm - m) * a.scale, kLeast);
         const double w = in ? (double)__builtin_amdgcn_exp2f(d) : 0.0;
-        S = wave_sum(w * cs);
-        E = wave_sum(w * (ce + (double)d * cs));
+        const double all_s = wave_sum_to_last(w * cs), all_e = wave_sum_to_last(w * (ce + (double)d * cs));
+        if (lane == kWave - 1) { sh.s[wave] = all_s; sh.e[wave] = all_e; }
         if (TOP) {
             uint64_t bound = 1;  // the largest of the chunks' last ones: K keys are not below it
-            for (int c = threadIdx.x; c < a.chunks; c += kThreads) {
-                const uint64_t k = fetch(a.keys + ((size_t)row * a.chunks + c) * a.K + a.K - 1);
-                bound = k > bound ? k : bound;
-            }
+            auto last_of_chunk = [&](uint64_t key, int at) { if (at % a.K == a.K - 1) bound = key > bound ? key : bound; };
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) last_of_chunk(k[i], threadIdx.x + i * kThreads);
+            for (int at = threadIdx.x + kMine * kThreads; at < total; at += kThreads) last_of_chunk(fetch(theirs_keys + at), at);
             for (int o = 1; o < kWave; o <<= 1) { const uint64_t other = shfl_xor64(bound, o); bound = other > bound ? other : bound; }
             if (lane == 0) sh.key[wave] = bound;
             if (threadIdx.x == 0) sh.n = 0;
             __syncthreads();
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) bound = sh.key[w] > bound ? sh.key[w] : bound;
-            for (int i = threadIdx.x; i < a.chunks * a.K; i += kThreads) {
-                const uint64_t k = fetch(a.keys + (size_t)row * a.chunks * a.K + i);
-                if (k >= bound) keys[atomicAdd(&sh.n, 1)] = k;
-            }
+            auto list = [&](uint64_t key) { if (key >= bound) keys[atomicAdd(&sh.n, 1)] = key; };
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) list(k[i]);
+            for (int at = threadIdx.x + kMine * kThreads; at < total; at += kThreads) list(fetch(theirs_keys + at));
             __syncthreads();
             const int n = sh.n;
             rank(keys, n, a.K, sh.top);
         }
         __syncthreads();
         if (threadIdx.x == 0) __hip_atomic_store(a.arrivals + row, a.call_id << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for a graph's next replay
+        S = sh.s[wave];
+        E = sh.e[wave];
     }
     const double log_s = S > 0.0 ? log(S) : __builtin_nan("");  // (no finite logit, or an infinite one: no sum)
     auto logprob = [&](float zv) { return (float)(((double)zv - (double)m) * a.inv_t - log_s); };
     if (threadIdx.x == 0 && a.entropy) a.entropy[row] = (float)(log_s - E / S * kLn2);
     for (int t = threadIdx.x; t < a.M; t += kThreads) {
-        const int id = a.tokens[(size_t)row * a.M + t];
-        float zv = id >= 0 && id < a.V ? value_of(z + id) : -INFINITY;
+        float zv = given;
+        if (t >= kThreads) {
+            const int id = a.tokens[(size_t)row * a.M + t];
+            zv = id >= 0 && id < a.V ? value_of(z + id) : -INFINITY;
+        }
         if (zv != zv) zv = -INFINITY;
         a.logprobs[(size_t)row * a.M + t] = logprob(zv);
     }
