@@ -19,6 +19,7 @@ _LIB_PATH = os.path.join(_HERE, "libfaser_verify.so")
 _MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
 _lib = None
 _calls = None  # entry point -> its native call object
+_marshal_module = None
 
 F32, BF16 = 0, 1
 PROBS, LOGITS, GREEDY = 0, 1, 2
@@ -157,6 +158,8 @@ def load_library():
         lib.fsr_static_scratch_bytes.restype = ctypes.c_size_t
         from . import _marshal
 
+        global _marshal_module
+        _marshal_module = _marshal
         calls = {}
         for name, arguments in _ARGUMENTS.items():
             kinds, names = zip(*(a.split(":") for a in arguments.split()))
@@ -626,6 +629,13 @@ def _one_of(tensor, shape, dtype, device, name):
     return tensor
 
 
+def _new(like, types, *shapes):
+    """New tensors on the device of `like`: 'f' float32, 'i' int32, 'b' uint8, 't' of its dtype."""
+    if _calls is None:
+        load_library()
+    return _marshal_module.new(like, types, *shapes)
+
+
 def _on_gpu(t, name):  # (that all others are, and on the current device, is seen where they are handed over)
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
@@ -657,7 +667,7 @@ def kv_append_rope(q, k_new, v_new, cos_sin, k_cache, v_cache, block_tables, ctx
         raise ValueError(f"positions must have {N_cap} entries, got {tuple(positions.shape)}")
     words = _tree_words(tree_mask, N_cap) if tree_mask is not None else 0
     if q_out is None:
-        q_out = torch.empty(rows, dtype=dtype, device=q.device)
+        q_out, = _new(q, "t", rows)
     elif q_out.shape != rows or q_out.dtype != dtype:
         raise ValueError(f"q_out must be {tuple(rows)} of {dtype}, got {tuple(q_out.shape)} of {q_out.dtype}")
     _on_gpu(q, "q")
@@ -694,14 +704,17 @@ def verify_attention_tree(q, k_cache, v_cache, block_tables, ctx_lens, cu_q, tre
         raise ValueError("head dim of q and k_cache differ")
     words = _tree_words(tree_mask, N_cap)
     _on_gpu(q, "q")
-    out, out_dtype = _outputs(rows, out, lse, out_dtype, dtype, q.device)
+    if out is None and out_dtype in (None, dtype) and (lse is None or lse.shape == (N_cap, H_q)):
+        (out,), out_dtype = _new(q, "t", rows), dtype
+    else:
+        out, out_dtype = _outputs(rows, out, lse, out_dtype, dtype, q.device)
     code, out_code = _code(dtype), _code(out_dtype)
     p = _ATTN_BYTES.pack(B, N_cap, H_q, H_kv, D, P, block_tables.shape[1], n_pages, code, out_code, float(scale), int(max_q_len), int(max_workgroups),
                          int(kv_layout))
     token = None
     if workspace is None:
         ws_bytes = _tree_workspace(N_cap, H_q, H_kv, D, code, out_code)
-        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+        workspace, = _new(q, "b", (ws_bytes,))
     else:
         token = _guard_workspace(workspace)
         ws_bytes = workspace.numel() * workspace.element_size()
@@ -722,9 +735,8 @@ def tree_accept(target_tokens, draft_tokens, tree_mask, cu_q, *, S_max, accepted
     if S < 1:
         raise ValueError("S_max must not be negative")
     _on_gpu(cu_q, "cu_q")
-    if accepted_len is None and n_emitted is None and emitted is None and path is None:  # (one allocation)
-        accepted_len, n_emitted, emitted, path = torch.empty(2 * B * (S + 1), dtype=torch.int32, device=cu_q.device).split((B, B, B * S, B * S))
-        emitted, path = emitted.view(B, S), path.view(B, S)
+    if accepted_len is None and n_emitted is None and emitted is None and path is None:
+        accepted_len, n_emitted, emitted, path = _new(cu_q, "iiii", (B,), (B,), (B, S), (B, S))
     else:
         accepted_len = _one_of(accepted_len, (B,), torch.int32, cu_q.device, "accepted_len")
         n_emitted = _one_of(n_emitted, (B,), torch.int32, cu_q.device, "n_emitted")
@@ -775,10 +787,12 @@ def token_logprobs(logits, tokens=None, *, top_k=0, temperature=1.0, n_rows=None
     if K < 0:
         raise ValueError("top_k must not be negative")
     _on_gpu(logits, "logits")
-    if logprobs is None and entropy is None and top_ids is None and top_logprobs is None:  # (one allocation)
-        logprobs, entropy, top_ids, top_logprobs = torch.empty(N_cap * (M + 1 + 2 * K), dtype=torch.float32, device=dev).split((N_cap * M, N_cap, N_cap * K, N_cap * K))
-        logprobs = None if given is None else logprobs.view(given)
-        top_ids, top_logprobs = (top_ids.view(torch.int32).view(N_cap, K), top_logprobs.view(N_cap, K)) if K else (None, None)
+    if entropy is None and logprobs is None and top_ids is None and top_logprobs is None:
+        logprobs, entropy, top_ids, top_logprobs = _new(logits, "ffif", given or (0,), (N_cap,), (N_cap, K), (N_cap, K))
+        if given is None:
+            logprobs = None
+        if not K:
+            top_ids = top_logprobs = None
     else:
         logprobs = None if given is None else _one_of(logprobs, given, torch.float32, dev, "logprobs")
         entropy = _one_of(entropy, (N_cap,), torch.float32, dev, "entropy")
@@ -788,7 +802,7 @@ def token_logprobs(logits, tokens=None, *, top_k=0, temperature=1.0, n_rows=None
     token = None
     if workspace is None:
         ws_bytes = _logprob_workspace(N_cap, V, M, K, code)
-        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+        workspace, = _new(logits, "b", (ws_bytes,))
     else:
         token = _guard_workspace(workspace)
         ws_bytes = workspace.numel() * workspace.element_size()

@@ -10,6 +10,7 @@
 // found in LDS and read once more, 32 K bytes.  The workgroup of a row that is done last joins the chunks.
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "common.hpp"
 #include "device_utils.hpp"
@@ -34,7 +35,7 @@ struct LogprobArgs {
     float scale;   // log2(e) / T
     double inv_t;
     int chunks, tiles;  // of a row, of a chunk
-    unsigned long long* arrivals;  // [N_cap]
+    unsigned long long* arrivals;  // [N_cap], kArrivalStep apart
     uint64_t* stats;    // [N_cap * chunks][3]: m, S, sum of S's terms times x, as doubles
     uint64_t* keys;     // [N_cap * chunks][K]
     unsigned long long call_id;
@@ -65,7 +66,9 @@ __device__ __forceinline__ int id_of_key(uint64_t key) { return (int)~(uint32_t)
 constexpr int kTilesMax = 32;    // of a chunk
 constexpr int kChunksMax = 64;   // of a row
 constexpr int kWorkgroups = 1024; // that a call is cut into, if its rows are fewer
+constexpr int kArrivalStep = 16;  // words from a row's arrival counter to the next: a line of memory each (side by side: 64 rows of 32 chunks 56 us)
 constexpr int kGroupsMax = 512;  // groups that may hold alternatives, listed
+constexpr int kGroupsMore = 32;   // than K, that are read as they are
 constexpr float kLeast = -200.0f; // least power of two that is told from no weight at all
 static_assert((long long)kTilesMax * kChunksMax * kThreads * 8 == 1 << 22, "longest row of fp32");
 
@@ -115,14 +118,46 @@ struct Sums {
     }
 };
 
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int o) {
-    return (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, kWave) << 32 | (uint32_t)__shfl_xor((int)v, o, kWave);
+// Steps of a reduction over the wave by DPP: lanes 1, 2, 4, 8 to the left in a row of 16, then lane 15 of a row to the next one, lane 31
+// to the upper half; lane 63 has it all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_max(float v) {
+    return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max_by_dpp(float v) {
+    v = dpp_max<0x111, 0xf>(v);
+    v = dpp_max<0x112, 0xf>(v);
+    v = dpp_max<0x114, 0xf>(v);
+    v = dpp_max<0x118, 0xf>(v);
+    v = dpp_max<0x142, 0xa>(v);
+    v = dpp_max<0x143, 0xc>(v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), kWave - 1));
+}
+__device__ __forceinline__ uint32_t wave_largest(uint32_t v) {
+    auto step = [&](auto ctrl, auto rows) {
+        const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        v = other > v ? other : v;
+    };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, kWave - 1);
+}
+// The larger key of a lane and its neighbour in a group of four.
+template <int PERM>
+__device__ __forceinline__ uint64_t larger_of_four(uint64_t k) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)k, PERM, 0xf, 0xf, true), hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(k >> 32), PERM, 0xf, 0xf, true);
+    const uint64_t other = (uint64_t)hi << 32 | lo;
+    return other > k ? other : k;
 }
 
 struct Shared {
     double s[kThreads / kWave], e[kThreads / kWave];
     float m[kThreads / kWave];
-    uint64_t key[kThreads / kWave];
+    uint32_t set_top[kWave], set_id[kWave];  // keys of 64 sets, in halves
     int count[kThreads / kWave], n, last;
     int chosen[FSR_TOP_MAX];
     uint64_t top[FSR_TOP_MAX];
@@ -141,6 +176,30 @@ __device__ __forceinline__ void rank(const uint64_t* keys, int n, int K, uint64_
         for (int j = 0; j < n; ++j) before += keys[j] > mine;
         if (mine != 0 && before < K) top[before] = mine;
     }
+}
+
+// A key that r of 64 keys in LDS (all different, or 0: none) are not below, and few others; 1 if there are not so many.  By every wave
+// for itself.  Their upper halves alone are compared, unless many of them are equal.
+__device__ __forceinline__ uint64_t rth_of_64(const Shared& sh, int r) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const uint32_t top = sh.set_top[lane];
+    int before = 0;
+#pragma unroll
+    for (int j = 0; j < kWave; ++j) before += sh.set_top[j] > top;
+    // the r-th largest upper half, some lane's that has it: fewer than r are larger, and with its equals there are r
+    uint32_t bound = before < r ? top : 0xffffffffu;
+    bound = ~(uint32_t)wave_largest(~bound);
+    const unsigned long long equal = __ballot(top == bound);
+    if (bound == 0) return 1;
+    if (__popcll(equal) <= 8) return (uint64_t)bound << 32;
+    const uint64_t mine = (uint64_t)top << 32 | sh.set_id[lane];
+    before = 0;
+#pragma unroll 8
+    for (int j = 0; j < kWave; ++j) before += ((uint64_t)sh.set_top[j] << 32 | sh.set_id[j]) > mine;
+    const unsigned long long is = __ballot(before == r - 1);
+    if (is == 0) return 1;
+    const int at = __ffsll(is) - 1;
+    return (uint64_t)bound << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, at);
 }
 
 // Groups in descending order of their largest logits, the first of them first among equals.
@@ -201,16 +260,19 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     }
 
     // sums of the chunk
-    const float wave_m = wave_max(sums.m);
+    const float wave_m = wave_max_by_dpp(sums.m);
     if (lane == 0) sh.m[wave] = wave_m;
     if (threadIdx.x == 0) sh.n = 0;
-    uint64_t least = ~0ull;  // of the threads' sets of 8 (4): the largest key of a set, the least of those of all sets
+    // A bound that at least K groups are not below, and few more are: the K-th of the largest keys of 64 sets of four threads each.
     if (TOP) {
+        static_assert(kWaves == 4, "four lanes a set");
         uint64_t k = any ? key_of(best, best_tile * kThreads + threadIdx.x) : 0;
-        const int set = a.K <= kThreads / 8 ? 8 : 4;
-        for (int o = 1; o < set; o <<= 1) { const uint64_t other = shfl_xor64(k, o); k = other > k ? other : k; }
-        for (int o = set; o < kWave; o <<= 1) { const uint64_t other = shfl_xor64(k, o); k = other < k ? other : k; }
-        if (lane == 0) sh.key[wave] = k;
+        k = larger_of_four<0xb1>(k);  // (lanes 1 0 3 2)
+        k = larger_of_four<0x4e>(k);  // (lanes 2 3 0 1)
+        if ((threadIdx.x & 3) == 0) {
+            sh.set_top[threadIdx.x >> 2] = (uint32_t)(k >> 32);
+            sh.set_id[threadIdx.x >> 2] = (uint32_t)k;
+        }
     }
     __syncthreads();
     float m = sh.m[0];
@@ -220,17 +282,27 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     const double ws = wave_sum_to_last((double)sums.s), we = wave_sum_to_last((double)sums.e);
     if (lane == kWave - 1) { sh.s[wave] = ws; sh.e[wave] = we; }
     if (TOP) {
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) least = sh.key[w] < least ? sh.key[w] : least;
-        // (at least K groups come before it or are it, if there are so many)
+        const uint64_t least = rth_of_64(sh, a.K);
+        const float least_top = value_of_key(least);  // (1: NaN)
         auto has = [&](int t) { return first + t * kTile + (int)threadIdx.x * N < a.V; };
-        for (int t = 0; t < tiles; ++t) {
-            const uint64_t k = has(t) ? group_key(tops[t * kThreads + threadIdx.x], t) : 0;
-            if (k != 0 && k >= least) {
-                const int at = atomicAdd(&sh.n, 1);
-                if (at < kGroupsMax) sh.list[at] = k;
+        auto look = [&](float top, int t) __attribute__((always_inline)) {
+            if (!(top < least_top) && has(t)) {
+                const uint64_t k = group_key(top, t);
+                if (k >= least) {
+                    const int at = atomicAdd(&sh.n, 1);
+                    if (at < kGroupsMax) sh.list[at] = k;
+                }
             }
+        };
+        int t = 0;
+        for (; t + 8 <= tiles; t += 8) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = tops[(t + k) * kThreads + threadIdx.x];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) look(x[k], t + k);
         }
+        for (; t < tiles; ++t) look(tops[t * kThreads + threadIdx.x], t);
         __syncthreads();
         int n = sh.n;
         if (n > kGroupsMax) {
@@ -257,15 +329,22 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
             __syncthreads();
             n = sh.n;
         }
-        rank(sh.list, n, a.K, sh.top);
-        __syncthreads();
-        // the logits of those groups that are not below the last group's largest one (of fewer than K groups: all)
-        const int groups = min(n, a.K);
-        const uint64_t bound = groups == a.K ? sh.top[groups - 1] >> 32 << 32 : 0;
+        // The logits of those groups that are not below the last group's largest one (of fewer than K groups: all).  A few groups more
+        // than K are read as they are.
+        const uint64_t* groups_of = sh.list;
+        int groups = n;
+        uint64_t bound = n < a.K ? 0 : least >> 32 << 32;
+        if (n > a.K + kGroupsMore) {
+            rank(sh.list, n, a.K, sh.top);
+            __syncthreads();
+            groups_of = sh.top;
+            groups = a.K;
+            bound = sh.top[a.K - 1] >> 32 << 32;
+        }
         if (threadIdx.x == 0) sh.n = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < groups * N; i += kThreads) {
-            const int id = first + id_of_key(sh.top[i / N]) * N + i % N;
+            const int id = first + id_of_key(groups_of[i / N]) * N + i % N;
             const uint64_t k = id < a.V ? key_of(value_of(z + id), id) : 0;
             if (k >= bound && k != 0) keys[atomicAdd(&sh.n, 1)] = k;
         }
@@ -289,42 +368,43 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
             for (int k = threadIdx.x; k < a.K; k += kThreads) publish(a.keys + entry * a.K + k, sh.top[k]);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the chunk is in memory once every wave's stores are acknowledged
         __syncthreads();
-        if (threadIdx.x == 0) sh.last = count_arrival(a.arrivals + row, a.call_id) == a.chunks;
+        if (threadIdx.x == 0) sh.last = count_arrival(a.arrivals + (size_t)row * kArrivalStep, a.call_id) == a.chunks;
         __syncthreads();
         if (!sh.last) return;
-        // The chunks' sums, one a lane (every wave for itself), in an order that does not depend on who was last.
-        const bool in = lane < a.chunks;
-        const size_t theirs = (size_t)row * a.chunks + min(lane, a.chunks - 1);
-        const double cm = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs)), cs = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 1)),
-                     ce = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 2));
-        // ... and their keys beside them, the first 1024 of up to 4096 in registers
+        // The chunks' sums, one a lane, in an order that does not depend on who was last (the second wave); their keys beside them, the first
+        // 1024 of up to 4096 in registers, and a bound again: of the chunks' j-th keys the r-th, where r chunks with j keys each make K.
         constexpr int kMine = 4;
         const uint64_t* theirs_keys = a.keys + (size_t)row * a.chunks * a.K;
         const int total = a.chunks * a.K;
-        uint64_t k[kMine];
-        if (TOP)
+        uint64_t k[kMine], jth = 0;
+        const int nth = TOP ? min((2 * a.K + a.chunks - 1) / a.chunks, a.K) : 1, r = (a.K + nth - 1) / nth;
+        if (TOP) {
+            if ((int)threadIdx.x < a.chunks) jth = fetch(theirs_keys + threadIdx.x * a.K + nth - 1);
 #pragma unroll
             for (int i = 0; i < kMine; ++i) {
                 const int at = threadIdx.x + i * kThreads;
                 k[i] = at < total ? fetch(theirs_keys + at) : 0;
             }
-        m = wave_max(in ? (float)cm : -3.402823466e38f);
-        const float d = fmaxf(((float)cm - m) * a.scale, kLeast);
-        const double w = in ? (double)__builtin_amdgcn_exp2f(d) : 0.0;
-        const double all_s = wave_sum_to_last(w * cs), all_e = wave_sum_to_last(w * (ce + (double)d * cs));
-        if (lane == kWave - 1) { sh.s[wave] = all_s; sh.e[wave] = all_e; }
+        }
+        if (wave == 1) {
+            const bool in = lane < a.chunks;
+            const size_t theirs = (size_t)row * a.chunks + min(lane, a.chunks - 1);
+            const double cm = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs)), cs = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 1)),
+                         ce = __builtin_bit_cast(double, fetch(a.stats + 3 * theirs + 2));
+            const float all_m = wave_max_by_dpp(in ? (float)cm : -3.402823466e38f);
+            const float d = fmaxf(((float)cm - all_m) * a.scale, kLeast);
+            const double w = in ? (double)__builtin_amdgcn_exp2f(d) : 0.0;
+            const double all_s = wave_sum_to_last(w * cs), all_e = wave_sum_to_last(w * (ce + (double)d * cs));
+            if (lane == kWave - 1) { sh.s[0] = all_s; sh.e[0] = all_e; sh.m[0] = all_m; }
+        }
         if (TOP) {
-            uint64_t bound = 1;  // the largest of the chunks' last ones: K keys are not below it
-            auto last_of_chunk = [&](uint64_t key, int at) { if (at % a.K == a.K - 1) bound = key > bound ? key : bound; };
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) last_of_chunk(k[i], threadIdx.x + i * kThreads);
-            for (int at = threadIdx.x + kMine * kThreads; at < total; at += kThreads) last_of_chunk(fetch(theirs_keys + at), at);
-            for (int o = 1; o < kWave; o <<= 1) { const uint64_t other = shfl_xor64(bound, o); bound = other > bound ? other : bound; }
-            if (lane == 0) sh.key[wave] = bound;
+            if (threadIdx.x < kWave) {
+                sh.set_top[threadIdx.x] = (uint32_t)(jth >> 32);
+                sh.set_id[threadIdx.x] = (uint32_t)jth;
+            }
             if (threadIdx.x == 0) sh.n = 0;
             __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) bound = sh.key[w] > bound ? sh.key[w] : bound;
+            const uint64_t bound = rth_of_64(sh, r);
             auto list = [&](uint64_t key) { if (key >= bound) keys[atomicAdd(&sh.n, 1)] = key; };
 #pragma unroll
             for (int i = 0; i < kMine; ++i) list(k[i]);
@@ -334,11 +414,14 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
             rank(keys, n, a.K, sh.top);
         }
         __syncthreads();
-        if (threadIdx.x == 0) __hip_atomic_store(a.arrivals + row, a.call_id << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for a graph's next replay
-        S = sh.s[wave];
-        E = sh.e[wave];
+        if (threadIdx.x == 0) __hip_atomic_store(a.arrivals + (size_t)row * kArrivalStep, a.call_id << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for a graph's next replay
+        S = sh.s[0];
+        E = sh.e[0];
+        m = sh.m[0];
     }
-    const double log_s = S > 0.0 ? log(S) : __builtin_nan("");  // (no finite logit, or an infinite one: no sum)
+    // (no finite logit, or an infinite one: no sum.  S lies between 1 and V: its fraction's logarithm is off by 2^-24 at most.)
+    const float sum = (float)S;
+    const double log_s = S > 0.0 ? ((double)__builtin_amdgcn_frexp_expf(sum) + (double)__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(sum))) * kLn2 : __builtin_nan("");
     auto logprob = [&](float zv) { return (float)(((double)zv - (double)m) * a.inv_t - log_s); };
     if (threadIdx.x == 0 && a.entropy) a.entropy[row] = (float)(log_s - E / S * kLn2);
     for (int t = threadIdx.x; t < a.M; t += kThreads) {
@@ -366,15 +449,15 @@ Cut cut(const fsr_logprob_params* p) {
     const int tile = kThreads * (p->dtype == FSR_F32 ? 8 : 16), all = (p->V + tile - 1) / tile, least = (all + kTilesMax - 1) / kTilesMax;
     const long long n = std::max(p->N_cap, 1);
     const int most = std::min(all, kChunksMax);
-    const int wanted = std::max(least, (int)std::min((long long)most, (kWorkgroups + n - 1) / n));
+    const int wanted = std::max(least, (int)std::min((long long)most, std::max(kWorkgroups / n, 1LL)));
     Cut c;
     c.tiles = (all + wanted - 1) / wanted;
     c.chunks = (all + c.tiles - 1) / c.tiles;
     // (rows times chunks of no smaller call are more)
-    const size_t entries = (size_t)std::max(n * least, std::min(n * most, kWorkgroups + n));
+    const size_t entries = (size_t)std::max(n * least, std::min(n * most, std::max((long long)kWorkgroups, n)));
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t x = at; at += align_up(bytes, 256); return x; };
-    c.arrivals = take(n * 8);
+    c.arrivals = take(n * 8 * kArrivalStep);
     c.stats = take(entries * 24);
     c.keys = take(entries * p->K * 8);
     c.total = at;
@@ -388,7 +471,7 @@ void launch(const LogprobArgs& a, void* stream) {
         hipLaunchKernelGGL((logprob_kernel<T, false>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
         return;
     }
-    const size_t room = std::max({(size_t)a.tiles * kThreads * 4, (size_t)a.K * Group<T>::kN * 8, a.chunks > 1 ? (size_t)a.chunks * a.K * 8 : 0});
+    const size_t room = std::max({(size_t)a.tiles * kThreads * 4, (size_t)(a.K + kGroupsMore) * Group<T>::kN * 8, a.chunks > 1 ? (size_t)a.chunks * a.K * 8 : 0});
     hipLaunchKernelGGL((logprob_kernel<T, true>), grid, dim3(kThreads), room, (hipStream_t)stream, a);
 }
 
