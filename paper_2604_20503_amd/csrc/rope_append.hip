@@ -1,9 +1,10 @@
 // Cache append with the position rotation on the way: a call's query and key rows are turned to their positions, keys and values enter
 // the request's pages.
 //     first R elements of a head, pairs (a, b) = (x[i], x[i + R/2]) or (x[2i], x[2i + 1]):   a cos - b sin,  b cos + a sin
-// Memory-bound: every element is read once and written once.  A workgroup takes a row; a thread takes 16 elements that are rotated with
-// each other, or 8 that are only moved.  Its loads go out before the row's request, page and position are known (four round trips to
-// memory one after the other: offsets, length and table, cosines).
+// Memory-bound: every element is read once and written once.  A workgroup takes a row.  A thread takes the same 16 elements, which are
+// rotated with each other, of several heads (or 8 that are only moved), so that its cosines stay in registers and places need no divisions.
+// Its first loads go out before the row's request, page and position are known (four round trips to memory one after the other: offsets,
+// length and table, cosines).
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>
@@ -14,8 +15,9 @@
 namespace fsr {
 namespace {
 
-constexpr int kThreads = 256, kAtOnce = 2;  // pieces of a thread that are loaded before the first is stored
-constexpr int kMaxRows = 1 << 22;           // workgroups of a launch
+constexpr int kThreads = 256;
+constexpr int kAtOnce = 1;          // heads of a thread that are loaded before the first is stored (with 2: 371 MB 84 us, not 78)
+constexpr int kMaxRows = 1 << 22;   // of a launch, a workgroup each
 
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
 typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2;
@@ -37,8 +39,9 @@ struct RopeArgs {
     const int32_t* ctx;
     const int32_t* cu_q;
     long long q_stride, k_stride, v_stride;  // elements from a row to the next
-    int B, N_cap, H_q, H_kv, D, R, P, max_pages, n_pages, T, tree_words, token_major;
-    int turned, per_head, q_pieces, pieces;  // pieces of a head that are rotated, of a head, of the queries, of a row
+    int B, N_cap, H_q, H_kv, D, R, P, p_shift, max_pages, n_pages, T, tree_words, token_major;
+    int turned, per_head;  // pieces of a head that are rotated, of a head
+    int lanes, step;       // threads of a head, heads at once
 };
 
 // Eight elements.
@@ -70,142 +73,161 @@ struct Eight<float> {
     __device__ __forceinline__ void set(const float* v) { x = f32x4{v[0], v[1], v[2], v[3]}; y = f32x4{v[4], v[5], v[6], v[7]}; }
 };
 
-// Where a piece of a row lies: its head (queries, keys, values one behind the other) and its elements.
-struct At {
-    int part, head, first, second;  // part 0 query, 1 key, 2 value; second < 0: eight elements that are moved as they are
-    int turn;                       // the first of its eight angles
+// x / scale as fp32 rounds it.  The quotient by the rounded inverse is off by a unit at most, and one step of Newton's method, whose
+// residual an fma gives exactly, rounds it as the division would (3 instructions, not 10): for scales of ordinary size, but for those whose
+// fraction is all ones.
+struct Divisor {
+    float scale, inverse;
+    bool plain;
+    __device__ __forceinline__ void set(float s) {
+        scale = s;
+        inverse = 1.0f / s;
+        plain = !(fabsf(s) > 1e-15f && fabsf(s) < 1e30f) || (__builtin_bit_cast(uint32_t, s) & 0x7fffffu) == 0x7fffffu;
+    }
+    __device__ __forceinline__ float of(float x) const {
+        if (plain) return x / scale;
+        const float q = x * inverse, better = fmaf(fmaf(-q, scale, x), inverse, q);
+        return fabsf(q) < INFINITY && fabsf(x) > 1e-30f ? better : q;  // (the residual of a smaller x is below fp32; its code is 0)
+    }
 };
-template <bool PAIRS>
-__device__ __forceinline__ At piece_at(const RopeArgs& a, int n) {
-    At p;
-    const bool is_q = n < a.q_pieces;
-    if (!is_q) n -= a.q_pieces;
-    const int k_pieces = a.H_kv * a.per_head;
-    if (!is_q && n >= k_pieces) {
-        n -= k_pieces;
-        const int each = a.D >> 3;
-        p.part = 2;
-        p.head = (int)((uint32_t)n / (uint32_t)each);
-        p.first = (n - p.head * each) * 8;
-        p.second = -1;
-        return p;
-    }
-    p.part = is_q ? 0 : 1;
-    p.head = (int)((uint32_t)n / (uint32_t)a.per_head);
-    const int u = n - p.head * a.per_head;
-    p.turn = 8 * u;
-    if (u < a.turned) {
-        p.first = PAIRS ? 16 * u : 8 * u;
-        p.second = PAIRS ? 16 * u + 8 : 8 * u + a.R / 2;
-    } else {
-        p.first = a.R + 8 * (u - a.turned);
-        p.second = -1;
-    }
-    return p;
-}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <typename T, bool PAIRS, bool KV8>
 __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs a) {
-    for (int row = blockIdx.x; row < a.N_cap; row += gridDim.x) {
-        const T* from[3] = {(const T*)a.q + row * a.q_stride, (const T*)a.k_new + row * a.k_stride, (const T*)a.v_new + row * a.v_stride};
-        Eight<T> x[kAtOnce], y[kAtOnce];
-        At at[kAtOnce];
-        auto fetch = [&](int n, int s) __attribute__((always_inline)) {
-            at[s] = piece_at<PAIRS>(a, min(n, a.pieces - 1));
-            const T* p = (at[s].part == 0 ? from[0] : at[s].part == 1 ? from[1] : from[2]) + at[s].head * a.D;
-            x[s].load(p + at[s].first);
-            y[s].load(p + max(at[s].second, 0));
-        };
-#pragma unroll
-        for (int s = 0; s < kAtOnce; ++s) fetch(threadIdx.x + s * kThreads, s);
-        if (row >= a.cu_q[a.B]) return;
-        const int i = owner_by_wave(a.cu_q, a.B, row), j = row - a.cu_q[i];
-        const long long t = (long long)a.ctx[i] + j;
-        long long pos = t;
-        if (a.positions) pos = a.positions[row];
-        if (a.tree) {  // the depth in the tree
-            pos = (long long)a.ctx[i] - 1;
-            for (int w = 0; w < a.tree_words; ++w) pos += __popcll(a.tree[(size_t)row * a.tree_words + w]);
+    const int row = blockIdx.x, heads = a.H_q + 2 * a.H_kv;
+    const int lane_head = (int)((uint32_t)threadIdx.x / (uint32_t)a.lanes), lane = threadIdx.x - lane_head * a.lanes;
+    const bool idle = lane_head >= a.step;  // (threads that are left over where a head's pieces do not divide their number)
+    const T* const from_q = (const T*)a.q + row * a.q_stride;
+    const T* const from_k = (const T*)a.k_new + row * a.k_stride;
+    const T* const from_v = (const T*)a.v_new + row * a.v_stride;
+    int first = 0, second = 0;  // the thread's elements of every head; second < 0: eight that are moved as they are
+    auto place_piece = [&](int u) __attribute__((always_inline)) {
+        if (u < a.turned) {
+            first = PAIRS ? 16 * u : 8 * u;
+            second = PAIRS ? 16 * u + 8 : 8 * u + a.R / 2;
+        } else {
+            first = a.R + 8 * (u - a.turned);
+            second = -1;
         }
-        pos = pos < 0 ? 0 : pos >= a.T ? a.T - 1 : pos;
-        bool stored = t >= 0 && t < (long long)a.max_pages * a.P;  // there is a page for this position
-        size_t slot = 0, head_step = 0;
-        if (stored) {
-            const int pg = (int)(t / a.P), in = (int)(t - (long long)pg * a.P);
-            const int page = a.bt[(size_t)i * a.max_pages + pg];
-            stored = page >= 0 && page < a.n_pages;  // never write outside the pool
-            slot = a.token_major ? ((size_t)page * a.P + in) * a.H_kv : (size_t)page * a.H_kv * a.P + in;
-            head_step = a.token_major ? 1 : a.P;
-        }
-        const float* table = a.cos_sin + (size_t)pos * a.R;
-        auto finish = [&](int s) __attribute__((always_inline)) {
-            const At p = at[s];
-            float u[8], w[8];
+    };
+    Eight<T> x[kAtOnce], y[kAtOnce];
+    auto fetch = [&](int h, int s) __attribute__((always_inline)) {
+        if (idle || h >= heads) return;
+        const T* at = h < a.H_q ? from_q + h * a.D : h < a.H_q + a.H_kv ? from_k + (h - a.H_q) * a.D : from_v + (h - a.H_q - a.H_kv) * a.D;
+        x[s].load(at + first);
+        if (second >= 0) y[s].load(at + second);
+    };
+    place_piece(lane);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                u[k] = PAIRS ? (k < 4 ? x[s].get(2 * k) : y[s].get(2 * k - 8)) : x[s].get(k);
-                w[k] = PAIRS ? (k < 4 ? x[s].get(2 * k + 1) : y[s].get(2 * k - 7)) : y[s].get(k);
-            }
-            if (p.second >= 0) {
-                Eight<float> c, n;
-                c.load(table + p.turn);
-                n.load(table + a.R / 2 + p.turn);
+    for (int s = 0; s < kAtOnce; ++s) fetch(lane_head + s * a.step, s);
+
+    // all of this is the same for the whole workgroup
+    if (row >= uniform(a.cu_q[a.B])) return;
+    const int i = uniform(owner_by_wave(a.cu_q, a.B, row)), c = uniform(a.ctx[i]), j = row - uniform(a.cu_q[i]);
+    const long long t = (long long)c + j;
+    long long pos = t;
+    if (a.positions) pos = uniform(a.positions[row]);
+    if (a.tree) {  // the depth in the tree
+        int bits = 0;
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(a.tree + (size_t)row * a.tree_words);
+        for (int w = 0; w < 2 * a.tree_words; ++w) bits += __popc((unsigned)uniform((int)words[w]));
+        pos = (long long)c + bits - 1;
+    }
+    const int turn = pos < 0 ? 0 : pos >= a.T ? a.T - 1 : (int)pos;
+    bool stored = t >= 0 && t < min((long long)a.max_pages * a.P, 1LL << 31);  // there is a page for this position
+    size_t slot = 0, head_step = 0;
+    if (stored) {
+        const uint32_t pg = a.p_shift >= 0 ? (uint32_t)t >> a.p_shift : (uint32_t)t / (uint32_t)a.P, in = (uint32_t)t - pg * (uint32_t)a.P;
+        const int page = uniform(a.bt[(size_t)i * a.max_pages + pg]);
+        stored = page >= 0 && page < a.n_pages;  // never write outside the pool
+        slot = (a.token_major ? ((size_t)page * a.P + in) * a.H_kv : (size_t)page * a.H_kv * a.P + in) * a.D;
+        head_step = (size_t)(a.token_major ? 1 : a.P) * a.D;
+    }
+    if (idle) return;
+    const float* table = a.cos_sin + (size_t)turn * a.R;
+    T* const to_q = (T*)a.q_out + (size_t)row * a.H_q * a.D;
+
+    for (int piece = lane; piece < a.per_head; piece += a.lanes) {  // (once, but for heads of more pieces than there are threads)
+        Eight<float> cosines, sines;
+        if (piece < a.turned) {
+            cosines.load(table + 8 * piece);
+            sines.load(table + a.R / 2 + 8 * piece);
+        }
+        if (piece != lane) {
+            place_piece(piece);
+#pragma unroll
+            for (int s = 0; s < kAtOnce; ++s) fetch(lane_head + s * a.step, s);
+        }
+        auto finish = [&](int h, int s) __attribute__((always_inline)) {
+            const bool is_q = h < a.H_q, is_k = !is_q && h < a.H_q + a.H_kv;
+            const int g = is_q ? h : is_k ? h - a.H_q : h - a.H_q - a.H_kv;
+            const bool turns = second >= 0 && (is_q || is_k);
+            float u[8], w[8];  // the two of each pair
+            if (turns) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float turned = u[k] * c.get(k) - w[k] * n.get(k);
-                    w[k] = w[k] * c.get(k) + u[k] * n.get(k);
-                    u[k] = turned;
+                    const float v = PAIRS ? (k < 4 ? x[s].get(2 * k) : y[s].get(2 * k - 8)) : x[s].get(k);
+                    const float z = PAIRS ? (k < 4 ? x[s].get(2 * k + 1) : y[s].get(2 * k - 7)) : y[s].get(k);
+                    const float turned = v * cosines.get(k) - z * sines.get(k), other = z * cosines.get(k) + v * sines.get(k);
+                    if (!PAIRS) {
+                        u[k] = turned;
+                        w[k] = other;
+                    } else if (k < 4) {
+                        u[2 * k] = turned;
+                        u[2 * k + 1] = other;
+                    } else {
+                        w[2 * k - 8] = turned;
+                        w[2 * k - 7] = other;
+                    }
                 }
-                if (PAIRS) {
-                    float lo[8], hi[8];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) { lo[2 * k] = u[k]; lo[2 * k + 1] = w[k]; hi[2 * k] = u[k + 4]; hi[2 * k + 1] = w[k + 4]; }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) { u[k] = lo[k]; w[k] = hi[k]; }
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) u[k] = x[s].get(k);
             }
-            if (p.part != 0 && !stored) return;
-            if (KV8 && p.part != 0) {  // from the fp32 value: one rounding
-                const float scale = (p.part == 1 ? a.k_scale : a.v_scale)[p.head];
-                uint8_t* to = (uint8_t*)(p.part == 1 ? a.k_cache : a.v_cache) + (slot + p.head * head_step) * a.D;
-                auto put = [&](const float* v, int first) {
+            if (KV8 && !is_q) {  // from the fp32 value: one rounding
+                if (!stored) return;
+                if (!turns) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        u[k] = x[s].get(k);
+                        w[k] = y[s].get(k);
+                    }
+                }
+                Divisor scale;
+                scale.set((is_k ? a.k_scale : a.v_scale)[g]);
+                uint8_t* to = (uint8_t*)(is_k ? a.k_cache : a.v_cache) + slot + g * head_step;
+                auto put = [&](const float* v, int at) {
                     uint32_t o[2];
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
-                        o[k] = pack_e4m3(v[4 * k + 2] / scale, v[4 * k + 3] / scale, pack_e4m3(v[4 * k] / scale, v[4 * k + 1] / scale, 0u, false), true);
-                    *reinterpret_cast<u32x2*>(to + first) = u32x2{o[0], o[1]};
+                        o[k] = pack_e4m3(scale.of(v[4 * k + 2]), scale.of(v[4 * k + 3]), pack_e4m3(scale.of(v[4 * k]), scale.of(v[4 * k + 1]), 0u, false), true);
+                    *reinterpret_cast<u32x2*>(to + at) = u32x2{o[0], o[1]};
                 };
-                put(u, p.first);
-                if (p.second >= 0) put(w, p.second);
-                return;
+                put(u, first);
+                if (second >= 0) put(w, second);
+            } else if (is_q || stored) {
+                T* to = is_q ? to_q + g * a.D : (T*)(is_k ? a.k_cache : a.v_cache) + slot + g * head_step;
+                if (turns) {  // (what is only moved keeps its bits)
+                    x[s].set(u);
+                    y[s].set(w);
+                }
+                x[s].store(to + first);
+                if (second >= 0) y[s].store(to + second);
             }
-            T* to = p.part == 0 ? (T*)a.q_out + ((size_t)row * a.H_q + p.head) * a.D
-                                : (T*)(p.part == 1 ? a.k_cache : a.v_cache) + (slot + p.head * head_step) * a.D;
-            if (p.second >= 0) {
-                x[s].set(u);
-                y[s].set(w);
-                y[s].store(to + p.second);
-            }
-            x[s].store(to + p.first);  // (what is only moved keeps its bits)
         };
-        for (int n = threadIdx.x; n < a.pieces;) {
+        for (int h = lane_head; h < heads;) {
 #pragma unroll
             for (int s = 0; s < kAtOnce; ++s)
-                if (n + s * kThreads < a.pieces) finish(s);
-            n += kAtOnce * kThreads;
-            if (n < a.pieces)
+                if (h + s * a.step < heads) finish(h + s * a.step, s);
+            h += kAtOnce * a.step;
+            if (h < heads)
 #pragma unroll
-                for (int s = 0; s < kAtOnce; ++s) fetch(n + s * kThreads, s);
+                for (int s = 0; s < kAtOnce; ++s) fetch(h + s * a.step, s);
         }
     }
 }
 
 template <typename T, bool KV8>
 void launch(const RopeArgs& a, bool pairs, void* stream) {
-    const dim3 grid((unsigned)std::min(a.N_cap, kMaxRows)), block(kThreads);
+    const dim3 grid((unsigned)a.N_cap), block(kThreads);
     if (pairs) hipLaunchKernelGGL((rope_append_kernel<T, true, KV8>), grid, block, 0, (hipStream_t)stream, a);
     else hipLaunchKernelGGL((rope_append_kernel<T, false, KV8>), grid, block, 0, (hipStream_t)stream, a);
 }
@@ -223,7 +245,7 @@ int append(const char* who, bool kv8, const void* q, const void* k_new, const vo
     if (p->R <= 0 || p->R > p->D) return fail(FSR_ESHAPE, "%s: R=%d must be 1 .. D=%d", who, p->R, p->D);
     if (p->R % 16 != 0 || p->D % (kv8 ? 16 : 8) != 0 || p->D > 8192)
         return fail(FSR_EUNSUP, "%s: R=%d D=%d (R a multiple of 16, D of %d up to 8192)", who, p->R, p->D, kv8 ? 16 : 8);
-    if (p->H_q > 65535 || p->H_kv > 65535 || (long long)(p->H_q + 2LL * p->H_kv) * (p->D / 8) > (1 << 28)) return fail(FSR_EUNSUP, "%s: H_q=%d H_kv=%d D=%d are too large", who, p->H_q, p->H_kv, p->D);
+    if (p->H_q > 65535 || p->H_kv > 65535 || p->N_cap > kMaxRows) return fail(FSR_EUNSUP, "%s: H_q=%d H_kv=%d (up to 65535) N_cap=%d (up to 2^22)", who, p->H_q, p->H_kv, p->N_cap);
     const int elem = p->dtype == FSR_F32 ? 4 : 2;
     const long long q_row = (long long)p->H_q * p->D, kv_row = (long long)p->H_kv * p->D;
     if (p->q_stride < q_row || p->k_stride < kv_row || p->v_stride < kv_row)
@@ -244,12 +266,13 @@ int append(const char* who, bool kv8, const void* q, const void* k_new, const vo
     a.bt = block_tables; a.ctx = ctx_lens; a.cu_q = cu_q;
     a.q_stride = p->q_stride; a.k_stride = p->k_stride; a.v_stride = p->v_stride;
     a.B = p->B; a.N_cap = p->N_cap; a.H_q = p->H_q; a.H_kv = p->H_kv; a.D = p->D; a.R = p->R; a.P = p->P;
+    a.p_shift = (p->P & (p->P - 1)) == 0 ? __builtin_ctz((unsigned)p->P) : -1;
     a.max_pages = p->max_pages; a.n_pages = p->n_pages; a.T = p->T; a.tree_words = p->tree_words;
     a.token_major = p->kv_layout == FSR_KV_TOKEN_MAJOR;
     a.turned = p->R / 16;
     a.per_head = a.turned + (p->D - p->R) / 8;
-    a.q_pieces = p->H_q * a.per_head;
-    a.pieces = a.q_pieces + p->H_kv * (a.per_head + p->D / 8);
+    a.lanes = std::min(a.per_head, kThreads);
+    a.step = kThreads / a.lanes;
     if (kv8) launch<uint16_t, true>(a, p->pairs, stream);
     else if (p->dtype == FSR_BF16) launch<uint16_t, false>(a, p->pairs, stream);
     else launch<float, false>(a, p->pairs, stream);

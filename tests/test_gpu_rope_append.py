@@ -194,3 +194,25 @@ def test_replays(fsr):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out[:r.N].cpu(), want) and torch.equal(k, caches[0]) and torch.equal(v, caches[1])
+
+
+def test_codes_are_those_of_kv_append_kv8(fsr):
+    """Values, and keys by the cosine 1 and the sine 0, enter 8-bit caches as fsr_kv_append_kv8 stores them, whatever the scale: powers
+    of two, fractions of all ones, tiny, huge and zero ones; values from the smallest to infinities and NaN."""
+    announce("append with rotation, codes")
+    scales = torch.tensor([1.0, 0.0123, 2.0 ** -9 * (2 - 2.0 ** -23), 3e-20, 1e-41, 7e33, 0.0, 1.7e-3])
+    gen = torch.Generator().manual_seed(9)
+    bits = torch.randint(-32768, 32768, (64, 8, 64), generator=gen).to(torch.int16)
+    k, v = bits.view(BF).cuda(), (torch.randn(64, 8, 64, generator=gen) * scales[:, None] * 100).to(BF).cuda()
+    v[:32] = (scales[:, None] * torch.arange(-16, 16)[:, None, None] / 16 * torch.linspace(0, 64, 64)).to(BF).cuda()  # on ties and beside them
+    bt, ctx, cu = (torch.tensor(x, dtype=torch.int32).cuda() for x in ([[0, 1, 2, 3]], [0], [0, 64]))
+    caches = [torch.zeros(4, 8, 16, 64, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    table = torch.cat([torch.ones(64, 32), torch.zeros(64, 32)], 1).cuda()
+    fsr.kv_append_kv8(v, v, caches[0], caches[1], scales.cuda(), scales.cuda(), bt, ctx, cu)
+    fsr.kv_append_rope(v, v, v, table, caches[2], caches[3], bt, ctx, cu, k_scale=scales.cuda(), v_scale=scales.cuda())
+    value = lambda x: x.view(torch.float8_e4m3fn).float().nan_to_num(nan=1e3)  # noqa: E731
+    assert [int((value(caches[0]) != value(caches[2]))[:, h].sum()) for h in range(8)] == [0] * 8 and torch.equal(caches[1], caches[3])  # (-0 - -0 * 0 = 0: the sign of a zero key may differ)
+    # (what is not finite meets the sine 0, so of these only values are compared)
+    fsr.kv_append_kv8(k, k, caches[0], caches[1], scales.cuda(), scales.cuda(), bt, ctx, cu)
+    fsr.kv_append_rope(k, k, k, table, caches[2], caches[3], bt, ctx, cu, k_scale=scales.cuda(), v_scale=scales.cuda())
+    assert torch.equal(caches[1], caches[3])
