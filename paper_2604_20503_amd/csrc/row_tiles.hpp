@@ -210,6 +210,43 @@ __device__ __forceinline__ long long shfl_up64(long long v, int d) {
     return ((long long)hi << 32) | (uint32_t)lo;
 }
 
+// The share of a line whose units have been added up, `total`; the sequence in which it begins is still to be found.
+template <class C>
+__device__ __forceinline__ Line cut_line(const Args& a, int share, long long total, int n) {
+    Line l;
+    l.shares = (int)max(1LL, min((long long)a.nb, quotient(total, a.min_share)));
+    l.each = quotient(total, l.shares);
+    l.longer = (int)(total - l.each * l.shares);
+    l.seq = n;
+    l.seq_start = total;
+    l.lo = l.hi = 0;
+    if (total > 0 && share < l.shares) {
+        l.lo = l.begin(share);
+        l.hi = l.begin(share + 1);
+    }
+    return l;
+}
+
+// Trees of up to 64 requests: a request a lane, every wave for itself, without LDS and barriers (5700 -> 3400 cycles at the start of a call).
+template <class C>
+__device__ __forceinline__ Line find_share_by_wave(const Args& a, int share) {
+    const int n = n_sequences<C::kOp>(a), lane = threadIdx.x & (kWave - 1);
+    long long upto = lane < n ? sequence_units<C>(a, sequence<C::kOp>(a, lane)) : 0;
+    const long long mine = upto;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const long long up = shfl_up64(upto, o);
+        if (lane >= o) upto += up;
+    }
+    auto of_lane = [&](long long v, int at) { return (long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, at); };
+    Line l = cut_line<C>(a, share, of_lane(upto, kWave - 1), n);
+    if (l.lo < l.hi) {
+        l.seq = __popcll(__ballot(upto <= l.lo));  // (those that end in front of the share)
+        l.seq_start = of_lane(upto - mine, l.seq);
+    }
+    return l;
+}
+
 // Adds up the line; `scratch`: LDS for C::kBlockThreads sums and one sum per wave.
 template <class C>
 __device__ __forceinline__ Line find_share(const Args& a, int share, long long* scratch) {
@@ -229,17 +266,8 @@ __device__ __forceinline__ Line find_share(const Args& a, int share, long long* 
     for (int w = 0; w < (tid >> 6); ++w) upto += scratch[C::kBlockThreads + w];
     scratch[tid] = upto;
     __syncthreads();
-    Line l;
-    const long long total = scratch[C::kBlockThreads - 1];
-    l.shares = (int)max(1LL, min((long long)a.nb, quotient(total, a.min_share)));
-    l.each = quotient(total, l.shares);
-    l.longer = (int)(total - l.each * l.shares);
-    l.seq = n;
-    l.seq_start = total;
-    l.lo = l.hi = 0;
-    if (total > 0 && share < l.shares) {
-        l.lo = l.begin(share);
-        l.hi = l.begin(share + 1);
+    Line l = cut_line<C>(a, share, scratch[C::kBlockThreads - 1], n);
+    if (l.lo < l.hi) {
         int first = 0, last = C::kBlockThreads - 1;  // the chunk of sequences that holds unit lo
         while (first < last) {
             const int mid = (first + last) >> 1;
@@ -578,7 +606,7 @@ struct Tiled {
     static constexpr int kBlockThreads = kThreads, kWaves = row_tiles::kWaves;
     static constexpr int kPerUnit = 2;                // workgroups of a compute unit, two waves to a SIMD
     static constexpr int kItemCost = 5;  // measured: 20000 cycles (loads that nothing hides, tiles with masked keys, sums on their way out) against 4000 a tile
-    static constexpr int kMinShare = kItemCost + 1;
+    static constexpr int kMinShare = OP == kTree ? 1 : kItemCost + 1;  // (18 trees of 25-34 rows behind 221 tokens, 8/2 heads of 64: 15.6 us, not 19.7)
     static constexpr bool kEven = false;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kTailAt + kKeys * KT * 2;
     static constexpr int kBuf = kVAt + kKeys * DV * 2;
@@ -1157,7 +1185,7 @@ template <class C>
 __global__ __launch_bounds__(C::kBlockThreads, 1) void simple_kernel(Args a) {
     __shared__ long long scratch[kThreads + kWaves];
     const int share = share_of_block(blockIdx.x, a.nb);
-    const Line line = find_share<C>(a, share, scratch);
+    const Line line = C::kOp == kTree && a.B <= kWave ? find_share_by_wave<C>(a, share) : find_share<C>(a, share, scratch);
     Walk<C> walk;
     walk.begin(a, share, line);
     Piece p;
@@ -1169,7 +1197,7 @@ __global__ __launch_bounds__(C::kBlockThreads, 2) void tiled_kernel(Args a) {  /
     __shared__ __align__(1024) char buf0[C::kBuf];
     __shared__ __align__(1024) char buf1[C::kBuf];
     const int share = share_of_block(blockIdx.x, a.nb);
-    const Line line = find_share<C>(a, share, reinterpret_cast<long long*>(buf0));
+    const Line line = C::kOp == kTree && a.B <= kWave ? find_share_by_wave<C>(a, share) : find_share<C>(a, share, reinterpret_cast<long long*>(buf0));
     Walk<C> walk;
     walk.begin(a, share, line);
     Piece p;
@@ -1380,6 +1408,9 @@ inline int compute_units() {
 }
 
 template <class C>
+void launch_tree_join(const Args& a, hipStream_t s);  // (tree_tiles.hpp)
+
+template <class C>
 int launch(Args a, int max_workgroups, void* stream, const char* who) {
     int units = compute_units();
     if (max_workgroups > 0) units = std::min(units, max_workgroups);  // (any number is allowed: taken times the workgroups of a unit only now)
@@ -1399,6 +1430,8 @@ int launch(Args a, int max_workgroups, void* stream, const char* who) {
             const size_t now = std::min(rows - first, kMost);
             hipLaunchKernelGGL((join_rows_kernel<C>), dim3((unsigned)((now + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a, first);
         }
+    } else if constexpr (C::kOp == kTree) {
+        launch_tree_join<C>(a, s);
     } else {
         // 16 workgroups a share: one row a wave of a latent tile, two of a tile of heads; with 32 there the launching of workgroups took longer: 20 us, not 17.6
         hipLaunchKernelGGL((join_shares_kernel<C>), dim3(a.even_cap, std::min(16, (a.m_cap + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, a);

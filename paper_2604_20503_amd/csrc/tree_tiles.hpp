@@ -201,6 +201,102 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
     return true;
 }
 
+// Joins the pieces of an item as row_tiles.hpp does, ROWS rows a wave at once: a row's statistics and then its sums are two round trips to
+// memory, which a wave that takes its rows one after the other waits for each time (16 requests of 24-64 rows behind 1024-4096 tokens:
+// 17 us).
+template <class C, int ROWS>
+__global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
+    constexpr int kColumns = C::kDv / 64;
+    constexpr Reference kNone{-INFINITY, 0.0f};
+    const int32_t* desc = a.desc + (size_t)blockIdx.x * kDescInts;
+    const int pieces = desc[0], row0 = desc[1], hk = desc[2], rt = desc[3], rows = desc[4], first_slot = desc[5], second_slot = desc[6], step = desc[7];
+    const int r0 = (blockIdx.y * kWaves + uniform(threadIdx.x >> 6)) * ROWS, lane = threadIdx.x & 63;
+    if (pieces <= 0 || r0 >= rows) return;
+    auto slot = [&](int k) { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
+    float o[ROWS][kColumns], l[ROWS];
+    Reference of[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        l[r] = 0.0f;
+        of[r] = kNone;
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) o[r][c] = 0.0f;
+    }
+    for (int first = 0; first < pieces; first += kWave) {
+        const int n = min(pieces - first, kWave);
+        const size_t at = (size_t)slot(first + min(lane, n - 1)) * a.m_cap;
+        f32x4 stats[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) stats[r] = *reinterpret_cast<const f32x4*>(a.part_ml + (at + min(r0 + r, rows - 1)) * 4);
+        float w[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const float pl = lane < n ? stats[r][2] : 0.0f;
+            const Reference pm = pl == 0.0f ? kNone : Reference{stats[r][0], stats[r][1]};  // (none: a piece without a visible key)
+            const float top = fmaxf(wave_max(fmaf(pm.raw, a.scale_log2, pm.log2)), fmaf(of[r].raw, a.scale_log2, of[r].log2));
+            Reference use{0.0f, top};
+            if (!(fabsf(top) <= kNear)) use = furthest(pm, of[r], a.scale_log2);
+            const float before = l[r] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(of[r], use, a.scale_log2));
+            w[r] = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(pm, use, a.scale_log2));
+            float sum = w[r] * pl;
+#pragma unroll
+            for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, kWave);
+            l[r] = l[r] * before + sum;
+            of[r] = l[r] == 0.0f ? kNone : use;
+#pragma unroll
+            for (int c = 0; c < kColumns; ++c) o[r][c] *= before;
+        }
+        // the sums of `many` pieces of all rows at once
+        auto add = [&](int k0, auto many) __attribute__((always_inline)) {
+            float y[many.value][ROWS][kColumns];
+#pragma unroll
+            for (int i = 0; i < many.value; ++i) {
+                const float* x = a.part_o + (size_t)slot(first + k0 + i) * a.m_cap * C::kDv + lane * kColumns;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) __builtin_memcpy(y[i][r], x + (size_t)min(r0 + r, rows - 1) * C::kDv, kColumns * 4);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < many.value; ++i)
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w[r]), k0 + i));
+#pragma unroll
+                    for (int c = 0; c < kColumns; ++c) o[r][c] = fmaf(wk, y[i][r][c], o[r][c]);
+                }
+        };
+        int k = 0;
+#pragma unroll 1
+        for (; n - k >= 4; k += 4) add(k, std::integral_constant<int, 4>());
+        if (n - k >= 2) add(k, std::integral_constant<int, 2>()), k += 2;
+        if (n - k >= 1) add(k, std::integral_constant<int, 1>());
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        if (r0 + r >= rows) break;
+        const Place to = place_of(a, row0, hk, rt * C::kM + r0 + r);
+        const size_t row = (size_t)to.row * a.H + to.head;
+        const float inv = inverse(l[r]);
+        typename C::Out y[kColumns];
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) {
+            if constexpr (sizeof(typename C::Out) == 2) y[c] = (uint16_t)bf16_bits(o[r][c] * inv);
+            else y[c] = o[r][c] * inv;
+        }
+        __builtin_memcpy((typename C::Out*)a.out + row * C::kDv + lane * kColumns, y, sizeof y);
+        if (a.lse && lane == 0) a.lse[row] = log_sum<C::kOp>(of[r], l[r], a.scale);
+    }
+}
+
+// Two rows a wave where tiles are large (16 requests of 24-64 rows, 32/8 heads: 90.6 us, not 92.4), one where they are not and the pieces many
+// (12 rows behind 777 tokens: 18.7, not 20.6; fp32, 2-23 rows, 28/4 heads: 20.4, not 23.8).
+template <class C>
+void launch_tree_join(const Args& a, hipStream_t s) {
+    const int rows = std::min(a.m_cap, C::kM);
+    if (rows > 64) hipLaunchKernelGGL((join_tree_kernel<C, 2>), dim3(a.nb, (rows + 2 * kWaves - 1) / (2 * kWaves)), dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((join_tree_kernel<C, 1>), dim3(a.nb, (rows + kWaves - 1) / kWaves), dim3(kThreads), 0, s, a);
+}
+
 template <int KH, int KT, int DV, class OUT, bool PAGES16>
 struct Pieces<Tiled<kTree, KH, KT, DV, OUT, PAGES16>> {
     typedef Tiled<kTree, KH, KT, DV, OUT, PAGES16> C;
