@@ -198,6 +198,8 @@ struct Line {
     int seq;               // sequence in which this share begins
     long long seq_start;   // its first unit
     long long lo, hi;      // this share
+    bool known;            // `first` is that sequence
+    Seq first;
     __device__ __forceinline__ long long begin(int s) const { return each * s + min(s, longer); }
     __device__ __forceinline__ int share_of(long long u) const {
         const long long head = (each + 1) * longer;
@@ -220,6 +222,7 @@ __device__ __forceinline__ Line cut_line(const Args& a, int share, long long tot
     l.seq = n;
     l.seq_start = total;
     l.lo = l.hi = 0;
+    l.known = false;
     if (total > 0 && share < l.shares) {
         l.lo = l.begin(share);
         l.hi = l.begin(share + 1);
@@ -231,7 +234,8 @@ __device__ __forceinline__ Line cut_line(const Args& a, int share, long long tot
 template <class C>
 __device__ __forceinline__ Line find_share_by_wave(const Args& a, int share) {
     const int n = n_sequences<C::kOp>(a), lane = threadIdx.x & (kWave - 1);
-    long long upto = lane < n ? sequence_units<C>(a, sequence<C::kOp>(a, lane)) : 0;
+    const Seq q = sequence<C::kOp>(a, min(lane, n - 1));
+    long long upto = lane < n ? sequence_units<C>(a, q) : 0;
     const long long mine = upto;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
@@ -243,6 +247,13 @@ __device__ __forceinline__ Line find_share_by_wave(const Args& a, int share) {
     if (l.lo < l.hi) {
         l.seq = __popcll(__ballot(upto <= l.lo));  // (those that end in front of the share)
         l.seq_start = of_lane(upto - mine, l.seq);
+        l.known = true;
+        l.first = q;
+        l.first.row0 = __builtin_amdgcn_readlane(q.row0, l.seq);
+        l.first.rows = __builtin_amdgcn_readlane(q.rows, l.seq);
+        l.first.k_end = __builtin_amdgcn_readlane(q.k_end, l.seq);
+        l.first.base = __builtin_amdgcn_readlane(q.base, l.seq);
+        l.first.table = l.seq;
     }
     return l;
 }
@@ -605,7 +616,7 @@ struct Tiled {
     static constexpr int kM = kTileRows, kKeys = 64;
     static constexpr int kBlockThreads = kThreads, kWaves = row_tiles::kWaves;
     static constexpr int kPerUnit = 2;                // workgroups of a compute unit, two waves to a SIMD
-    static constexpr int kItemCost = 5;  // measured: 20000 cycles (loads that nothing hides, tiles with masked keys, sums on their way out) against 4000 a tile
+    static constexpr int kItemCost = OP == kTree ? 7 : 5;  // measured: 20000 cycles (loads that nothing hides, tiles with masked keys, sums on their way out) against 4000 a tile; of trees 23000 against 3100
     static constexpr int kMinShare = OP == kTree ? 1 : kItemCost + 1;  // (18 trees of 25-34 rows behind 221 tokens, 8/2 heads of 64: 15.6 us, not 19.7)
     static constexpr bool kEven = false;
     static constexpr int kHeadAt = 0, kTailAt = kKeys * KH * 2, kVAt = kTailAt + kKeys * KT * 2;
@@ -1116,7 +1127,7 @@ struct Walk {
         for (;;) {
             if (!inside) {
                 if (s >= n || seq_start >= line.hi) return false;
-                q = sequence<C::kOp>(a, s);
+                q = line.known && s == line.seq ? line.first : sequence<C::kOp>(a, s);
                 tiles = row_tiles_of<C>(a, q);
                 head_units = units_before<C>(a, q, tiles);
                 hk = rt = 0;

@@ -10,12 +10,25 @@
 namespace fsr {
 namespace row_tiles {
 
-// Where the lane's row sees a key of the tile: bit k of 64.
-__device__ __forceinline__ uint64_t tile_window(const uint32_t* row, int words, int base, int k_end, int key0) {
-    uint64_t w = (uint64_t)tree_window(row, words, base, key0 + 32) << 32 | tree_window(row, words, base, key0);
-    const int there = k_end - key0;  // > 0
-    return there >= 64 ? w : w & ((1ull << there) - 1);
-}
+// Where the lane's row sees a key of a tile: bit k of 64.  The words that say it are fetched a tile ahead.
+struct TileWindow {
+    uint32_t word[3];
+    __device__ __forceinline__ void fetch(const uint32_t* row, int words, int base, int key0) {
+        const int w = (key0 - base) >> 5;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) word[k] = w + k >= 0 && w + k < words ? row[w + k] : 0u;
+    }
+    __device__ __forceinline__ uint64_t get(int base, int k_end, int key0) const {
+        const int off = key0 - base, sh = off & 31, w = off >> 5;  // (words in front of the mask's are those of the context: all ones)
+        uint32_t x[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k) x[k] = w + k < 0 ? 0xffffffffu : word[k];
+        const uint32_t lo = __builtin_amdgcn_alignbit(x[1], x[0], sh), hi = __builtin_amdgcn_alignbit(x[2], x[1], sh);
+        const uint64_t bits = (uint64_t)hi << 32 | lo;
+        const int there = k_end - key0;  // > 0
+        return there >= 64 ? bits : bits & ((1ull << there) - 1);
+    }
+};
 
 // Whether a wave's rows of a tile's values hold one that is not finite: 16 rows of kDv elements, in LDS.
 template <class C>
@@ -119,13 +132,13 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
         for (int s = 0; s < C::kDk / 16; ++s) w.q[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s + 8 * h);
         w.tree = a.tree + (size_t)at.row * a.tree_words;
     }
-    w.tree_words = a.tree_words;
-    w.tree_base = p.q.base;
     if (t < p.t1) {
         loads.take(a, p);
         load_all(buf0);
         loads.find(a, p, min(t + 1, p.t1 - 1), wave, lane);
         const int whole_until = min(p.t1, p.q.base / C::kKeys);  // tiles of the context alone
+        TileWindow windows;
+        windows.fetch(w.tree, a.tree_words, p.q.base, max(t, whole_until) * C::kKeys);
         // A tile of the fast loop; false: a reference moves, and the tile is still to be added (the next one's loads are under way).
         auto step = [&](const char* now, char* then) __attribute__((always_inline)) {
             arrive();  // (and nobody reads the other buffer any more)
@@ -151,7 +164,8 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
             loaded = false;
             uint64_t window = ~0ull;
             if (t >= whole_until) {  // (for the whole workgroup: a value must not meet the weight 0 of a row that does not see it)
-                window = tile_window(w.tree, w.tree_words, w.tree_base, p.q.k_end, t * C::kKeys);
+                window = windows.get(p.q.base, p.q.k_end, t * C::kKeys);
+                windows.fetch(w.tree, a.tree_words, p.q.base, (t + 1) * C::kKeys);
                 const bool mine = wave_odd<C>(now + C::kVAt, wave, lane);
                 if (lane == 0) flags[wave] = mine;
                 lds_barrier();
@@ -201,53 +215,58 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
     return true;
 }
 
-// Joins the pieces of an item as row_tiles.hpp does, ROWS rows a wave at once: a row's statistics and then its sums are two round trips to
-// memory, which a wave that takes its rows one after the other waits for each time (16 requests of 24-64 rows behind 1024-4096 tokens:
-// 17 us).
+// Joins the pieces of an item, ROWS rows a wave.  Of 64 / ROWS pieces at once a lane takes the statistics of one piece of one row, so that a row's
+// largest reference and its sum take a few exchanges; then come the sums, 16 loads at a time.  (A wave that takes its rows one after the
+// other, all its lanes a row's pieces, waits for two round trips and twelve exchanges each time: 16 requests of 24-64 rows, 17 us.)
 template <class C, int ROWS>
 __global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
-    constexpr int kColumns = C::kDv / 64;
+    constexpr int kColumns = C::kDv / 64, kChunk = kWave / ROWS, kBatch = ROWS == 1 ? 8 : 16 / ROWS;
     constexpr Reference kNone{-INFINITY, 0.0f};
     const int32_t* desc = a.desc + (size_t)blockIdx.x * kDescInts;
     const int pieces = desc[0], row0 = desc[1], hk = desc[2], rt = desc[3], rows = desc[4], first_slot = desc[5], second_slot = desc[6], step = desc[7];
     const int r0 = (blockIdx.y * kWaves + uniform(threadIdx.x >> 6)) * ROWS, lane = threadIdx.x & 63;
     if (pieces <= 0 || r0 >= rows) return;
     auto slot = [&](int k) { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
-    float o[ROWS][kColumns], l[ROWS];
-    Reference of[ROWS];
+    const int mine = lane % ROWS, piece = lane / ROWS, my_row = min(r0 + mine, rows - 1);
+    float o[ROWS][kColumns], l = 0.0f;  // (l and of: of the lane's row)
+    Reference of = kNone;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        l[r] = 0.0f;
-        of[r] = kNone;
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) o[r][c] = 0.0f;
-    }
-    for (int first = 0; first < pieces; first += kWave) {
-        const int n = min(pieces - first, kWave);
-        const size_t at = (size_t)slot(first + min(lane, n - 1)) * a.m_cap;
-        f32x4 stats[ROWS];
+    for (int first = 0; first < pieces; first += kChunk) {
+        const int n = min(pieces - first, kChunk);
+        const f32x4 stats = *reinterpret_cast<const f32x4*>(a.part_ml + ((size_t)slot(first + min(piece, n - 1)) * a.m_cap + my_row) * 4);
+        const float pl = piece < n ? stats[2] : 0.0f;
+        const Reference pm = pl == 0.0f ? kNone : Reference{stats[0], stats[1]};  // (none: a piece without a visible key)
+        // Any number near the furthest reference will do; where powers of two are too coarse for one, it is that reference itself.
+        float top = fmaxf(fmaf(pm.raw, a.scale_log2, pm.log2), fmaf(of.raw, a.scale_log2, of.log2));
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) stats[r] = *reinterpret_cast<const f32x4*>(a.part_ml + (at + min(r0 + r, rows - 1)) * 4);
-        float w[ROWS];
+        for (int x = ROWS; x < kWave; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
+        Reference use{0.0f, top};
+        if (__any(!(fabsf(top) <= kNear))) {
+            Reference furthest = distance(pm, of, a.scale_log2) > 0.0f ? pm : of;
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const float pl = lane < n ? stats[r][2] : 0.0f;
-            const Reference pm = pl == 0.0f ? kNone : Reference{stats[r][0], stats[r][1]};  // (none: a piece without a visible key)
-            const float top = fmaxf(wave_max(fmaf(pm.raw, a.scale_log2, pm.log2)), fmaf(of[r].raw, a.scale_log2, of[r].log2));
-            Reference use{0.0f, top};
-            if (!(fabsf(top) <= kNear)) use = furthest(pm, of[r], a.scale_log2);
-            const float before = l[r] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(of[r], use, a.scale_log2));
-            w[r] = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(pm, use, a.scale_log2));
-            float sum = w[r] * pl;
-#pragma unroll
-            for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x, kWave);
-            l[r] = l[r] * before + sum;
-            of[r] = l[r] == 0.0f ? kNone : use;
-#pragma unroll
-            for (int c = 0; c < kColumns; ++c) o[r][c] *= before;
+            for (int x = ROWS; x < kWave; x <<= 1) {
+                const Reference y{__shfl_xor(furthest.raw, x, kWave), __shfl_xor(furthest.log2, x, kWave)};
+                if (distance(y, furthest, a.scale_log2) > 0.0f) furthest = y;
+            }
+            furthest = Reference{__shfl(furthest.raw, mine, kWave), __shfl(furthest.log2, mine, kWave)};  // (lanes may hold different ones of the same height)
+            if (!(fabsf(top) <= kNear)) use = furthest;
         }
-        // the sums of `many` pieces of all rows at once
-        auto add = [&](int k0, auto many) __attribute__((always_inline)) {
+        const float before = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(of, use, a.scale_log2));
+        const float w = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(pm, use, a.scale_log2));
+        float sum = w * pl;
+#pragma unroll
+        for (int x = ROWS; x < kWave; x <<= 1) sum += __shfl_xor(sum, x, kWave);
+        l = l * before + sum;
+        of = l == 0.0f ? kNone : use;
+        if (first > 0)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                for (int c = 0; c < kColumns; ++c) o[r][c] *= __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, before), r));
+        auto add = [&](int k0, auto many) __attribute__((always_inline)) {  // the sums of `many` pieces of all rows at once
             float y[many.value][ROWS][kColumns];
 #pragma unroll
             for (int i = 0; i < many.value; ++i) {
@@ -260,40 +279,45 @@ __global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
             for (int i = 0; i < many.value; ++i)
 #pragma unroll
                 for (int r = 0; r < ROWS; ++r) {
-                    const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w[r]), k0 + i));
+                    const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (k0 + i) * ROWS + r));
 #pragma unroll
                     for (int c = 0; c < kColumns; ++c) o[r][c] = fmaf(wk, y[i][r][c], o[r][c]);
                 }
         };
-        int k = 0;
+        int k0 = 0;
 #pragma unroll 1
-        for (; n - k >= 4; k += 4) add(k, std::integral_constant<int, 4>());
-        if (n - k >= 2) add(k, std::integral_constant<int, 2>()), k += 2;
-        if (n - k >= 1) add(k, std::integral_constant<int, 1>());
+        for (; n - k0 >= kBatch; k0 += kBatch) add(k0, std::integral_constant<int, kBatch>());
+        if (kBatch > 4 && n - k0 >= 4) add(k0, std::integral_constant<int, 4>()), k0 += 4;
+        if (kBatch > 2 && n - k0 >= 2) add(k0, std::integral_constant<int, 2>()), k0 += 2;
+        if (kBatch > 1 && n - k0 >= 1) add(k0, std::integral_constant<int, 1>());
     }
+    const float inv = inverse(l);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         if (r0 + r >= rows) break;
         const Place to = place_of(a, row0, hk, rt * C::kM + r0 + r);
         const size_t row = (size_t)to.row * a.H + to.head;
-        const float inv = inverse(l[r]);
+        const float by = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inv), r));
         typename C::Out y[kColumns];
 #pragma unroll
         for (int c = 0; c < kColumns; ++c) {
-            if constexpr (sizeof(typename C::Out) == 2) y[c] = (uint16_t)bf16_bits(o[r][c] * inv);
-            else y[c] = o[r][c] * inv;
+            if constexpr (sizeof(typename C::Out) == 2) y[c] = (uint16_t)bf16_bits(o[r][c] * by);
+            else y[c] = o[r][c] * by;
         }
         __builtin_memcpy((typename C::Out*)a.out + row * C::kDv + lane * kColumns, y, sizeof y);
-        if (a.lse && lane == 0) a.lse[row] = log_sum<C::kOp>(of[r], l[r], a.scale);
+    }
+    if (a.lse && lane < ROWS && r0 + lane < rows) {
+        const Place to = place_of(a, row0, hk, rt * C::kM + r0 + lane);
+        a.lse[(size_t)to.row * a.H + to.head] = log_sum<C::kOp>(of, l, a.scale);
     }
 }
 
-// Two rows a wave where tiles are large (16 requests of 24-64 rows, 32/8 heads: 90.6 us, not 92.4), one where they are not and the pieces many
-// (12 rows behind 777 tokens: 18.7, not 20.6; fp32, 2-23 rows, 28/4 heads: 20.4, not 23.8).
+// Four rows a wave where tiles are large (16 requests of 24-64 rows, 32/8 heads: 86.8 us; two rows 90.0, eight 87.8; 28 of 5-131, 8/2 heads:
+// 48.9, 50.5 and 52.0), one where they are not and pieces are many (fp32, 2-23 rows, 28/4 heads: 20.4; two rows 22.5, four 23.1).
 template <class C>
 void launch_tree_join(const Args& a, hipStream_t s) {
     const int rows = std::min(a.m_cap, C::kM);
-    if (rows > 64) hipLaunchKernelGGL((join_tree_kernel<C, 2>), dim3(a.nb, (rows + 2 * kWaves - 1) / (2 * kWaves)), dim3(kThreads), 0, s, a);
+    if (rows > 64) hipLaunchKernelGGL((join_tree_kernel<C, 4>), dim3(a.nb, (rows + 4 * kWaves - 1) / (4 * kWaves)), dim3(kThreads), 0, s, a);
     else hipLaunchKernelGGL((join_tree_kernel<C, 1>), dim3(a.nb, (rows + kWaves - 1) / kWaves), dim3(kThreads), 0, s, a);
 }
 
