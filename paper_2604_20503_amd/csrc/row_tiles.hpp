@@ -374,6 +374,12 @@ __device__ __forceinline__ float log_sum(Reference of, float l, float scale) {
 }
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_at(const char* base, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000); }
+// A store that goes past the caches of a die (16: its device-scope bit).  Whole lines of sums that other workgroups read: what lies in a die's
+// L2 at a launch's end has to be written from there before the next one starts (28 trees of 5-131 rows, 8/2 heads: 48.3 us, not 45.6).
+__device__ __forceinline__ void store_through(Buffer to, int at, f32x4 x) { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at, 0, 16); }
+
 // Where the result of a row's share of the keys goes.
 template <class C>
 struct Target {
@@ -420,7 +426,14 @@ __device__ __forceinline__ void hand_over(const Args& a, const Piece& p, int r_t
         each([&](int d, f32x4 x) { store4(to.out + d, x * inv); });
         if (first_lane && to.lse) *to.lse = log_sum<C::kOp>(of, l, a.scale);
     } else {
-        each([&](int d, f32x4 x) { store4(to.sums + d, x); });
+        if constexpr (C::kOp == kTree) {  // as the lanes hold them: 64 lanes' four columns beside each other
+            float* at = a.part_o + (size_t)p.slot * a.m_cap * C::kDv + (r_tile / C::kPartRows) * (C::kDv / C::kPartColumns) * 256 + (threadIdx.x & 63) * 4;
+            const Buffer sums = buffer_at((const char*)a.part_o, 0x7fffffffu);
+            const int base = (int)((at - a.part_o) * 4);
+            each([&](int d, f32x4 x) { store_through(sums, base + (d / C::kPartColumns) * 1024, x); });
+        } else {
+            each([&](int d, f32x4 x) { store4(to.sums + d, x); });
+        }
         if (first_lane) store4(to.ml, f32x4{of.raw, of.log2, l, 0.0f});
     }
 }
@@ -439,6 +452,7 @@ struct Simple {
     static constexpr int kItemCost = 2;  // key tiles that taking up an item is worth (measured: 14000 cycles against 7000)
     static constexpr bool kEven = false; // (even pieces)
     static constexpr int kMinShare = 1;  // units of a share of a short line: a tile of its own costs less than waiting for a neighbour's
+    static constexpr int kPartRows = 16, kPartColumns = 16;  // of a wave; for each four of a lane
     typedef float Out;
 };
 
@@ -615,6 +629,7 @@ struct Tiled {
     static constexpr bool kPair = sizeof(OUT) == 4;   // weights enter the second product as a pair of bf16
     static constexpr int kM = kTileRows, kKeys = 64;
     static constexpr int kBlockThreads = kThreads, kWaves = row_tiles::kWaves;
+    static constexpr int kPartRows = 32, kPartColumns = 8;  // of a wave; for each four of a lane
     static constexpr int kPerUnit = 2;                // workgroups of a compute unit, two waves to a SIMD
     static constexpr int kItemCost = OP == kTree ? 7 : 5;  // measured: 20000 cycles (loads that nothing hides, tiles with masked keys, sums on their way out) against 4000 a tile; of trees 23000 against 3100
     static constexpr int kMinShare = OP == kTree ? 1 : kItemCost + 1;  // (18 trees of 25-34 rows behind 221 tokens, 8/2 heads of 64: 15.6 us, not 19.7)
@@ -634,8 +649,6 @@ __device__ __forceinline__ void to_lds(const char* from, char* to) {
 
 // The same by a buffer descriptor, a lane's offset and a common one.  (Not only fewer instructions: behind a load in the other form the
 // compiler takes every wait for an LDS read to be one for all of them.)
-typedef __amdgpu_buffer_rsrc_t Buffer;
-__device__ __forceinline__ Buffer buffer_at(const char* base, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000); }
 __device__ __forceinline__ void to_lds(Buffer from, int lane_at, int at, char* to) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_at, at, 0, 0);
 }
@@ -1171,8 +1184,8 @@ struct Walk {
             p.share0 = share;
             p.pieces = 1;
             if (!p.whole) {
-                p.share0 = line.share_of(item + C::kItemCost);
-                p.pieces = line.share_of(item + C::kItemCost + nk - 1) - p.share0 + 1;
+                if constexpr (C::kOp != kTree) p.share0 = line.share_of(item + C::kItemCost);
+                if (C::kOp != kTree || p.t0 == 0) p.pieces = line.share_of(item + C::kItemCost + nk - 1) - p.share0 + 1;  // (of a tree's item only the first needs to know)
                 p.slot = 2 * share + (p.t0 == 0 ? 1 : 0);  // an item that begins here, or one that began before
                 if (C::kOp != kShared && p.t0 == 0 && threadIdx.x == 0) {
                     int32_t* desc = a.desc + (size_t)share * kDescInts;

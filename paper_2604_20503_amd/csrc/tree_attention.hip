@@ -28,7 +28,8 @@ int check(const fsr_attn_params* p, const char* who) {
 }
 
 Layout layout(const fsr_attn_params* p, int& m_cap) {
-    m_cap = (int)std::max(1LL, std::min((long long)p->N_cap * (p->H_q / p->H_kv), (long long)kTileRows));
+    // (whole rows of a wave's)
+    m_cap = (int)align_up((size_t)std::max(1LL, std::min((long long)p->N_cap * (p->H_q / p->H_kv), (long long)kTileRows)), 32);
     return layout_of(m_cap, p->D, (long long)p->N_cap * p->H_q, false);
 }
 

@@ -215,110 +215,92 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
     return true;
 }
 
-// Joins the pieces of an item, ROWS rows a wave.  Of 64 / ROWS pieces at once a lane takes the statistics of one piece of one row, so that a row's
-// largest reference and its sum take a few exchanges; then come the sums, 16 loads at a time.  (A wave that takes its rows one after the
-// other, all its lanes a row's pieces, waits for two round trips and twelve exchanges each time: 16 requests of 24-64 rows, 17 us.)
-template <class C, int ROWS>
+// Joins the pieces of an item.  Sums lie as the lanes of a wave held them, and so they are read: a lane has one row, whose statistics of all
+// pieces it takes for itself, and four columns of it at a time.  A workgroup joins the rows of one wave, each of its waves a quarter of the
+// columns.  (With a row's columns in a row, stores were of 32 bytes a row, 4500 cycles a piece, and a wave's lanes had to exchange
+// statistics: 16 requests of 24-64 rows, 32/8 heads, 9 us.)
+template <class C>
 __global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
-    constexpr int kColumns = C::kDv / 64, kChunk = kWave / ROWS, kBatch = ROWS == 1 ? 8 : 16 / ROWS;
+    constexpr int kGroups = C::kDv / C::kPartColumns, kMine = kGroups / kWaves, kChunk = 8, kBatch = 4;
+    static_assert(kGroups % kWaves == 0, "a share of the columns for each wave");
     constexpr Reference kNone{-INFINITY, 0.0f};
     const int32_t* desc = a.desc + (size_t)blockIdx.x * kDescInts;
     const int pieces = desc[0], row0 = desc[1], hk = desc[2], rt = desc[3], rows = desc[4], first_slot = desc[5], second_slot = desc[6], step = desc[7];
-    const int r0 = (blockIdx.y * kWaves + uniform(threadIdx.x >> 6)) * ROWS, lane = threadIdx.x & 63;
-    if (pieces <= 0 || r0 >= rows) return;
+    if (pieces <= 0 || (int)blockIdx.y * C::kPartRows >= rows) return;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), r = blockIdx.y * C::kPartRows + lane % C::kPartRows;
     auto slot = [&](int k) { return k == 0 ? first_slot : second_slot + (k - 1) * step; };
-    const int mine = lane % ROWS, piece = lane / ROWS, my_row = min(r0 + mine, rows - 1);
-    float o[ROWS][kColumns], l = 0.0f;  // (l and of: of the lane's row)
+    auto sums_of = [&](int k) { return reinterpret_cast<const f32x4*>(a.part_o + (size_t)slot(k) * a.m_cap * C::kDv) + (blockIdx.y * kGroups + wave * kMine) * 64 + lane; };
+    f32x4 o[kMine];
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) o[c] = f32x4{0, 0, 0, 0};
+    float l = 0.0f;
     Reference of = kNone;
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-        for (int c = 0; c < kColumns; ++c) o[r][c] = 0.0f;
     for (int first = 0; first < pieces; first += kChunk) {
         const int n = min(pieces - first, kChunk);
-        const f32x4 stats = *reinterpret_cast<const f32x4*>(a.part_ml + ((size_t)slot(first + min(piece, n - 1)) * a.m_cap + my_row) * 4);
-        const float pl = piece < n ? stats[2] : 0.0f;
-        const Reference pm = pl == 0.0f ? kNone : Reference{stats[0], stats[1]};  // (none: a piece without a visible key)
-        // Any number near the furthest reference will do; where powers of two are too coarse for one, it is that reference itself.
-        float top = fmaxf(fmaf(pm.raw, a.scale_log2, pm.log2), fmaf(of.raw, a.scale_log2, of.log2));
+        f32x4 stats[kChunk], y[kBatch][kMine];
 #pragma unroll
-        for (int x = ROWS; x < kWave; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
-        Reference use{0.0f, top};
-        if (__any(!(fabsf(top) <= kNear))) {
-            Reference furthest = distance(pm, of, a.scale_log2) > 0.0f ? pm : of;
+        for (int i = 0; i < kChunk; ++i)
+            if (i < n) stats[i] = reinterpret_cast<const f32x4*>(a.part_ml)[(size_t)slot(first + i) * a.m_cap + min(r, rows - 1)];
+        auto fetch = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int x = ROWS; x < kWave; x <<= 1) {
-                const Reference y{__shfl_xor(furthest.raw, x, kWave), __shfl_xor(furthest.log2, x, kWave)};
-                if (distance(y, furthest, a.scale_log2) > 0.0f) furthest = y;
-            }
-            furthest = Reference{__shfl(furthest.raw, mine, kWave), __shfl(furthest.log2, mine, kWave)};  // (lanes may hold different ones of the same height)
-            if (!(fabsf(top) <= kNear)) use = furthest;
-        }
-        const float before = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(of, use, a.scale_log2));
-        const float w = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(pm, use, a.scale_log2));
-        float sum = w * pl;
+            for (int i = 0; i < kBatch; ++i)
+                if (k0 + i < n) {
+                    const f32x4* x = sums_of(first + k0 + i);
 #pragma unroll
-        for (int x = ROWS; x < kWave; x <<= 1) sum += __shfl_xor(sum, x, kWave);
-        l = l * before + sum;
-        of = l == 0.0f ? kNone : use;
-        if (first > 0)
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-                for (int c = 0; c < kColumns; ++c) o[r][c] *= __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, before), r));
-        auto add = [&](int k0, auto many) __attribute__((always_inline)) {  // the sums of `many` pieces of all rows at once
-            float y[many.value][ROWS][kColumns];
-#pragma unroll
-            for (int i = 0; i < many.value; ++i) {
-                const float* x = a.part_o + (size_t)slot(first + k0 + i) * a.m_cap * C::kDv + lane * kColumns;
-#pragma unroll
-                for (int r = 0; r < ROWS; ++r) __builtin_memcpy(y[i][r], x + (size_t)min(r0 + r, rows - 1) * C::kDv, kColumns * 4);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < many.value; ++i)
-#pragma unroll
-                for (int r = 0; r < ROWS; ++r) {
-                    const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), (k0 + i) * ROWS + r));
-#pragma unroll
-                    for (int c = 0; c < kColumns; ++c) o[r][c] = fmaf(wk, y[i][r][c], o[r][c]);
+                    for (int c = 0; c < kMine; ++c) y[i][c] = x[c * 64];
                 }
         };
-        int k0 = 0;
-#pragma unroll 1
-        for (; n - k0 >= kBatch; k0 += kBatch) add(k0, std::integral_constant<int, kBatch>());
-        if (kBatch > 4 && n - k0 >= 4) add(k0, std::integral_constant<int, 4>()), k0 += 4;
-        if (kBatch > 2 && n - k0 >= 2) add(k0, std::integral_constant<int, 2>()), k0 += 2;
-        if (kBatch > 1 && n - k0 >= 1) add(k0, std::integral_constant<int, 1>());
-    }
-    const float inv = inverse(l);
+        fetch(0);
+        // Any number near the furthest reference will do; where powers of two are too coarse for one, it is that reference itself.
+        float top = fmaf(of.raw, a.scale_log2, of.log2);
+        Reference furthest = of;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        if (r0 + r >= rows) break;
-        const Place to = place_of(a, row0, hk, rt * C::kM + r0 + r);
-        const size_t row = (size_t)to.row * a.H + to.head;
-        const float by = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inv), r));
-        typename C::Out y[kColumns];
-#pragma unroll
-        for (int c = 0; c < kColumns; ++c) {
-            if constexpr (sizeof(typename C::Out) == 2) y[c] = (uint16_t)bf16_bits(o[r][c] * by);
-            else y[c] = o[r][c] * by;
+        for (int i = 0; i < kChunk; ++i) {
+            if (i >= n || stats[i][2] == 0.0f) continue;  // (a piece without a visible key)
+            const Reference pm{stats[i][0], stats[i][1]};
+            top = fmaxf(top, fmaf(pm.raw, a.scale_log2, pm.log2));
+            if (distance(pm, furthest, a.scale_log2) > 0.0f) furthest = pm;
         }
-        __builtin_memcpy((typename C::Out*)a.out + row * C::kDv + lane * kColumns, y, sizeof y);
+        const Reference use = fabsf(top) <= kNear ? Reference{0.0f, top} : furthest;
+        const float before = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(of, use, a.scale_log2));
+        l *= before;
+#pragma unroll
+        for (int c = 0; c < kMine; ++c) o[c] *= before;
+        float w[kChunk];
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            const float pl = i < n ? stats[i][2] : 0.0f;
+            w[i] = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(Reference{stats[i][0], stats[i][1]}, use, a.scale_log2));
+            l = fmaf(w[i], pl, l);
+        }
+        of = l == 0.0f ? kNone : use;
+#pragma unroll
+        for (int k0 = 0; k0 < kChunk; k0 += kBatch) {
+            if (k0 > 0 && k0 < n) fetch(k0);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (k0 + i < n)
+#pragma unroll
+                    for (int c = 0; c < kMine; ++c)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[c][e] = fmaf(w[k0 + i], y[i][c][e], o[c][e]);
+        }
     }
-    if (a.lse && lane < ROWS && r0 + lane < rows) {
-        const Place to = place_of(a, row0, hk, rt * C::kM + r0 + lane);
-        a.lse[(size_t)to.row * a.H + to.head] = log_sum<C::kOp>(of, l, a.scale);
-    }
+    if (r >= rows) return;
+    const float inv = inverse(l);
+    const Place to = place_of(a, row0, hk, rt * C::kM + r);
+    const size_t row = (size_t)to.row * a.H + to.head;
+    // (Tiled: group b, g of a lane's half h are columns 32 b + 8 g + 4 h; Simple: of lane group lg 16 b + 4 lg)
+    typename C::Out* out = (typename C::Out*)a.out + row * C::kDv + wave * kMine * C::kPartColumns + (lane / C::kPartRows) * 4;
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) store4(out + c * C::kPartColumns, o[c] * inv);
+    if (a.lse && wave == 0 && lane < C::kPartRows) a.lse[row] = log_sum<C::kOp>(of, l, a.scale);
 }
 
-// Four rows a wave where tiles are large (16 requests of 24-64 rows, 32/8 heads: 86.8 us; two rows 90.0, eight 87.8; 28 of 5-131, 8/2 heads:
-// 48.9, 50.5 and 52.0), one where they are not and pieces are many (fp32, 2-23 rows, 28/4 heads: 20.4; two rows 22.5, four 23.1).
 template <class C>
 void launch_tree_join(const Args& a, hipStream_t s) {
     const int rows = std::min(a.m_cap, C::kM);
-    if (rows > 64) hipLaunchKernelGGL((join_tree_kernel<C, 4>), dim3(a.nb, (rows + 4 * kWaves - 1) / (4 * kWaves)), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((join_tree_kernel<C, 1>), dim3(a.nb, (rows + kWaves - 1) / kWaves), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((join_tree_kernel<C>), dim3(a.nb, (rows + C::kPartRows - 1) / C::kPartRows), dim3(kThreads), 0, s, a);
 }
 
 template <int KH, int KT, int DV, class OUT, bool PAGES16>
