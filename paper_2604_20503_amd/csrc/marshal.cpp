@@ -13,6 +13,8 @@
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/cuda/Event.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/utils/object_ptr.h>
 #include <ATen/ops/empty.h>
 
 #include <cstdint>
@@ -186,39 +188,32 @@ PyObject* without_system_fence(PyObject*, PyObject* event) {
 // new(like, types, *sizes): uninitialised tensors on the device of `like`, one for each letter of types ('f' float32, 'i' int32, 'b'
 // uint8, 't' as `like`) and tuple of sizes.  (torch.empty from Python takes 1.4 us apiece, here 0.5.)
 PyObject* new_tensors(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS  // (as torch's own calls: out of memory is torch.OutOfMemoryError)
     const char* types = n >= 2 ? PyUnicode_AsUTF8(args[1]) : nullptr;
     if (n < 2 || !THPVariable_Check(args[0]) || !types || (Py_ssize_t)std::char_traits<char>::length(types) != n - 2) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "a tensor, a letter for each result, and their sizes as tuples are wanted");
         return nullptr;
     }
-    PyObject* out = PyTuple_New(n - 2);
+    const at::Tensor& like = THPVariable_Unpack(args[0]);
+    THPObjectPtr out(PyTuple_New(n - 2));
     if (!out) return nullptr;
-    try {
-        const at::Tensor& like = THPVariable_Unpack(args[0]);
-        for (Py_ssize_t k = 0; k < n - 2; ++k) {
-            PyObject* sizes = args[k + 2];
-            c10::SmallVector<int64_t, 5> shape;
-            const Py_ssize_t dims = PyTuple_Check(sizes) ? PyTuple_GET_SIZE(sizes) : -1;
-            for (Py_ssize_t d = 0; d < dims; ++d) shape.push_back(PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, d)));
-            if (dims < 0 || PyErr_Occurred()) {
-                if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "sizes are tuples");
-                Py_DECREF(out);
-                return nullptr;
-            }
-            const char t = types[k];
-            const at::ScalarType type = t == 'f' ? at::kFloat : t == 'i' ? at::kInt : t == 'b' ? at::kByte : like.scalar_type();
-            PyTuple_SET_ITEM(out, k, THPVariable_Wrap(at::empty(shape, like.options().dtype(type).requires_grad(false))));
-            if (!PyTuple_GET_ITEM(out, k)) {
-                Py_DECREF(out);
-                return nullptr;
-            }
+    for (Py_ssize_t k = 0; k < n - 2; ++k) {
+        PyObject* sizes = args[k + 2];
+        if (!PyTuple_Check(sizes)) {
+            PyErr_SetString(PyExc_TypeError, "sizes are tuples");
+            return nullptr;
         }
-    } catch (const std::exception& e) {  // (out of memory, sizes below zero)
-        Py_DECREF(out);
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+        c10::SmallVector<int64_t, 5> shape;
+        for (Py_ssize_t d = 0; d < PyTuple_GET_SIZE(sizes); ++d) shape.push_back(PyLong_AsLongLong(PyTuple_GET_ITEM(sizes, d)));
+        if (PyErr_Occurred()) return nullptr;
+        const char t = types[k];
+        const at::ScalarType type = t == 'f' ? at::kFloat : t == 'i' ? at::kInt : t == 'b' ? at::kByte : like.scalar_type();
+        PyObject* made = THPVariable_Wrap(at::empty(shape, like.options().dtype(type).requires_grad(false)));
+        if (!made) return nullptr;
+        PyTuple_SET_ITEM(out.get(), k, made);
     }
-    return out;
+    return out.release();
+    END_HANDLE_TH_ERRORS
 }
 
 PyMethodDef methods[] = {{"new", (PyCFunction)(void (*)())new_tensors, METH_FASTCALL, "new(like, types, *sizes): uninitialised tensors"},
