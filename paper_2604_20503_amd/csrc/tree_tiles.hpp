@@ -218,10 +218,11 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
 // Joins the pieces of an item.  Sums lie as the lanes of a wave held them, and so they are read: a lane has one row, whose statistics of all
 // pieces it takes for itself, and four columns of it at a time.  A workgroup joins the rows of one wave, each of its waves a quarter of the
 // columns.  (With a row's columns in a row, stores were of 32 bytes a row, 4500 cycles a piece, and a wave's lanes had to exchange
-// statistics: 16 requests of 24-64 rows, 32/8 heads, 9 us.)
+// statistics.)  Eight pieces are under way at once (four: 12 rows behind 777 tokens, 32/8 heads, 18.5 us, not 17.5); with sixteen, or the
+// columns over more workgroups, which compute the same weights again, 16 requests of 24-64 rows took up to 14 us more, of 82.
 template <class C>
 __global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
-    constexpr int kGroups = C::kDv / C::kPartColumns, kMine = kGroups / kWaves, kChunk = 8, kBatch = 4;
+    constexpr int kGroups = C::kDv / C::kPartColumns, kMine = kGroups / kWaves, kChunk = 8;
     static_assert(kGroups % kWaves == 0, "a share of the columns for each wave");
     constexpr Reference kNone{-INFINITY, 0.0f};
     const int32_t* desc = a.desc + (size_t)blockIdx.x * kDescInts;
@@ -237,26 +238,27 @@ __global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
     Reference of = kNone;
     for (int first = 0; first < pieces; first += kChunk) {
         const int n = min(pieces - first, kChunk);
-        f32x4 stats[kChunk], y[kBatch][kMine];
+        f32x4 stats[kChunk], y[kChunk][kMine];
 #pragma unroll
         for (int i = 0; i < kChunk; ++i)
             if (i < n) stats[i] = reinterpret_cast<const f32x4*>(a.part_ml)[(size_t)slot(first + i) * a.m_cap + min(r, rows - 1)];
-        auto fetch = [&](int k0) __attribute__((always_inline)) {
+        auto fetch = [&]() __attribute__((always_inline)) {  // (in two plain loops, of which the compiler makes one: 8 requests in fp32 17.6 us, not 15.1)
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (k0 + i < n) {
-                    const f32x4* x = sums_of(first + k0 + i);
+            for (int i = 0; i < kChunk; ++i)
+                if (i < n) {
+                    const f32x4* x = sums_of(first + i);
 #pragma unroll
                     for (int c = 0; c < kMine; ++c) y[i][c] = x[c * 64];
                 }
         };
-        fetch(0);
+        fetch();
         // Any number near the furthest reference will do; where powers of two are too coarse for one, it is that reference itself.
         float top = fmaf(of.raw, a.scale_log2, of.log2);
         Reference furthest = of;
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) {
-            if (i >= n || stats[i][2] == 0.0f) continue;  // (a piece without a visible key)
+            if (i >= n) break;
+            if (stats[i][2] == 0.0f) continue;  // (a piece without a visible key)
             const Reference pm{stats[i][0], stats[i][1]};
             top = fmaxf(top, fmaf(pm.raw, a.scale_log2, pm.log2));
             if (distance(pm, furthest, a.scale_log2) > 0.0f) furthest = pm;
@@ -269,22 +271,19 @@ __global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
         float w[kChunk];
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) {
-            const float pl = i < n ? stats[i][2] : 0.0f;
+            if (i >= n) break;
+            const float pl = stats[i][2];
             w[i] = pl == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(distance(Reference{stats[i][0], stats[i][1]}, use, a.scale_log2));
             l = fmaf(w[i], pl, l);
         }
         of = l == 0.0f ? kNone : use;
 #pragma unroll
-        for (int k0 = 0; k0 < kChunk; k0 += kBatch) {
-            if (k0 > 0 && k0 < n) fetch(k0);
+        for (int i = 0; i < kChunk; ++i)
+            if (i < n)
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (k0 + i < n)
+                for (int c = 0; c < kMine; ++c)
 #pragma unroll
-                    for (int c = 0; c < kMine; ++c)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[c][e] = fmaf(w[k0 + i], y[i][c][e], o[c][e]);
-        }
+                    for (int e = 0; e < 4; ++e) o[c][e] = fmaf(w[i], y[i][c][e], o[c][e]);
     }
     if (r >= rows) return;
     const float inv = inverse(l);

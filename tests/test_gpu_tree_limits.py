@@ -195,3 +195,20 @@ def test_offsets_that_do_not_hold_together_stay_inside_the_tensors(fsr):
             fsr.kv_commit(cache.clone(), cache.clone(), bt, i32(ctx), i32([3, 90]), i32([[0, 5, 1 << 30, 9], [0, -4, 7, 1 << 20]]))
     torch.cuda.synchronize()
     assert (guard[:10] == 7).all() and (guard[20:] == 7).all() and torch.equal(cache, before)
+
+
+def test_two_calls_at_once(fsr):
+    """Log probabilities of two batches on two streams, many times: each call has its own workspace."""
+    announce("log probabilities, two streams")
+    z = [logprobs.logits(5, 60000, BF, seed=1), logprobs.logits(3, 128256, F32, seed=2)]
+    want = [[x.clone() for x in fsr.token_logprobs(x, top_k=9)[1:]] for x in z]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in z]
+    for _ in range(20):
+        got = []
+        for x, s in zip(z, streams):
+            with torch.cuda.stream(s):
+                got.append(fsr.token_logprobs(x, top_k=9)[1:])
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(g, w))
