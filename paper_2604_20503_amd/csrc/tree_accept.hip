@@ -4,11 +4,12 @@
 // A tree is given by its rows' bits: a row's parent is the highest of its bits below itself.  fsr_tree_accept looks at all rows at
 // once for a child that carries the token which the target chose at its parent (the first one, by an atomic minimum: the result does
 // not depend on the order), then walks down from the first row.  One wave a request; bound by a few round trips to memory, then by
-// one LDS read per accepted token.
+// one LDS read per accepted token: 12 rows 2 us, 256 requests of 8-160 rows 4 us.
 //
 // fsr_kv_commit: path[k] >= k, so that a row moves to the front or stays.  A thread owns 16 bytes of one head for all rows of a
 // request: it reads kBatch rows of the path, then writes them, in ascending order.  A write at place k meets no later read: those are
-// at places >= k' > k.
+// at places >= k' > k.  Bound by the round trips length -> path -> pages -> rows: 8 heads of 128, up to 8 tokens, 4 requests 5 us,
+// 256 (8-bit, 4 MB) 6 us.
 #include <algorithm>
 #include <cstdint>
 

@@ -1,6 +1,10 @@
 // Verification attention of trees: a request's rows are a tree of drafted tokens, and a row attends to the context and to its
 // ancestors.  The rows of a request and the query heads of a KV head are packed into tiles (row_tiles.hpp); keys of the context are seen
 // by all of them, so that only the last tiles of an item, where the call's own rows lie, look at the rows' bits.
+//
+// 12 requests of 33-150 rows behind 2048-16384 tokens, 64/8 heads of 128: 302 us, 760 TFLOP/s, bound by LDS (2560 of a tile's 3100 cycles);
+// 16 of 24-64 rows behind 1024-4096 tokens, 32/8 heads: 80 us, of which the starts and ends of pieces (23000 cycles each) and the join (10
+// us) are a half; 12 rows behind 777 tokens: 16.4 us, two launches and two chains of loads.
 #include "tree_tiles.hpp"
 
 namespace fsr {

@@ -218,7 +218,7 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
 // Joins the pieces of an item.  Sums lie as the lanes of a wave held them, and so they are read: a lane has one row, whose statistics of all
 // pieces it takes for itself, and four columns of it at a time.  A workgroup joins the rows of one wave, each of its waves a quarter of the
 // columns.  (With a row's columns in a row, stores were of 32 bytes a row, 4500 cycles a piece, and a wave's lanes had to exchange
-// statistics.)  Eight pieces are under way at once (four: 12 rows behind 777 tokens, 32/8 heads, 18.5 us, not 17.5); with sixteen, or the
+// statistics.)  Eight pieces are under way at once (four: 12 rows behind 777 tokens, 32/8 heads, 18.5 us, not 16.4); with sixteen, or the
 // columns over more workgroups, which compute the same weights again, 16 requests of 24-64 rows took up to 14 us more, of 82.
 template <class C>
 __global__ __launch_bounds__(kThreads) void join_tree_kernel(Args a) {
