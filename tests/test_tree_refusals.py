@@ -184,3 +184,18 @@ def test_binding_refuses_what_does_not_fit():
         x = {**dict(z=z, tokens=i32(4)), **bad}
         with pytest.raises(ValueError):
             b.token_logprobs(x.pop("z"), x.pop("tokens"), top_k=5, **x)
+
+
+def test_call_ids_are_no_bytes_of_other_tensors(lib):
+    """What tells a call's arrivals from whatever a workspace held before (the word's upper 48 bits) is met by no bytes of masks, no indexes
+    and no counts, from a process's first call on."""
+    next_id = lib._ZN3fsr12next_call_idEv
+    next_id.restype, next_id.argtypes = ctypes.c_ulonglong, []
+    ids = [next_id() for _ in range(300)]
+    assert len(set(ids)) == 300 and all(0 < i < 1 << 48 for i in ids)
+    for i in ids:
+        word = i << 16
+        tail = word.to_bytes(8, "little")[2:]  # (the count is below)
+        assert any(x > 1 for x in tail), "a mask's bytes"
+        assert word >= 1 << 62, "64-bit indexes"
+        assert abs(float(torch.tensor([(i >> 32) - (1 << 16)], dtype=torch.int16).view(torch.bfloat16))) > 1e30, "floats, bf16"
