@@ -162,7 +162,10 @@ struct Shared {
     double s[kThreads / kWave], e[kThreads / kWave];
     float m[kThreads / kWave];
     uint32_t set_top[kWave], set_id[kWave];  // keys of 64 sets, in halves
-    int count[kThreads / kWave], n, last;
+    // Lengths of the lists: of groups, of the chunk's keys, of all chunks' keys.  Each has a counter of its own, cleared at the start: one that is
+    // used again would have to be cleared behind a barrier that every wave reaches after it has read it.
+    int groups, keys, joined;
+    int count[kThreads / kWave], last;
     int chosen[FSR_TOP_MAX];
     uint64_t top[FSR_TOP_MAX];
     uint64_t list[kGroupsMax];
@@ -266,7 +269,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
     // sums of the chunk
     const float wave_m = wave_max_by_dpp(sums.m);
     if (lane == 0) sh.m[wave] = wave_m;
-    if (threadIdx.x == 0) sh.n = 0;
+    if (threadIdx.x == 0) sh.groups = sh.keys = sh.joined = 0;
     // A bound that at least K groups are not below, and few more are: the K-th of the largest keys of 64 sets of four threads each.
     if (TOP) {
         static_assert(kWaves == 4, "four lanes a set");
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
             if (!(top < least_top) && has(t)) {
                 const uint64_t k = group_key(top, t);
                 if (k >= least) {
-                    const int at = atomicAdd(&sh.n, 1);
+                    const int at = atomicAdd(&sh.groups, 1);
                     if (at < kGroupsMax) sh.list[at] = k;
                 }
             }
@@ -308,7 +311,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
         }
         for (; t < tiles; ++t) look(tops[t * kThreads + threadIdx.x], t);
         __syncthreads();
-        int n = sh.n;
+        int n = sh.groups;
         if (n > kGroupsMax) {
             // Many groups of few threads: the K-th key, bit by bit.
             uint64_t kth = 0;
@@ -324,14 +327,14 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
                 if (c >= a.K) kth = probe;
                 __syncthreads();
             }
-            if (threadIdx.x == 0) sh.n = 0;
+            if (threadIdx.x == 0) sh.groups = 0;  // (everyone has read it, 64 times two barriers ago)
             __syncthreads();
             for (int t = 0; t < tiles; ++t) {
                 const uint64_t k = has(t) ? group_key(tops[t * kThreads + threadIdx.x], t) : 0;
-                if (k != 0 && k >= kth) sh.list[min(atomicAdd(&sh.n, 1), kGroupsMax - 1)] = k;
+                if (k != 0 && k >= kth) sh.list[min(atomicAdd(&sh.groups, 1), kGroupsMax - 1)] = k;
             }
             __syncthreads();
-            n = sh.n;
+            n = sh.groups;
         }
         // The logits of those groups that are not below the last group's largest one (of fewer than K groups: all).  A few groups more
         // than K are read as they are.
@@ -345,15 +348,13 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
             groups = a.K;
             bound = sh.top[a.K - 1] >> 32 << 32;
         }
-        if (threadIdx.x == 0) sh.n = 0;
-        __syncthreads();
         for (int i = threadIdx.x; i < groups * N; i += kThreads) {
             const int id = first + id_of_key(groups_of[i / N]) * N + i % N;
             const uint64_t k = id < a.V ? key_of(value_of(z + id), id) : 0;
-            if (k >= bound && k != 0) keys[atomicAdd(&sh.n, 1)] = k;
+            if (k >= bound && k != 0) keys[atomicAdd(&sh.keys, 1)] = k;  // (where the groups' largest logits lay: all have been read)
         }
         __syncthreads();
-        n = sh.n;
+        n = sh.keys;
         rank(keys, n, a.K, sh.top);
     }
     __syncthreads();
@@ -406,15 +407,14 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(LogprobArgs a) {
                 sh.set_top[threadIdx.x] = (uint32_t)(jth >> 32);
                 sh.set_id[threadIdx.x] = (uint32_t)jth;
             }
-            if (threadIdx.x == 0) sh.n = 0;
             __syncthreads();
             const uint64_t bound = rth_of_64(sh, r);
-            auto list = [&](uint64_t key) { if (key >= bound) keys[atomicAdd(&sh.n, 1)] = key; };
+            auto list = [&](uint64_t key) { if (key >= bound) keys[atomicAdd(&sh.joined, 1)] = key; };
 #pragma unroll
             for (int i = 0; i < kMine; ++i) list(k[i]);
             for (int at = threadIdx.x + kMine * kThreads; at < total; at += kThreads) list(fetch(theirs_keys + at));
             __syncthreads();
-            const int n = sh.n;
+            const int n = sh.joined;
             rank(keys, n, a.K, sh.top);
         }
         __syncthreads();

@@ -1,0 +1,78 @@
+"""Kernels whose waves hand each other data through LDS, on the CPU with the waves in orders of our choice: no result may depend on it."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+import workgroup_on_cpu
+
+BF, F32 = torch.bfloat16, torch.float32
+ORDERS = [0, 1, 2, 3]  # of waves: ascending, descending, two shuffles
+U = 2.0 ** -24
+
+pytestmark = pytest.mark.skipif(not os.path.exists(workgroup_on_cpu.CLANG), reason="no clang for the host")
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    lib = workgroup_on_cpu.build(str(tmp_path_factory.mktemp("kernels")), ["library.hip", "token_logprobs.hip"])
+    lib.fsr_last_error.restype = ctypes.c_char_p
+    return lib
+
+
+def pointer(x):
+    return None if x is None else ctypes.c_void_p(x.data_ptr())
+
+
+def aligned(n):
+    """n bytes of a workspace."""
+    room = torch.randint(0, 255, (n + 256,), dtype=torch.uint8)
+    return room[-room.data_ptr() % 256:][:n]
+
+
+def token_logprobs(lib, z, tokens, K, T=1.0, N_cap=None):
+    """The first rows' results; N_cap: rows allocated, of which a call's cut depends."""
+    from paper_2604_20503_amd.binding import LogprobParams
+
+    (N, V), N_cap = z.shape, N_cap or len(z)
+    p = LogprobParams(N_cap=N_cap, V=V, M=tokens.shape[1], K=K, dtype=int(z.dtype == BF), reserved=0, stride=V, temperature=T)
+    need = ctypes.c_size_t()
+    assert lib.fsr_logprob_workspace_bytes(ctypes.byref(p), ctypes.byref(need)) == 0
+    ws, n_rows = aligned(need.value), torch.tensor([N], dtype=torch.int32)
+    lp, entropy, ids, top = torch.empty(tokens.shape), torch.empty(N), torch.full((N, K), -7, dtype=torch.int32), torch.empty(N, K)
+    rc = lib.fsr_token_logprobs(pointer(z), pointer(n_rows), pointer(tokens), pointer(lp), pointer(entropy), pointer(ids), pointer(top), ctypes.byref(p), pointer(ws),
+                                ctypes.c_size_t(need.value), None)
+    assert rc == 0, lib.fsr_last_error()
+    return lp, entropy, ids, top
+
+
+def rows(kind, V):
+    gen = torch.Generator().manual_seed(V)
+    if kind == "normal":
+        return torch.randn(1, V, generator=gen) * 2.5
+    if kind == "equal":  # every group has the largest logit: more groups than are listed
+        return torch.zeros(1, V)
+    z = torch.full((1, V), -float("inf"))  # a few that are allowed
+    z[0, torch.randperm(V, generator=gen)[:9]] = torch.randn(9, generator=gen)
+    return z
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("kind,V,K", [("normal", 5000, 5), ("normal", 700, 20), ("normal", 20000, 64), ("equal", 14000, 3), ("few", 6000, 20), ("normal", 3, 2)])
+def test_alternatives_do_not_depend_on_the_order_of_waves(lib, kind, V, K, dtype, order):
+    lib.set_wave_order(order)
+    N_cap = 1024 if kind == "equal" else 1  # (a row in one chunk, of more groups than are listed; or in as many as it has tiles)
+    z = rows(kind, V).to(dtype)
+    tokens = torch.tensor([[0, V - 1]], dtype=torch.int32)
+    lp, entropy, ids, top = token_logprobs(lib, z, tokens, K, N_cap=N_cap)
+    x = z.double()
+    want = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :K]
+    assert torch.equal(ids, want.int())
+    logp = torch.log_softmax(x, 1)
+    # a sum of V weights, each off by 2 u and 3 u |x|, |x| < 40 where a weight counts; added up in any order: V u
+    off = (V + 130) * U
+    for got, exact in ((lp, logp.gather(1, tokens.long())), (top, logp.gather(1, want))):
+        same = got.double() == exact
+        assert (same | ((got.double() - exact).abs() <= off + U * exact.abs())).all()
