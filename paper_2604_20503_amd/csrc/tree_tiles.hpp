@@ -190,19 +190,17 @@ __device__ __forceinline__ bool run_tree(const Args& a, const Piece& p, char* bu
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);  // the load too many has its place until it has come
     }
-    if constexpr (C::kPair) {
-        if (p.t1 - p.t0 > 1) {
-            float odd = 0.0f;
+    if constexpr (C::kPair) {  // (of one tile of the context too: its values have not been looked at)
+        float odd = 0.0f;
 #pragma unroll
-            for (int b = 0; b < R::kBlocks; ++b)
+        for (int b = 0; b < R::kBlocks; ++b)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) odd = fmaf(w.acc[b][e], 0.0f, odd);
-            const int mine = __any(odd != 0.0f);
-            __syncthreads();
-            if (lane == 0) flags[wave] = mine;
-            __syncthreads();
-            if (uniform(flags[0] | flags[1] | flags[2] | flags[3])) return false;
-        }
+            for (int e = 0; e < 16; ++e) odd = fmaf(w.acc[b][e], 0.0f, odd);
+        const int mine = __any(odd != 0.0f);
+        __syncthreads();
+        if (lane == 0) flags[wave] = mine;
+        __syncthreads();
+        if (uniform(flags[0] | flags[1] | flags[2] | flags[3])) return false;
     }
     w.l += other_half(w.l);
     if (active && first + li < n_packed)
