@@ -685,6 +685,7 @@ struct TileLoads {
     typedef RowLoads<CV, C::kWaves> Value;
     static constexpr int kTails = CT ? Tail::kEach : 0, kEach = Head::kEach + kTails + Value::kEach;
     Where next;
+    int next_key;        // the wave's first (of rows that follow each other)
     uint32_t slot;
     Buffer head, tail, value;
     int head_xor, head_add, tail_at, value_xor, value_add;
@@ -698,7 +699,8 @@ struct TileLoads {
     }
     __device__ __forceinline__ void find(const Args& a, const Piece& p, int t, int wave, int lane) {
         const int key = p.q.k_begin + t * C::kKeys;
-        next = find_key<C::kOp>(a, p.q, C::kPages16 ? min(key + 16 * wave, (p.q.k_end - 1) & ~15) : min(key + lane, p.q.k_end - 1));
+        next_key = C::kPages16 ? min(key + 16 * wave, (p.q.k_end - 1) & ~15) : min(key + lane, p.q.k_end - 1);
+        next = find_key<C::kOp>(a, p.q, next_key);
     }
     // The loads to come are those of the tile that has been found.
     __device__ __forceinline__ void take(const Args& a, const Piece& p) {
@@ -707,15 +709,19 @@ struct TileLoads {
             slot = (uint32_t)uniform((int)slot);
             // (behind the last key there may be no row: a load from there is zeros)
             const uint32_t rows = C::kOp == kExpanded ? min((uint32_t)a.T_cap - min(slot, (uint32_t)a.T_cap), 16u) : 16u;
-            auto at = [&](const char* base, uint32_t stride) { return buffer_at(base + (uint64_t)slot * stride, rows ? (rows - 1) * stride + stride : 0u); };
-            head = at(a.k_head + (size_t)p.hk * a.head_hk, a.head_stride);
-            if constexpr (CT > 0) tail = at(a.k_tail, a.tail_stride);
-            value = at(a.v + (size_t)p.hk * a.v_hk, a.v_stride);
+            // (A tree's values in a page's free slots, which may be anything and meet weights of 0, are zeros too.)
+            const uint32_t values = C::kOp == kTree ? (uint32_t)min(p.q.k_end - next_key, 16) : rows;
+            auto at = [&](const char* base, uint32_t stride, uint32_t n) { return buffer_at(base + (uint64_t)slot * stride, n ? (n - 1) * stride + stride : 0u); };
+            head = at(a.k_head + (size_t)p.hk * a.head_hk, a.head_stride, rows);
+            if constexpr (CT > 0) tail = at(a.k_tail, a.tail_stride, rows);
+            value = at(a.v + (size_t)p.hk * a.v_hk, a.v_stride, values);
         }
     }
-    // (Where rows may end inside the 16, in the expanded form, all of the offset is the lane's: that is what is held against the descriptor.)
+    // (Where rows may end inside the 16, in the expanded form and among a tree's values, all of the offset is the lane's: that is what is held
+    // against the descriptor.)
+    template <bool ENDS = C::kOp == kExpanded>
     static __device__ __forceinline__ void get(Buffer from, int lane_at, int at, char* to) {
-        if constexpr (C::kOp == kExpanded) to_lds(from, lane_at + at, 0, to);
+        if constexpr (ENDS) to_lds(from, lane_at + at, 0, to);
         else to_lds(from, lane_at, at, to);
     }
     __device__ __forceinline__ void issue(int i, const Args& a, const Piece& p, char* buf, int wave, int lane) const {
@@ -729,7 +735,7 @@ struct TileLoads {
             else Tail::issue(j, a.k_tail, a.tail_stride, slot, buf + C::kTailAt, wave, lane);
         } else {
             const int j = i - Head::kEach - kTails, k = j * Value::kRows;
-            if constexpr (C::kPages16) get(value, (value_xor ^ ((k & 7) << 5)) + value_add, k * (int)a.v_stride, buf + C::kVAt + (16 * wave + k) * C::kDv * 2);
+            if constexpr (C::kPages16) get<C::kOp == kExpanded || C::kOp == kTree>(value, (value_xor ^ ((k & 7) << 5)) + value_add, k * (int)a.v_stride, buf + C::kVAt + (16 * wave + k) * C::kDv * 2);
             else Value::issue(j, a.v + (size_t)p.hk * a.v_hk, a.v_stride, slot, buf + C::kVAt, wave, lane);
         }
     }

@@ -3,7 +3,8 @@
 // Tiles of the context are those of row_tiles.hpp: whole, with nothing but products in the loop.  The first tile of a piece, which finds
 // the rows' references, and the tiles in which the call's own rows lie, which look at the rows' bits, take one path of their own: all
 // scores, then their largest, then weights, then the second product, for 64 keys at once.  Where the values of a tile with the call's own
-// rows are not all finite (each wave looks at 16 of them), the piece is given up and taken as row_tiles.hpp takes any.
+// rows are not all finite (each wave looks at 16 of them), the piece is given up and taken as row_tiles.hpp takes any: its keys are read twice.
+// Slots of the last page that no row has yet are no part of this, whatever they hold.
 #pragma once
 #include "row_tiles.hpp"
 
