@@ -711,7 +711,9 @@ int fsr_logprob_workspace_bytes(const fsr_logprob_params* p /*host*/, size_t* ou
  *   top_ids      [N_cap, K] int32, top_logprobs [N_cap, K] float32: the K largest logits in descending order, the lowest id first
  *                among equals
  * of logits [N_cap, V] dtype, rows `stride` elements apart.  A NaN logit counts as -inf, which has probability 0.  A row without a
- * finite logit, or with one that is +inf, has NaN for its log probabilities and entropy; its top_ids are as ever.
+ * finite logit, or with one that is +inf, has NaN for its log probabilities and entropy; its top_ids are as ever.  Of a row in which
+ * one token has nearly all the mass, that token's log probability and the entropy are as small as the mass of the others, and as
+ * precise as fp32 sums of it (down to about 1e-14).
  *   tokens [N_cap, M] int32;  n_rows nullable [1] int32, device: rows from n_rows[0] on are neither read nor written (&cu_q[B])
  *   workspace >= fsr_logprob_workspace_bytes(p) bytes, 256-byte aligned
  */

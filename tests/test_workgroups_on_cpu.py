@@ -76,3 +76,35 @@ def test_alternatives_do_not_depend_on_the_order_of_waves(lib, kind, V, K, dtype
     for got, exact in ((lp, logp.gather(1, tokens.long())), (top, logp.gather(1, want))):
         same = got.double() == exact
         assert (same | ((got.double() - exact).abs() <= off + U * exact.abs())).all()
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V,at,N_cap", [(3, 1, 1), (5000, 4999, 1), (20000, 0, 1), (14000, 7000, 1024)])
+def test_digits_of_a_near_certain_token(lib, V, at, N_cap, dtype, order):
+    """log p of a token that has nearly all the mass is about minus the mass of all others, and keeps its digits."""
+    lib.set_wave_order(order)
+    z = rows("normal", V)
+    z[0, at] = 30.0
+    z = z.to(dtype)
+    lp, entropy, ids, _ = token_logprobs(lib, z, torch.tensor([[at]], dtype=torch.int32), 1, N_cap=N_cap)
+    x = z.double() - 30.0
+    x[0, at] = -float("inf")
+    rest, much = x.exp().sum(), (x.exp() * x.clamp(min=-99)).sum()
+    want, H = -torch.log1p(rest), torch.log1p(rest) - much / (1 + rest)
+    # a weight is off by 3 u |x| + 2 u, |x| < 45; a thread adds V / 256 of them (or all of its tiles'), a few sums more; sums of 1 and more are
+    # kept in 53 bits
+    off = (137 + V / 256 + 60) * U
+    assert ids[0, 0] == at and abs(lp[0, 0].double() - want) <= off * want.abs() + 2.0 ** -47
+    assert abs(entropy[0].double() - H) <= 3 * off * H + 2.0 ** -47
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("at", [0, 700, 2999])
+def test_one_logit_at_the_end_of_the_type(lib, at, order):
+    """The lowest finite logit is the only one: it has all the mass."""
+    lib.set_wave_order(order)
+    z = torch.full((1, 3000), -float("inf"))
+    z[0, at] = torch.finfo(F32).min
+    lp, entropy, ids, top = token_logprobs(lib, z, torch.tensor([[at, (at + 1) % 3000]], dtype=torch.int32), 1)
+    assert lp.tolist() == [[0.0, -float("inf")]] and entropy.tolist() == [0.0] and ids.tolist() == [[at]] and top.tolist() == [[0.0]]
