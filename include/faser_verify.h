@@ -642,10 +642,11 @@ int fsr_verify_attention_shared(const void* q, const void* k_cache, const void* 
  * elements from R on, and values, stay as they are.  t is positions[row] where given, else ctx_lens[i] + depth by tree_mask where
  * given, else ctx_lens[i] + j.  The arithmetic is fp32; results are rounded once.  Any other use of positions (several axes, scaled
  * frequencies) goes by the table.
- *   q [N_cap, H_q, D], k_new, v_new [N_cap, H_kv, D] dtype, rows apart by the strides; rows >= cu_q[B] are not used
+ *   q [N_cap, H_q, D], k_new, v_new [N_cap, H_kv, D] dtype, rows apart by the strides; rows in front of cu_q[0] and
+ *              from cu_q[B] on are not used
  *   cos_sin    [T, R] float32: the R/2 cosines of a position, then its sines
  *   positions  [N_cap] int32, nullable; tree_mask nullable; not both
- *   q_out      [N_cap, H_q, D] dtype, dense; may be q itself where q is dense; rows >= cu_q[B] are not written
+ *   q_out      [N_cap, H_q, D] dtype, dense; may be q itself where q is dense; those rows are not written
  *   caches, block_tables, ctx_lens, cu_q as for fsr_kv_append; positions without a page and page ids outside the pool are skipped
  * fsr_kv_append_rope_kv8: into 8-bit caches as fsr_kv_append_kv8 stores them (bf16 rows); a rotated key is rounded once, from fp32.
  * Pointers of rows, caches and cos_sin 16-byte aligned, no workspace.

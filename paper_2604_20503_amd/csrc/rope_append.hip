@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs a) {
     for (int s = 0; s < kAtOnce; ++s) fetch(lane_head + s * a.step, s);
 
     // all of this is the same for the whole workgroup
-    if (row >= uniform(a.cu_q[a.B])) return;
+    if (row < uniform(a.cu_q[0]) || row >= uniform(a.cu_q[a.B])) return;  // (offsets out of a longer list may begin anywhere)
     const int i = uniform(owner_by_wave(a.cu_q, a.B, row)), c = uniform(a.ctx[i]), j = row - uniform(a.cu_q[i]);
     const long long t = (long long)c + j;
     long long pos = t;
