@@ -356,7 +356,7 @@ int fsr_verify_attention_kv8_planned(const void* q, const void* k_cache, const v
  * bit for bit, to page block_tables[i * max_pages + t / P], slot t % P of the caches.  Call it
  * before fsr_verify_attention of the same rows (same stream).
  *
- *   k_new, v_new  [N_cap, H_kv, D] dtype; rows >= cu_q[B] are not read
+ *   k_new, v_new  [N_cap, H_kv, D] dtype; rows in front of cu_q[0] and from cu_q[B] on are not read
  *   k_cache, v_cache, block_tables, ctx_lens, cu_q and *p as for fsr_verify_attention (H_q, scale,
  *   out_dtype, max_q_len and flags are ignored; D * element size must be a multiple of 16)
  * Positions at or beyond max_pages * P and page ids outside [0, n_pages) are skipped.

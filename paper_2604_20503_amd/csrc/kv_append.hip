@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
     const long long vec_id = piece / per_vec;                   // (row, head)
     const int part = (int)(piece % per_vec);
     const int row = (int)(vec_id / a.H_kv), g = (int)(vec_id % a.H_kv);
-    if (row >= a.N_cap || row >= a.cu_q[a.B]) return;
+    if (row >= a.N_cap || row < a.cu_q[0] || row >= a.cu_q[a.B]) return;
     const int i = owner(a.cu_q, a.B, row);
     const long long t = (long long)a.ctx[i] + (row - a.cu_q[i]);
     if (t < 0 || t >= (long long)a.max_pages * a.P) return;     // no page for this position
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads) void kv_append8_kernel(Append8Args a) {
     const long long vec_id = piece / per_vec;
     const int part = (int)(piece % per_vec);
     const int row = (int)(vec_id / a.H_kv), g = (int)(vec_id % a.H_kv);
-    if (row >= a.N_cap || row >= a.cu_q[a.B]) return;
+    if (row >= a.N_cap || row < a.cu_q[0] || row >= a.cu_q[a.B]) return;
     const int i = owner(a.cu_q, a.B, row);
     const long long t = (long long)a.ctx[i] + (row - a.cu_q[i]);
     if (t < 0 || t >= (long long)a.max_pages * a.P) return;     // no page for this position

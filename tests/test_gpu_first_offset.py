@@ -55,3 +55,19 @@ def test_append_with_rotation(fsr, dtype, kv8):
     (out, *caches), (out_alone, *caches_alone) = results
     assert (out[:b["first"]] == 7).all() and torch.equal(out[b["first"]:], out_alone)
     assert all(torch.equal(x, y) for x, y in zip(caches, caches_alone))
+
+
+@pytest.mark.parametrize("dtype,kv8", [(BF, False), (F32, False), (BF, True)])
+def test_append(fsr, dtype, kv8):
+    announce(f"append, first offset {dtype} {kv8}")
+    b = batch(dtype, kv8)
+    results = []
+    for skip in (0, b["first"]):
+        k, v = (c.clone() for c in b["caches"])
+        if kv8:
+            fsr.kv_append_kv8(b["k"][skip:], b["v"][skip:], k, v, *b["scales"], b["bt"], b["ctx"], b["cu"] - skip)
+        else:
+            fsr.kv_append(b["k"][skip:], b["v"][skip:], k, v, b["bt"], b["ctx"], b["cu"] - skip)
+        torch.cuda.synchronize()
+        results.append([same_elsewhere(x, y, b["used"]) for x, y in zip(b["caches"], (k, v))])
+    assert all(torch.equal(x, y) for x, y in zip(*results))
