@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kWave) void tree_accept_kernel(AcceptArgs a) {
             a.emitted[out + count] = target[at];
         }
         ++count;
-        const int child = next[at];
+        const int child = __builtin_amdgcn_readfirstlane(next[at]);  // (read by the wave as one: the first lane writes there next)
         if (lane == 0) next[at] = -1;  // (on the path)
         if (child >= n || count > a.S_max) break;
         at = child;

@@ -6,6 +6,8 @@ import pytest
 import torch
 
 import workgroup_on_cpu
+from plain_attention import offsets
+from plain_tree import sees_of, tree, walk, words_of
 
 BF, F32 = torch.bfloat16, torch.float32
 ORDERS = [0, 1, 2, 3]  # of waves: ascending, descending, two shuffles
@@ -16,7 +18,7 @@ pytestmark = pytest.mark.skipif(not os.path.exists(workgroup_on_cpu.CLANG), reas
 
 @pytest.fixture(scope="module")
 def lib(tmp_path_factory):
-    lib = workgroup_on_cpu.build(str(tmp_path_factory.mktemp("kernels")), ["library.hip", "token_logprobs.hip"])
+    lib = workgroup_on_cpu.build(str(tmp_path_factory.mktemp("kernels")), ["library.hip", "token_logprobs.hip", "tree_accept.hip"])
     lib.fsr_last_error.restype = ctypes.c_char_p
     return lib
 
@@ -108,3 +110,28 @@ def test_one_logit_at_the_end_of_the_type(lib, at, order):
     z[0, at] = torch.finfo(F32).min
     lp, entropy, ids, top = token_logprobs(lib, z, torch.tensor([[at, (at + 1) % 3000]], dtype=torch.int32), 1)
     assert lp.tolist() == [[0.0, -float("inf")]] and entropy.tolist() == [0.0] and ids.tolist() == [[at]] and top.tolist() == [[0.0]]
+
+
+@pytest.mark.parametrize("S_max", [0, 2, 40])
+@pytest.mark.parametrize("sizes", [[12, 0, 1, 30], [64, 65, 130]], ids=str)
+def test_acceptance_of_trees(lib, sizes, S_max):
+    """Lanes one behind the other between the places where they wait for each other."""
+    from paper_2604_20503_amd.binding import TreeParams
+
+    lib.set_wave_order(0)
+    gen = torch.Generator().manual_seed(4)
+    B, N, cu, words = len(sizes), sum(sizes), offsets(sizes), 3
+    parents = [tree(n, gen, 0.6) if n else [] for n in sizes]
+    mask = torch.cat([words_of(sees_of(p), words) for p in parents if p])
+    draft, target = (torch.randint(0, 2, (N,), generator=gen, dtype=torch.int32) for _ in "dt")
+    accepted, emitted, path = (torch.full(s, -7, dtype=torch.int32) for s in ((2, B), (B, S_max + 1), (B, S_max + 1)))
+    keep = torch.full((N,), 9, dtype=torch.uint8)
+    p = TreeParams(B=B, N_cap=N, tree_words=words, S_max=S_max, reserved=0)
+    rc = lib.fsr_tree_accept(*(pointer(x) for x in (target, draft, mask, cu, accepted[0], accepted[1], emitted, path, keep)), ctypes.byref(p), None)
+    assert rc == 0, lib.fsr_last_error()
+    for i, parent in enumerate(parents):
+        a, b = int(cu[i]), int(cu[i + 1])
+        rows, tokens = walk(parent, draft[a:b].tolist(), target[a:b].tolist(), S_max)
+        pad = [-1] * (S_max + 1 - len(rows))
+        assert path[i].tolist() == rows + pad and emitted[i].tolist() == tokens + pad
+        assert accepted[:, i].tolist() == [len(rows) - 1, len(rows)] and keep[a:b].nonzero()[:, 0].tolist() == rows
