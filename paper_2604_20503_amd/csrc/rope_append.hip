@@ -17,7 +17,6 @@ namespace fsr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAtOnce = 1;          // heads of a thread that are loaded before the first is stored (with 2: 371 MB 84 us, not 78)
 constexpr int kMaxRows = 1 << 22;   // of a launch, a workgroup each
 
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4;
@@ -112,16 +111,15 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs a) {
             second = -1;
         }
     };
-    Eight<T> x[kAtOnce], y[kAtOnce];
-    auto fetch = [&](int h, int s) __attribute__((always_inline)) {
+    Eight<T> x, y;  // of one head: the next one's loads go out when it is stored (with two heads at once 371 MB took 84 us, not 78)
+    auto fetch = [&](int h) __attribute__((always_inline)) {
         if (idle || h >= heads) return;
         const T* at = h < a.H_q ? from_q + h * a.D : h < a.H_q + a.H_kv ? from_k + (h - a.H_q) * a.D : from_v + (h - a.H_q - a.H_kv) * a.D;
-        x[s].load(at + first);
-        if (second >= 0) y[s].load(at + second);
+        x.load(at + first);
+        if (second >= 0) y.load(at + second);
     };
     place_piece(lane);
-#pragma unroll
-    for (int s = 0; s < kAtOnce; ++s) fetch(lane_head + s * a.step, s);
+    fetch(lane_head);
 
     // all of this is the same for the whole workgroup
     if (row < uniform(a.cu_q[0]) || row >= uniform(a.cu_q[a.B])) return;  // (offsets out of a longer list may begin anywhere)
@@ -157,10 +155,9 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs a) {
         }
         if (piece != lane) {
             place_piece(piece);
-#pragma unroll
-            for (int s = 0; s < kAtOnce; ++s) fetch(lane_head + s * a.step, s);
+            fetch(lane_head);
         }
-        auto finish = [&](int h, int s) __attribute__((always_inline)) {
+        auto finish = [&](int h) __attribute__((always_inline)) {
             const bool is_q = h < a.H_q, is_k = !is_q && h < a.H_q + a.H_kv;
             const int g = is_q ? h : is_k ? h - a.H_q : h - a.H_q - a.H_kv;
             const bool turns = second >= 0 && (is_q || is_k);
@@ -168,8 +165,8 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs a) {
             if (turns) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float v = PAIRS ? (k < 4 ? x[s].get(2 * k) : y[s].get(2 * k - 8)) : x[s].get(k);
-                    const float z = PAIRS ? (k < 4 ? x[s].get(2 * k + 1) : y[s].get(2 * k - 7)) : y[s].get(k);
+                    const float v = PAIRS ? (k < 4 ? x.get(2 * k) : y.get(2 * k - 8)) : x.get(k);
+                    const float z = PAIRS ? (k < 4 ? x.get(2 * k + 1) : y.get(2 * k - 7)) : y.get(k);
                     const float turned = v * cosines.get(k) - z * sines.get(k), other = z * cosines.get(k) + v * sines.get(k);
                     if (!PAIRS) {
                         u[k] = turned;
@@ -188,8 +185,8 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs a) {
                 if (!turns) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        u[k] = x[s].get(k);
-                        w[k] = y[s].get(k);
+                        u[k] = x.get(k);
+                        w[k] = y.get(k);
                     }
                 }
                 Divisor scale;
@@ -207,21 +204,17 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs a) {
             } else if (is_q || stored) {
                 T* to = is_q ? to_q + g * a.D : (T*)(is_k ? a.k_cache : a.v_cache) + slot + g * head_step;
                 if (turns) {  // (what is only moved keeps its bits)
-                    x[s].set(u);
-                    y[s].set(w);
+                    x.set(u);
+                    y.set(w);
                 }
-                x[s].store(to + first);
-                if (second >= 0) y[s].store(to + second);
+                x.store(to + first);
+                if (second >= 0) y.store(to + second);
             }
         };
         for (int h = lane_head; h < heads;) {
-#pragma unroll
-            for (int s = 0; s < kAtOnce; ++s)
-                if (h + s * a.step < heads) finish(h + s * a.step, s);
-            h += kAtOnce * a.step;
-            if (h < heads)
-#pragma unroll
-                for (int s = 0; s < kAtOnce; ++s) fetch(h + s * a.step, s);
+            finish(h);
+            h += a.step;
+            fetch(h);
         }
     }
 }

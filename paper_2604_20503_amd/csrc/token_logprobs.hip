@@ -166,7 +166,6 @@ struct Shared {
     // used again would have to be cleared behind a barrier that every wave reaches after it has read it.
     int groups, keys, joined;
     int count[kThreads / kWave], last;
-    int chosen[FSR_TOP_MAX];
     uint64_t top[FSR_TOP_MAX];
     uint64_t list[kGroupsMax];
 };
