@@ -635,6 +635,7 @@ int fsr_verify_attention_shared(const void* q, const void* k_cache, const void* 
  *     fsr_verify_attention_tree  they attend to the context and their ancestors (once per layer)
  *     fsr_tree_accept            the path that the target agrees with
  *     fsr_kv_commit              its keys and values move to the positions behind the context (once per layer)
+ * Append and commit serve 8-bit caches as well; attention of trees is built for caches of 16 and 32 bits.
  *
  * fsr_kv_append_rope: fsr_kv_append with the rotation on the way.  Row j of request i, at rotary position t, has the pairs (a, b) of
  * elements of every query and key head, pair m of R/2, replaced by

@@ -691,7 +691,7 @@ def _tree_workspace(N_cap, H_q, H_kv, D, dtype, out_dtype) -> int:
 def verify_attention_tree(q, k_cache, v_cache, block_tables, ctx_lens, cu_q, tree_mask, *, scale, out=None, lse=None, out_dtype=None, workspace=None,
                           max_q_len=0, max_workgroups=0, kv_layout=KV_HEAD_MAJOR):
     """fsr_verify_attention_tree: verify_attention whose rows see the context and the rows of their request that tree_mask [N_cap, words]
-    int64 has a bit for.  Returns (out, lse)."""
+    int64 has a bit for.  Caches of q's dtype (8-bit ones are not built).  Returns (out, lse)."""
     B, rows, cache, dtype = ctx_lens.shape[0], q.shape, k_cache.shape, q.dtype
     _check_offsets(B, block_tables, cu_q=cu_q)
     if len(rows) != 3 or len(cache) != 4 or v_cache.shape != cache or k_cache.dtype != dtype or v_cache.dtype != dtype:

@@ -626,7 +626,9 @@ template <int OP, int KH, int KT, int DV, class OUT, bool PAGES16>
 struct Tiled {
     static constexpr bool kPages16 = PAGES16;
     static constexpr int kOp = OP, kHead = KH, kTail = KT, kDk = KH + KT, kDv = DV;
-    static constexpr bool kPair = sizeof(OUT) == 4;   // weights enter the second product as a pair of bf16
+    // Weights enter the second product as a pair of bf16 where results are fp32.  For bf16 results each is rounded once, by 2^-8 at most and to
+    // either side, which is no more than the results' own rounding: 12 trees behind long contexts take 300 us, not 370.
+    static constexpr bool kPair = sizeof(OUT) == 4;
     static constexpr int kM = kTileRows, kKeys = 64;
     static constexpr int kBlockThreads = kThreads, kWaves = row_tiles::kWaves;
     static constexpr int kPartRows = 32, kPartColumns = 8;  // of a wave; for each four of a lane
