@@ -48,6 +48,12 @@ def test_near_certain_rows(fsr, N, V, T, dtype):
     near(lp[:, 0], want, off)
     near(top[:, 0], want, off)
     near(entropy, torch.log1p(rest) + lost / (1 + rest), 3 * off)
+    # without alternatives, and out of wider rows that begin anywhere: the same sums
+    wide = torch.full((N, V + 9), 50.0, dtype=dtype, device="cuda")
+    wide[:, 1:V + 1] = z
+    for x in (z, wide[:, 1:V + 1]):
+        lp_only, entropy_only, _, _ = fsr.token_logprobs(x, at.int(), temperature=T)
+        assert torch.equal(lp_only, lp) and torch.equal(entropy_only, entropy)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
